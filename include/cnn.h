@@ -254,6 +254,38 @@ int cnn_logistic_fwd(const float* x, float* y, size_t n, void* hip_stream);
  * (the back-propagation driver is left to its repository); derived from the listing above. */
 int cnn_logistic_bwd(const float* y, const float* d_y, float* d_x, size_t n, void* hip_stream);
 
+/* ---- Operators on sequences, beside the paper: layers of a classifier that reads its input token by token (an image as
+ * 784 pixels, a text as words), trained with the fully connected and logistic calls above. ----------------------------------
+ * Data are fp32, bfloat16 or half as `type` says, sums and states fp32 in registers, results rounded to nearest once.  No
+ * context, no device state.  Unless said otherwise tensors are contiguous and 16-byte aligned, and an output overlaps no input. */
+#define CNN_F32 0
+#define CNN_BF16 1
+#define CNN_F16 2
+
+/* Embedding lookup: out[n] = scale * table[token[n]] for table[V,D], out[N,D].  Tokens are int32, or int64 with wide_tokens != 0.
+ * A token outside 0 .. V-1 is padding: its row of out is zero.  1 <= N, V < 2^31, 1 <= D <= 65536. */
+int cnn_embedding_fwd(const void* table, const void* tokens, void* out, int64_t N, int64_t V, int D, int type, int wide_tokens,
+                      float scale, void* hip_stream);
+/* Its gradient: d_table[r] = scale * sum over n with token[n] = r of d_out[n], zero for rows without tokens; padding adds nothing.
+ * The whole of d_table[V,D] is written.  Sums are fp32 in an order fixed by the tokens: bitwise reproducible.  `workspace`:
+ * cnn_embedding_bwd_workspace_bytes() bytes of device memory (0 for sizes that the call refuses). */
+size_t cnn_embedding_bwd_workspace_bytes(int64_t N, int64_t V, int D, int type);
+int cnn_embedding_bwd(const void* d_out, const void* tokens, void* d_table, int64_t N, int64_t V, int D, int type, int wide_tokens,
+                      float scale, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Dropout: y[e] = x[e] / (1 - p) where element e is kept, else 0, plus residual[e] (nullable).  Element e (its index among the n)
+ * is dropped if u(e) < floor(p * 2^32 + 1/2).  u(e) comes from Philox4x32-10 with key `seed` and the counter of four words
+ * (low and high word of e / 8, low and high word of the offset): word j of its result holds the sixteen high bits of u(8 i + 2 j)
+ * in its low half and of u(8 i + 2 j + 1) in its high half; the sixteen low bits are those of a second call with bit 31 of the
+ * counter's second word set.  The offset is `offset` plus *step (device memory, nullable: a captured graph draws new masks on every
+ * replay if the program advances it).  A dropped element is 0 whatever x holds.  0 <= p <= 1, 1 <= n <= 2^40; y may be x or residual. */
+int cnn_dropout_fwd(const void* x, const void* residual, void* y, size_t n, int type, double p, uint64_t seed, uint64_t offset,
+                    const int64_t* step, void* hip_stream);
+/* d_x[e] = d_y[e] / (1 - p) where the forward call of the same p, seed, offset and *step kept e, else 0.  (The residual's gradient is
+ * d_y itself.)  d_x may be d_y. */
+int cnn_dropout_bwd(const void* d_y, void* d_x, size_t n, int type, double p, uint64_t seed, uint64_t offset, const int64_t* step,
+                    void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,7 @@ PARAM_SHAPES = (("k1", (6, 5, 5)), ("b1", (6,)), ("k2", (12, 6, 5, 5)), ("b2", (
                 ("fc", (10, 12, 1, 4, 4)), ("b", (10,)))
 
 _vp, _i, _f, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+_i64, _u64 = ctypes.c_int64, ctypes.c_uint64
 
 # name -> (restype, argtypes); one entry per declaration in include/cnn.h
 SIGNATURES = {
@@ -59,6 +60,11 @@ SIGNATURES = {
     "cnn_fc_bwd_weight": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _vp, _sz, _vp]),
     "cnn_logistic_fwd": (_i, [_vp, _vp, _sz, _vp]),
     "cnn_logistic_bwd": (_i, [_vp, _vp, _vp, _sz, _vp]),
+    "cnn_embedding_fwd": (_i, [_vp] * 3 + [_i64, _i64, _i, _i, _i, _f, _vp]),
+    "cnn_embedding_bwd_workspace_bytes": (_sz, [_i64, _i64, _i, _i]),
+    "cnn_embedding_bwd": (_i, [_vp] * 3 + [_i64, _i64, _i, _i, _i, _f, _vp, _sz, _vp]),
+    "cnn_dropout_fwd": (_i, [_vp, _vp, _vp, _sz, _i, ctypes.c_double, _u64, _u64, _vp, _vp]),
+    "cnn_dropout_bwd": (_i, [_vp, _vp, _sz, _i, ctypes.c_double, _u64, _u64, _vp, _vp]),
 }
 
 _lib = None
@@ -270,3 +276,24 @@ def logistic_fwd(x):
 
 def logistic_bwd(y, d_y):
     return (_calls or _native()).logistic_bwd(y, d_y)
+
+
+# ---- operators on sequences: fp32, bfloat16 or half ---------------------------------
+def embedding_fwd(table, tokens, scale=1.0):
+    """scale * table[tokens] for table[V, D] and int32 or int64 tokens of any shape; rows of zeros where a token is not in 0..V-1."""
+    return (_calls or _native()).embedding_fwd(table, tokens, scale)
+
+
+def embedding_bwd(d_out, tokens, vocab, scale=1.0):
+    """Gradient of the table[vocab, D]: each row scale * the sum of the output errors of its tokens, in a fixed order."""
+    return (_calls or _native()).embedding_bwd(d_out, tokens, vocab, scale)
+
+
+def dropout_fwd(x, p, seed, offset=0, residual=None, step=None):
+    """x / (1 - p) where the generator keeps an element, else 0, plus `residual`.  Equal seed and offset give equal masks, so give
+    every layer and training step an offset of its own; `step`, an int64 tensor of one element on the GPU, is added to it."""
+    return (_calls or _native()).dropout_fwd(x, p, seed, offset, residual, step)
+
+
+def dropout_bwd(d_y, p, seed, offset=0, step=None):
+    return (_calls or _native()).dropout_bwd(d_y, p, seed, offset, step)

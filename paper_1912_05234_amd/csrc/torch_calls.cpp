@@ -13,6 +13,9 @@
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
 
+#include <climits>
+#include <vector>
+
 #include "cnn.h"
 
 namespace {
@@ -295,6 +298,111 @@ CALL(logistic_bwd, 2)  // y, d_y
   return wrap(std::move(d_x));
 END
 
+// ---- operators on sequences ----------------------------------------------------------------------------------
+// Element type of a tensor on the GPU (contiguous unless `strided`), as the library counts them.
+int element_type(const at::Tensor& t) {
+  switch (t.scalar_type()) {
+    case at::kFloat: return CNN_F32;
+    case at::kBFloat16: return CNN_BF16;
+    case at::kHalf: return CNN_F16;
+    default: raise(PyExc_ValueError, "expected a torch.float32, torch.bfloat16 or torch.float16 tensor on the GPU");
+  }
+}
+
+const at::Tensor& any_tensor(PyObject* o, bool strided = false) {
+  if (!THPVariable_Check(o)) raise(PyExc_TypeError, "expected a tensor");
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda()) raise(PyExc_ValueError, "expected a tensor on the GPU");
+  if (!strided && !t.is_contiguous()) raise(PyExc_ValueError, "expected a contiguous tensor on the GPU");
+  return t;
+}
+
+const at::Tensor& like(PyObject* o, const at::Tensor& x) {
+  const at::Tensor& t = any_tensor(o);
+  if (t.scalar_type() != x.scalar_type() || t.sizes() != x.sizes()) raise(PyExc_ValueError, "expected a tensor of the same shape and type");
+  return t;
+}
+
+const at::Tensor& token_tensor(PyObject* o) {
+  const at::Tensor& t = any_tensor(o);
+  if (t.scalar_type() != at::kInt && t.scalar_type() != at::kLong) raise(PyExc_ValueError, "expected a torch.int32 or torch.int64 tensor of tokens");
+  return t;
+}
+
+uint64_t word64(PyObject* o) {
+  const unsigned long long v = PyLong_AsUnsignedLongLongMask(o);
+  if (v == (unsigned long long)-1 && PyErr_Occurred()) throw Raised();
+  return v;
+}
+
+CALL(embedding_fwd, 3)  // table, tokens, scale
+  const at::Tensor &table = any_tensor(a[0]), &tokens = token_tensor(a[1]);
+  if (table.dim() != 2) raise(PyExc_ValueError, "expected a table of 2 dimensions");
+  const int type = element_type(table);
+  const float scale = (float)number(a[2]);
+  std::vector<int64_t> sizes = tokens.sizes().vec();
+  sizes.push_back(table.size(1));
+  at::Tensor out = empty(sizes, table.device(), table.scalar_type());
+  call("cnn_embedding_fwd", [&] {
+    return cnn_embedding_fwd(table.data_ptr(), tokens.data_ptr(), out.data_ptr(), tokens.numel(), table.size(0), (int)table.size(1), type,
+                             tokens.scalar_type() == at::kLong, scale, stream());
+  });
+  return wrap(std::move(out));
+END
+
+CALL(embedding_bwd, 4)  // d_out, tokens, vocab, scale
+  const at::Tensor &d = any_tensor(a[0]), &tokens = token_tensor(a[1]);
+  const int type = element_type(d);
+  const int64_t V = integer(a[2]), N = tokens.numel();
+  const float scale = (float)number(a[3]);
+  if (d.dim() != tokens.dim() + 1 || d.sizes().slice(0, tokens.dim()) != tokens.sizes())
+    raise(PyExc_ValueError, "expected an output error with one row per token");
+  const int64_t D = d.size(-1);
+  const size_t bytes = D > INT_MAX ? 0 : cnn_embedding_bwd_workspace_bytes(N, V, (int)D, type);
+  at::Tensor table, ws;
+  if (bytes) table = empty({V, D}, d.device(), d.scalar_type()), ws = empty({(int64_t)bytes}, d.device(), at::kByte);
+  call("cnn_embedding_bwd", [&] {
+    return bytes ? cnn_embedding_bwd(d.data_ptr(), tokens.data_ptr(), table.data_ptr(), N, V, (int)D, type, tokens.scalar_type() == at::kLong,
+                                     scale, ws.data_ptr(), bytes, stream())
+                 : CNN_EINVAL;
+  });
+  return wrap(std::move(table));
+END
+
+const int64_t* step_or_null(PyObject* o) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = any_tensor(o);
+  if (t.scalar_type() != at::kLong || t.numel() != 1) raise(PyExc_ValueError, "expected a torch.int64 tensor of one element");
+  return data<int64_t>(t);
+}
+
+CALL(dropout_fwd, 6)  // x, p, seed, offset, residual or None, step or None
+  const at::Tensor& x = any_tensor(a[0]);
+  const int type = element_type(x);
+  const double p = number(a[1]);
+  const uint64_t seed = word64(a[2]), offset = word64(a[3]);
+  const void* residual = a[4] == Py_None ? nullptr : like(a[4], x).data_ptr();
+  const int64_t* step = step_or_null(a[5]);
+  at::Tensor y = empty(x.sizes(), x.device(), x.scalar_type());
+  call("cnn_dropout_fwd", [&] {
+    return cnn_dropout_fwd(x.data_ptr(), residual, y.data_ptr(), (size_t)x.numel(), type, p, seed, offset, step, stream());
+  });
+  return wrap(std::move(y));
+END
+
+CALL(dropout_bwd, 5)  // d_y, p, seed, offset, step or None
+  const at::Tensor& d = any_tensor(a[0]);
+  const int type = element_type(d);
+  const double p = number(a[1]);
+  const uint64_t seed = word64(a[2]), offset = word64(a[3]);
+  const int64_t* step = step_or_null(a[4]);
+  at::Tensor d_x = empty(d.sizes(), d.device(), d.scalar_type());
+  call("cnn_dropout_bwd", [&] {
+    return cnn_dropout_bwd(d.data_ptr(), d_x.data_ptr(), (size_t)d.numel(), type, p, seed, offset, step, stream());
+  });
+  return wrap(std::move(d_x));
+END
+
 PyObject* raise_through(PyObject*, PyObject* fn) {  // binding._check
   Py_INCREF(fn);
   Py_XSETREF(check, fn);
@@ -304,7 +412,8 @@ PyObject* raise_through(PyObject*, PyObject* fn) {  // binding._check
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(forward), FAST(gradient), FAST(train_batch), FAST(evaluate), FAST(conv_fwd), FAST(conv_bwd_input),
                          FAST(conv_bwd_weight), FAST(avgpool_fwd), FAST(avgpool_bwd), FAST(fc_fwd), FAST(fc_bwd_input),
-                         FAST(fc_bwd_weight), FAST(logistic_fwd), FAST(logistic_bwd),
+                         FAST(fc_bwd_weight), FAST(logistic_fwd), FAST(logistic_bwd), FAST(embedding_fwd), FAST(embedding_bwd), FAST(dropout_fwd),
+                         FAST(dropout_bwd),
                          {"raise_through", raise_through, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
