@@ -286,6 +286,44 @@ int cnn_dropout_fwd(const void* x, const void* residual, void* y, size_t n, int 
 int cnn_dropout_bwd(const void* d_y, void* d_x, size_t n, int type, double p, uint64_t seed, uint64_t offset, const int64_t* step,
                     void* hip_stream);
 
+/* Linear attention with a decay a for each head: for every sequence and query head a state S[Dk,Dv] (fp32)
+ *   S_t = a S_{t-1} + k_t v_t^T,   o_t = scale * S_t^T q_t,   t = 0 .. length - 1.
+ * H query heads; Hk key and value heads, H a multiple of Hk, each used by H / Hk consecutive query heads.  Dk, Dv <= 256,
+ * B * H <= 2^20.  q, k, v (and d_o) are given with their strides, in elements, none negative, and need only be aligned to their
+ * element: slices of one projection's output serve as they are.  (Rows of whole packs of eight elements, all at multiples of 16
+ * bytes, are read sixteen bytes at a time, others element by element.)  Results are contiguous: [B,T,heads,width] and
+ * [B,H,Dk,Dv].  decay[H]: 0 <= a <= 1, not checked on the device; constants of the operator, without a gradient.
+ * lengths[B] (nullable: all T; below 0 counts as 0, above T as T): tokens past a sequence's length are not read, and their rows of
+ * the results are zero.  Inputs up to it must be finite and below 2^127.  An initial or final state may be NULL (zero; not wanted);
+ * they may be the same memory.  `workspace` holds states of pieces of the sequences where there are too few heads to fill the GPU,
+ * and the gradients of shared heads; the size queries return 0 where none is needed, and for refused shapes. */
+typedef struct {
+  int B, T, H, Hk, Dk, Dv, type;
+} cnn_linear_shape;
+typedef struct {
+  const void* data; /* element (b, t, h, d) at b * batch + t * token + h * head + d */
+  int64_t batch, token, head;
+} cnn_heads;
+size_t cnn_linear_attention_fwd_workspace_bytes(const cnn_linear_shape* shape);
+int cnn_linear_attention_fwd(const cnn_linear_shape* shape, const cnn_heads* q, const cnn_heads* k, const cnn_heads* v,
+                             const float* decay, float scale, const int32_t* lengths, const float* initial_state, void* o,
+                             float* final_state, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Gradients for the error d_o of o and (nullable) d_final_state of the final state: d_q, d_k, d_v and (nullable) d_initial_state.
+ * With G_t the error of S_t: G_t = scale q_t d_o_t^T + a G_{t+1} (d_final_state past the end), d_q_t = scale S_t d_o_t,
+ * d_k_t = G_t v_t, d_v_t = G_t^T k_t, summed over the query heads of a shared head; d_initial_state = a G_0, or d_final_state for a
+ * sequence of length 0; it must not be the memory of an input.  With a state's error given or wanted, 2^-100 <= |scale| <= 2^100. */
+size_t cnn_linear_attention_bwd_workspace_bytes(const cnn_linear_shape* shape);
+int cnn_linear_attention_bwd(const cnn_linear_shape* shape, const cnn_heads* q, const cnn_heads* k, const cnn_heads* v,
+                             const float* decay, const cnn_heads* d_o, float scale, const int32_t* lengths,
+                             const float* initial_state, const float* d_final_state, void* d_q, void* d_k, void* d_v,
+                             float* d_initial_state, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* One token of every sequence (T = 1, token strides unused): the state is updated in place, o[B,H,Dv].  state[pool,H,Dk,Dv];
+ * row b uses state slots[b] (nullable: state b, then pool >= B).  A slot outside 0 .. pool-1 marks a row without a sequence: its o
+ * is zero and no state changes.  No two rows may have the same slot. */
+int cnn_linear_attention_step(const cnn_linear_shape* shape, const cnn_heads* q, const cnn_heads* k, const cnn_heads* v,
+                              const float* decay, float scale, float* state, int64_t pool, const int32_t* slots, void* o,
+                              void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

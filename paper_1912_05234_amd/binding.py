@@ -67,6 +67,27 @@ SIGNATURES = {
     "cnn_dropout_bwd": (_i, [_vp, _vp, _sz, _i, ctypes.c_double, _u64, _u64, _vp, _vp]),
 }
 
+
+
+class LinearShape(ctypes.Structure):
+    """cnn_linear_shape"""
+    _fields_ = [(name, _i) for name in ("B", "T", "H", "Hk", "Dk", "Dv", "type")]
+
+
+class Heads(ctypes.Structure):
+    """cnn_heads"""
+    _fields_ = [("data", _vp), ("batch", _i64), ("token", _i64), ("head", _i64)]
+
+
+_shape, _heads = ctypes.POINTER(LinearShape), ctypes.POINTER(Heads)
+SIGNATURES.update({
+    "cnn_linear_attention_fwd_workspace_bytes": (_sz, [_shape]),
+    "cnn_linear_attention_fwd": (_i, [_shape] + [_heads] * 3 + [_vp, _f] + [_vp] * 5 + [_sz, _vp]),
+    "cnn_linear_attention_bwd_workspace_bytes": (_sz, [_shape]),
+    "cnn_linear_attention_bwd": (_i, [_shape] + [_heads] * 3 + [_vp, _heads, _f] + [_vp] * 8 + [_sz, _vp]),
+    "cnn_linear_attention_step": (_i, [_shape] + [_heads] * 3 + [_vp, _f, _vp, _i64, _vp, _vp, _vp]),
+})
+
 _lib = None
 _calls = None
 
@@ -297,3 +318,22 @@ def dropout_fwd(x, p, seed, offset=0, residual=None, step=None):
 
 def dropout_bwd(d_y, p, seed, offset=0, step=None):
     return (_calls or _native()).dropout_bwd(d_y, p, seed, offset, step)
+
+
+def linear_attention_fwd(q, k, v, decay, scale=1.0, lengths=None, initial_state=None, want_state=False):
+    """(o[B, T, H, Dv], final state [B, H, Dk, Dv] fp32 or None) of S_t = decay S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t, for
+    q[B, T, H, Dk], k[B, T, Hk, Dk], v[B, T, Hk, Dv] of any strides but the last, decay[H] fp32 and lengths[B] int32 (None: all T)."""
+    return (_calls or _native()).linear_attention_fwd(q, k, v, decay, scale, lengths, initial_state, bool(want_state))
+
+
+def linear_attention_bwd(q, k, v, decay, d_o, scale=1.0, lengths=None, initial_state=None, d_final_state=None, want_d_state=False):
+    """(d_q, d_k, d_v, error of the initial state or None) of the call above with the same arguments."""
+    (d_q, d_k), (d_v, d_state) = (_calls or _native()).linear_attention_bwd(q, k, v, decay, scale, d_o, lengths, initial_state, d_final_state,
+                                                                           bool(want_d_state))
+    return d_q, d_k, d_v, d_state
+
+
+def linear_attention_step(q, k, v, decay, state, scale=1.0, slots=None):
+    """o[B, H, Dv] of one token of every sequence, q[B, H, Dk], k[B, Hk, Dk], v[B, Hk, Dv]; state[pool, H, Dk, Dv] fp32 is updated in
+    place, row b using state slots[b] (int32; None: state b).  A slot outside the pool: a row without a sequence, its o is zero."""
+    return (_calls or _native()).linear_attention_step(q, k, v, decay, scale, state, slots)

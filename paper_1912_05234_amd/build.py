@@ -8,6 +8,8 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -54,9 +56,16 @@ def build_calls(verbose=False):
 
 
 def build(verbose=False, extra=()):
+    """Compiles the sources side by side, one hipcc each, and links them."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    run([LIB, hipcc] + HIPCC_FLAGS + list(extra) +
-        ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(PKG, "csrc")] + sources(), verbose)
+    include = ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(PKG, "csrc")]
+    jobs = int(os.environ.get("MAX_JOBS", "0")) or min(8, os.cpu_count() or 1)
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in sources()]
+        compile_one = lambda s, o: run([o, hipcc] + [f for f in HIPCC_FLAGS if f != "-shared"] + list(extra) + include + ["-c", s], verbose)  # noqa: E731
+        with ThreadPoolExecutor(jobs) as pool:
+            list(pool.map(compile_one, sources(), objects))
+        run([LIB, hipcc] + HIPCC_FLAGS + list(extra) + objects, verbose)
     build_calls(verbose)
     return LIB
 

@@ -1,0 +1,295 @@
+// Entry points of linear attention, its form for single tokens, and the kernels around the scan of cnn_linear.h.
+#include "cnn_linear.h"
+
+namespace cnn {
+namespace linear {
+namespace {
+
+// ---- states of the segments --------------------------------------------------------------------------------------------
+// carry[unit][j] holds what segment j adds to a state; afterwards the state that segment j starts from.
+constexpr int CARRY_THREADS = 256;
+__global__ __launch_bounds__(CARRY_THREADS) void carry_kernel(Args args) {
+  const Role& R = args.role[blockIdx.y];
+  const int64_t size = (int64_t)R.DK * R.DV, groups = (size + CARRY_THREADS - 1) / CARRY_THREADS;
+  const int64_t unit = blockIdx.x / groups, at = blockIdx.x % groups * CARRY_THREADS + threadIdx.x;
+  if (unit >= args.units || at >= size) return;
+  const int64_t batch = unit / args.heads, asked = args.lengths ? args.lengths[batch] : args.T;
+  const int64_t n = asked < 0 ? 0 : asked < args.T ? asked : args.T;
+  const float a = args.decay[unit % args.heads];
+  const double log2a = log2((double)a);
+  const auto power_of = [&](int64_t e) { return e > 0 ? (float)exp2(log2a * (double)e) : 1.0f; };
+  const float raw = R.first ? R.first[unit * size + at / R.DV * R.first_i + at % R.DV * R.first_j] : 0.0f;
+  float run = raw * R.first_by;
+  float* carry = R.carry + unit * args.segments * size + at;
+  const float full = power_of(args.segment_length);
+  for (int j = 0; j < args.segments; ++j) {
+    const int64_t left = n - j * args.segment_length;
+    const float added = carry[j * size];
+    carry[j * size] = run;
+    if (left <= 0) continue;
+    const int64_t count = left < args.segment_length ? left : args.segment_length;
+    const float by = j == 0 && R.reversed ? power_of(count - 1) : count == args.segment_length ? full : power_of(count);
+    run = run * by + added;
+  }
+  if (R.last) R.last[unit * size + at] = n == 0 ? raw : run * (R.last_by * (R.reversed ? a : 1.0f));
+}
+
+// ---- gradients of shared heads -----------------------------------------------------------------------------------------
+// out[row][h][d] = sum over the query heads of h of part[row][head][d], part in fp32.
+template <class T>
+__global__ __launch_bounds__(256) void share_kernel(const float* part, T* out, int64_t total, int share, int width) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const float* p = part + i / width * share * width + i % width;
+    float s = 0.0f;
+    for (int h = 0; h < share; ++h) s += p[(int64_t)h * width];
+    out[i] = (T)s;
+  }
+}
+
+// ---- one token ---------------------------------------------------------------------------------------------------------
+struct StepArgs {
+  Operand q, k, v;
+  const float* decay;
+  float* state;          // [pool][heads][DK][DV]
+  const int32_t* slots;  // [batch], nullable: row b uses state b
+  void* out;             // [batch][heads][DV]
+  int64_t pool;
+  int heads, DK, DV, blocks;
+  float scale;
+};
+
+constexpr int STEP_THREADS = 256, STEP_COLUMNS = 32;
+
+// A workgroup takes 32 columns of one state: the whole of DK, so that nothing has to be joined outside it.  Every thread
+// updates VN columns of one row in so many, and keeps their products with q; these are added over the rows at the end.
+template <class T, int VN>
+__global__ __launch_bounds__(STEP_THREADS) void step_kernel(StepArgs a) {
+  constexpr int LANES = STEP_COLUMNS / VN, ROWS = STEP_THREADS / LANES, AHEAD = 4;
+  using P = Pack<float, VN>;
+  __shared__ float sums[STEP_THREADS / 64][STEP_COLUMNS];
+  const int64_t job = blockIdx.x / a.blocks, batch = job / a.heads;
+  const int head = (int)(job % a.heads), lane = threadIdx.x % LANES, row0 = threadIdx.x / LANES;
+  const int col = (int)(blockIdx.x % a.blocks) * STEP_COLUMNS + lane * VN;
+  const int64_t slot = a.slots ? a.slots[batch] : batch;
+  T* out = static_cast<T*>(a.out) + job * a.DV;
+  const bool mine = col < a.DV;
+  if (slot < 0 || slot >= a.pool) {  // no sequence here
+    if (threadIdx.x < LANES && mine)
+#pragma unroll
+      for (int j = 0; j < VN; ++j) out[col + j] = (T)0.0f;
+    return;
+  }
+  const auto base = [&](const Operand& o) { return static_cast<const T*>(o.data) + batch * o.batch + head / o.share * o.head; };
+  const T *q = base(a.q), *k = base(a.k), *v = base(a.v);
+  float* state = a.state + (slot * a.heads + head) * a.DK * a.DV;
+  const float decay = a.decay[head];
+  float value[VN], sum[VN];
+#pragma unroll
+  for (int j = 0; j < VN; ++j) value[j] = mine ? (float)v[col + j] : 0.0f, sum[j] = 0.0f;
+  for (int i = row0; i < a.DK; i += ROWS * AHEAD) {
+    P s[AHEAD];
+    float key[AHEAD], query[AHEAD];
+#pragma unroll
+    for (int r = 0; r < AHEAD; ++r) {
+      const int row = i + r * ROWS;
+      if (row >= a.DK || !mine) continue;
+      s[r] = *reinterpret_cast<const P*>(state + (int64_t)row * a.DV + col);
+      key[r] = (float)k[row], query[r] = (float)q[row];
+    }
+#pragma unroll
+    for (int r = 0; r < AHEAD; ++r) {
+      const int row = i + r * ROWS;
+      if (row >= a.DK || !mine) continue;
+#pragma unroll
+      for (int j = 0; j < VN; ++j) {
+        s[r].v[j] = s[r].v[j] * decay + key[r] * value[j];
+        sum[j] += query[r] * s[r].v[j];
+      }
+      *reinterpret_cast<P*>(state + (int64_t)row * a.DV + col) = s[r];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < VN; ++j) {
+#pragma unroll
+    for (int d = LANES; d < 64; d *= 2) sum[j] += __shfl_xor(sum[j], d);
+    if (threadIdx.x % 64 < LANES) sums[threadIdx.x / 64][lane * VN + j] = sum[j];
+  }
+  __syncthreads();
+  if (threadIdx.x < STEP_COLUMNS) {
+    const int c = (int)(blockIdx.x % a.blocks) * STEP_COLUMNS + threadIdx.x;
+    float s = 0.0f;
+    for (int w = 0; w < STEP_THREADS / 64; ++w) s += sums[w][threadIdx.x];
+    if (c < a.DV) out[c] = (T)(s * a.scale);
+  }
+}
+
+// ---- arguments and plans ---------------------------------------------------------------------------------------------------
+bool shape_ok(const cnn_linear_shape* s) {
+  return s && s->B >= 1 && s->T >= 1 && s->H >= 1 && s->Hk >= 1 && s->H % s->Hk == 0 && s->Dk >= 1 && s->Dk <= 256 && s->Dv >= 1 &&
+         s->Dv <= 256 && type_known(s->type) && (int64_t)s->B * s->H <= 1 << 20;
+}
+
+bool heads_ok(const cnn_heads* h, int type) {
+  return h && h->data && reinterpret_cast<uintptr_t>(h->data) % type_bytes(type) == 0 && h->batch >= 0 && h->token >= 0 && h->head >= 0;
+}
+
+// Rows made of whole packs at aligned addresses, whatever token, head and sequence.
+bool packed_ok(const cnn_heads* h, int width, int type) {
+  const int64_t unit = 16 / (int64_t)type_bytes(type);
+  return aligned16(h->data) && width % 8 == 0 && h->batch % unit == 0 && h->token % unit == 0 && h->head % unit == 0;
+}
+
+Operand operand_of(const cnn_heads* h, int share) { return {h->data, h->batch, h->token, h->head, share}; }
+
+struct Plan {
+  int segments;
+  int64_t length;
+  size_t state_bytes;  // of one role's states, all segments
+  size_t wide_k, wide_v, bytes;
+};
+
+size_t rounded(size_t b) { return (b + 255) & ~(size_t)255; }
+
+constexpr int64_t JOBS = 512, SEGMENT = 256;  // workgroups wanted; tokens to a segment, at least
+
+Plan plan_of(const cnn_linear_shape& s, int roles) {
+  Plan p{};
+  const int64_t units = (int64_t)s.B * s.H;
+  const auto blocks = [](int dk, int dv) { return (dv + block_columns(dk, dv) - 1) / block_columns(dk, dv); };
+  const int64_t jobs = roles == 1 ? units * blocks(s.Dk, s.Dv) : units * (blocks(s.Dk, s.Dv) + 2 * blocks(s.Dv, s.Dk));
+  int64_t n = (JOBS + jobs - 1) / jobs, most = s.T / SEGMENT;
+  n = n < most ? n : most;
+  n = n < 1 ? 1 : n;
+  p.length = ((s.T + n - 1) / n + 63) / 64 * 64;
+  p.segments = (int)((s.T + p.length - 1) / p.length);
+  p.state_bytes = p.segments > 1 ? rounded((size_t)units * p.segments * s.Dk * s.Dv * 4) : 0;
+  p.bytes = p.state_bytes * roles;
+  if (roles > 1 && s.H != s.Hk) {
+    p.wide_k = p.bytes;
+    p.wide_v = p.wide_k + rounded((size_t)units * s.T * s.Dk * 4);
+    p.bytes = p.wide_v + rounded((size_t)units * s.T * s.Dv * 4);
+  }
+  return p;
+}
+
+Args args_of(const cnn_linear_shape& s, const Plan& p, const float* decay, const int32_t* lengths) {
+  Args a{};
+  a.decay = decay, a.lengths = lengths;
+  a.units = (int64_t)s.B * s.H, a.T = s.T, a.segment_length = p.length;
+  a.heads = s.H, a.segments = p.segments;
+  return a;
+}
+
+int run(Args& a, int type, int roles, hipStream_t st) {
+  const auto scan = type == CNN_F32 ? run_scan_f32 : type == CNN_BF16 ? run_scan_bf16 : run_scan_f16;
+  for (int r = 0; r < roles; ++r) a.role[r].blocks = (a.role[r].DV + block_columns(a.role[r].DK, a.role[r].DV) - 1) / block_columns(a.role[r].DK, a.role[r].DV);
+  if (a.segments > 1) {
+    const int rc = scan(a, roles, true, st);
+    if (rc != CNN_OK) return rc;
+    const int64_t groups = ((int64_t)a.role[0].DK * a.role[0].DV + CARRY_THREADS - 1) / CARRY_THREADS;
+    carry_kernel<<<dim3((unsigned)(a.units * groups), (unsigned)roles), CARRY_THREADS, 0, st>>>(a);
+    if (launch_status() != CNN_OK) return CNN_EHIP;
+  }
+  return scan(a, roles, false, st);
+}
+
+}  // namespace
+}  // namespace linear
+}  // namespace cnn
+
+extern "C" {
+
+size_t cnn_linear_attention_fwd_workspace_bytes(const cnn_linear_shape* s) { return cnn::linear::shape_ok(s) ? cnn::linear::plan_of(*s, 1).bytes : 0; }
+
+size_t cnn_linear_attention_bwd_workspace_bytes(const cnn_linear_shape* s) { return cnn::linear::shape_ok(s) ? cnn::linear::plan_of(*s, 3).bytes : 0; }
+
+int cnn_linear_attention_fwd(const cnn_linear_shape* s, const cnn_heads* q, const cnn_heads* k, const cnn_heads* v, const float* decay,
+                             float scale, const int32_t* lengths, const float* initial_state, void* o, float* final_state, void* workspace,
+                             size_t workspace_bytes, void* hip_stream) {
+  using namespace cnn;
+  using namespace cnn::linear;
+  if (!shape_ok(s) || !heads_ok(q, s->type) || !heads_ok(k, s->type) || !heads_ok(v, s->type) || !decay || !o) return CNN_EINVAL;
+  for (const void* p : {(const void*)decay, (const void*)lengths, (const void*)initial_state, (const void*)o, (const void*)final_state, (const void*)workspace})
+    if (!aligned16(p)) return CNN_EINVAL;
+  const Plan p = plan_of(*s, 1);
+  if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return CNN_EWORKSPACE;
+  Args a = args_of(*s, p, decay, lengths);
+  const int share = s->H / s->Hk;
+  Role& r = a.role[0];
+  r.q = operand_of(q, 1), r.k = operand_of(k, share), r.v = operand_of(v, share);
+  r.out = o, r.first = initial_state, r.last = final_state, r.carry = static_cast<float*>(workspace);
+  r.first_i = s->Dv, r.first_j = 1, r.DK = s->Dk, r.DV = s->Dv;
+  r.scale = scale, r.first_by = r.last_by = 1.0f;
+  r.packed = packed_ok(q, s->Dk, s->type) && packed_ok(k, s->Dk, s->type) && packed_ok(v, s->Dv, s->type);
+  return run(a, s->type, 1, (hipStream_t)hip_stream);
+}
+
+int cnn_linear_attention_bwd(const cnn_linear_shape* s, const cnn_heads* q, const cnn_heads* k, const cnn_heads* v, const float* decay,
+                             const cnn_heads* d_o, float scale, const int32_t* lengths, const float* initial_state, const float* d_final_state,
+                             void* d_q, void* d_k, void* d_v, float* d_initial_state, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  using namespace cnn;
+  using namespace cnn::linear;
+  if (!shape_ok(s) || !heads_ok(q, s->type) || !heads_ok(k, s->type) || !heads_ok(v, s->type) || !heads_ok(d_o, s->type)) return CNN_EINVAL;
+  if (!decay || !d_q || !d_k || !d_v) return CNN_EINVAL;
+  for (const void* p : {(const void*)decay, (const void*)lengths, (const void*)initial_state, (const void*)d_final_state, (const void*)d_q, (const void*)d_k,
+                        (const void*)d_v, (const void*)d_initial_state, (const void*)workspace})
+    if (!aligned16(p)) return CNN_EINVAL;
+  const float size = __builtin_fabsf(scale);
+  if ((d_final_state || d_initial_state) && !(size >= 0x1p-100f && size <= 0x1p100f)) return CNN_EINVAL;
+  const Plan p = plan_of(*s, 3);
+  if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return CNN_EWORKSPACE;
+  Args a = args_of(*s, p, decay, lengths);
+  char* ws = static_cast<char*>(workspace);
+  const int share = s->H / s->Hk;
+  const Operand Q = operand_of(q, 1), K = operand_of(k, share), V = operand_of(v, share), D = operand_of(d_o, 1);
+  const bool shared = share > 1;
+  const bool packed = packed_ok(q, s->Dk, s->type) && packed_ok(k, s->Dk, s->type) && packed_ok(v, s->Dv, s->type) && packed_ok(d_o, s->Dv, s->type);
+  for (int i = 0; i < 3; ++i) {
+    Role& r = a.role[i];
+    r.carry = reinterpret_cast<float*>(ws + i * p.state_bytes);
+    r.scale = scale, r.packed = packed, r.first_by = r.last_by = 1.0f;
+    r.reversed = i > 0, r.wide = i > 0 && shared;
+    r.DK = i < 2 ? s->Dv : s->Dk, r.DV = i < 2 ? s->Dk : s->Dv;
+    r.first = i == 0 ? initial_state : d_final_state;
+    r.first_i = i < 2 ? 1 : s->Dv, r.first_j = i < 2 ? s->Dv : 1;  // the first two hold the state transposed
+    if (i > 0) r.first_by = 1.0f / scale, r.last_by = scale;
+  }
+  a.role[0].q = D, a.role[0].k = V, a.role[0].v = K, a.role[0].out = d_q;
+  a.role[1].q = V, a.role[1].k = D, a.role[1].v = Q, a.role[1].out = shared ? ws + p.wide_k : d_k;
+  a.role[2].q = K, a.role[2].k = Q, a.role[2].v = D, a.role[2].out = shared ? ws + p.wide_v : d_v;
+  a.role[2].last = d_initial_state;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const int rc = run(a, s->type, 3, st);
+  if (rc != CNN_OK || !shared) return rc;
+  return with_type(s->type, [&](auto t) {
+    using T = decltype(t);
+    for (int i = 0; i < 2; ++i) {
+      const int width = i ? s->Dv : s->Dk;
+      const int64_t total = (int64_t)s->B * s->T * s->Hk * width, groups = (total + 255) / 256;
+      share_kernel<T><<<(unsigned)(groups < 8192 ? groups : 8192), 256, 0, st>>>(reinterpret_cast<const float*>(ws + (i ? p.wide_v : p.wide_k)),
+                                                                                static_cast<T*>(i ? d_v : d_k), total, share, width);
+    }
+    return launch_status();
+  });
+}
+
+int cnn_linear_attention_step(const cnn_linear_shape* s, const cnn_heads* q, const cnn_heads* k, const cnn_heads* v, const float* decay,
+                              float scale, float* state, int64_t pool, const int32_t* slots, void* o, void* hip_stream) {
+  using namespace cnn;
+  using namespace cnn::linear;
+  if (!shape_ok(s) || s->T != 1 || !heads_ok(q, s->type) || !heads_ok(k, s->type) || !heads_ok(v, s->type) || !decay || !state || !o) return CNN_EINVAL;
+  if (pool < 1 || pool > 1 << 30 || (!slots && pool < s->B)) return CNN_EINVAL;
+  for (const void* p : {(const void*)decay, (const void*)state, (const void*)slots, (const void*)o})
+    if (!aligned16(p)) return CNN_EINVAL;
+  const int share = s->H / s->Hk, blocks = (s->Dv + STEP_COLUMNS - 1) / STEP_COLUMNS;
+  const StepArgs a{operand_of(q, 1), operand_of(k, share), operand_of(v, share), decay, state, slots, o, pool, s->H, s->Dk, s->Dv, blocks, scale};
+  const unsigned grid = (unsigned)((int64_t)s->B * s->H * blocks);
+  return with_type(s->type, [&](auto t) {
+    using T = decltype(t);
+    if (s->Dv % 4 == 0) step_kernel<T, 4><<<grid, STEP_THREADS, 0, (hipStream_t)hip_stream>>>(a);
+    else step_kernel<T, 1><<<grid, STEP_THREADS, 0, (hipStream_t)hip_stream>>>(a);
+    return launch_status();
+  });
+}
+
+}  // extern "C"

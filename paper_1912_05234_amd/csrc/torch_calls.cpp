@@ -403,6 +403,122 @@ CALL(dropout_bwd, 5)  // d_y, p, seed, offset, step or None
   return wrap(std::move(d_x));
 END
 
+// A [batch, token, head, width] tensor with whatever strides (the step's has no tokens), its last dimension without gaps.
+cnn_heads heads_of(const at::Tensor& t) {
+  const bool tokens = t.dim() == 4;
+  return {t.data_ptr(), t.stride(0), tokens ? t.stride(1) : 0, t.stride(tokens ? 2 : 1)};
+}
+
+const at::Tensor& heads_tensor(PyObject* o, int dims, at::ScalarType type) {
+  const at::Tensor& t = any_tensor(o, true);
+  if (t.dim() != dims) {
+    PyErr_Format(PyExc_ValueError, "expected %d dimensions, got %d", dims, (int)t.dim());
+    throw Raised();
+  }
+  if (t.scalar_type() != type) raise(PyExc_ValueError, "expected tensors of one type");
+  if (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1) raise(PyExc_ValueError, "expected a last dimension without gaps");
+  return t;
+}
+
+const float* optional(PyObject* o, at::IntArrayRef sizes, const char* what) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  if (t.sizes() != sizes) {
+    PyErr_Format(PyExc_ValueError, "expected %s of another shape", what);
+    throw Raised();
+  }
+  return data(t);
+}
+
+struct Linear {
+  cnn_linear_shape shape;
+  cnn_heads q, k, v;
+  const float* decay;
+  float scale;
+  at::Device device;
+  at::ScalarType type;
+  int64_t B, T, H, Hk, Dk, Dv;
+};
+
+Linear linear_of(PyObject* const* a, int dims) {  // q, k, v, decay, scale
+  if (!THPVariable_Check(a[0])) raise(PyExc_TypeError, "expected a tensor");
+  const at::ScalarType type = THPVariable_Unpack(a[0]).scalar_type();
+  const at::Tensor &q = heads_tensor(a[0], dims, type), &k = heads_tensor(a[1], dims, type), &v = heads_tensor(a[2], dims, type);
+  const int code = element_type(q), h = dims - 2, d = dims - 1;
+  const int64_t B = q.size(0), T = dims == 4 ? q.size(1) : 1;
+  bool fits = k.size(0) == B && v.size(0) == B && k.size(h) == v.size(h) && k.size(d) == q.size(d);
+  if (dims == 4) fits = fits && k.size(1) == T && v.size(1) == T;
+  if (!fits) raise(PyExc_ValueError, "expected q, k and v of one batch and length, k and v of as many heads, q and k of one width");
+  for (const int64_t n : {B, T, q.size(h), q.size(d), v.size(d)})
+    if (n > INT_MAX) raise(PyExc_ValueError, "a dimension is too large");
+  const int64_t H = q.size(h), Hk = k.size(h), Dk = q.size(d), Dv = v.size(d);
+  const float* decay = a[3] == Py_None ? (raise(PyExc_TypeError, "expected a tensor of decays"), nullptr) : optional(a[3], {H}, "decays");
+  return {{(int)B, (int)T, (int)H, (int)Hk, (int)Dk, (int)Dv, code}, heads_of(q), heads_of(k), heads_of(v), decay, (float)number(a[4]), q.device(), type,
+          B, T, H, Hk, Dk, Dv};
+}
+
+const int32_t* whole_numbers(PyObject* o, int64_t count, const char* what) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o, at::kInt);
+  if (t.dim() != 1 || t.size(0) != count) {
+    PyErr_Format(PyExc_ValueError, "expected one of %s per sequence", what);
+    throw Raised();
+  }
+  return data<int32_t>(t);
+}
+
+PyObject* or_none(at::Tensor t) {
+  if (t.defined()) return wrap(std::move(t));
+  Py_RETURN_NONE;
+}
+
+CALL(linear_attention_fwd, 8)  // q, k, v, decay, scale, lengths or None, initial state or None, want_state
+  const Linear x = linear_of(a, 4);
+  const int32_t* lengths = whole_numbers(a[5], x.B, "the lengths");
+  const float* initial = optional(a[6], {x.B, x.H, x.Dk, x.Dv}, "a state");
+  const size_t bytes = cnn_linear_attention_fwd_workspace_bytes(&x.shape);
+  at::Tensor o = empty({x.B, x.T, x.H, x.Dv}, x.device, x.type), state, ws;
+  if (integer(a[7])) state = empty({x.B, x.H, x.Dk, x.Dv}, x.device);
+  if (bytes) ws = empty({(int64_t)bytes}, x.device, at::kByte);
+  call("cnn_linear_attention_fwd", [&] {
+    return cnn_linear_attention_fwd(&x.shape, &x.q, &x.k, &x.v, x.decay, x.scale, lengths, initial, o.data_ptr(),
+                                    state.defined() ? data(state) : nullptr, bytes ? ws.data_ptr() : nullptr, bytes, stream());
+  });
+  return pair(wrap(std::move(o)), or_none(std::move(state)));
+END
+
+CALL(linear_attention_bwd, 10)  // q, k, v, decay, scale, d_o, lengths, initial state, error of the final state, want_d_state
+  const Linear x = linear_of(a, 4);
+  const at::Tensor& d = heads_tensor(a[5], 4, x.type);
+  if (d.sizes() != at::IntArrayRef({x.B, x.T, x.H, x.Dv})) raise(PyExc_ValueError, "expected an output error of the output's shape");
+  const cnn_heads d_o = heads_of(d);
+  const int32_t* lengths = whole_numbers(a[6], x.B, "the lengths");
+  const float* initial = optional(a[7], {x.B, x.H, x.Dk, x.Dv}, "a state");
+  const float* d_final = optional(a[8], {x.B, x.H, x.Dk, x.Dv}, "a state's error");
+  const size_t bytes = cnn_linear_attention_bwd_workspace_bytes(&x.shape);
+  at::Tensor d_q = empty({x.B, x.T, x.H, x.Dk}, x.device, x.type), d_k = empty({x.B, x.T, x.Hk, x.Dk}, x.device, x.type);
+  at::Tensor d_v = empty({x.B, x.T, x.Hk, x.Dv}, x.device, x.type), d_state, ws;
+  if (integer(a[9])) d_state = empty({x.B, x.H, x.Dk, x.Dv}, x.device);
+  if (bytes) ws = empty({(int64_t)bytes}, x.device, at::kByte);
+  call("cnn_linear_attention_bwd", [&] {
+    return cnn_linear_attention_bwd(&x.shape, &x.q, &x.k, &x.v, x.decay, &d_o, x.scale, lengths, initial, d_final, d_q.data_ptr(), d_k.data_ptr(),
+                                    d_v.data_ptr(), d_state.defined() ? data(d_state) : nullptr, bytes ? ws.data_ptr() : nullptr, bytes, stream());
+  });
+  return pair(pair(wrap(std::move(d_q)), wrap(std::move(d_k))), pair(wrap(std::move(d_v)), or_none(std::move(d_state))));
+END
+
+CALL(linear_attention_step, 7)  // q, k, v, decay, scale, state, slots or None
+  const Linear x = linear_of(a, 3);
+  const at::Tensor& state = tensor(a[5], 4);
+  if (state.size(1) != x.H || state.size(2) != x.Dk || state.size(3) != x.Dv) raise(PyExc_ValueError, "expected a pool of states of another shape");
+  const int32_t* slots = whole_numbers(a[6], x.B, "the slots");
+  at::Tensor o = empty({x.B, x.H, x.Dv}, x.device, x.type);
+  call("cnn_linear_attention_step", [&] {
+    return cnn_linear_attention_step(&x.shape, &x.q, &x.k, &x.v, x.decay, x.scale, data(state), state.size(0), slots, o.data_ptr(), stream());
+  });
+  return wrap(std::move(o));
+END
+
 PyObject* raise_through(PyObject*, PyObject* fn) {  // binding._check
   Py_INCREF(fn);
   Py_XSETREF(check, fn);
@@ -413,7 +529,8 @@ PyObject* raise_through(PyObject*, PyObject* fn) {  // binding._check
 PyMethodDef methods[] = {FAST(forward), FAST(gradient), FAST(train_batch), FAST(evaluate), FAST(conv_fwd), FAST(conv_bwd_input),
                          FAST(conv_bwd_weight), FAST(avgpool_fwd), FAST(avgpool_bwd), FAST(fc_fwd), FAST(fc_bwd_input),
                          FAST(fc_bwd_weight), FAST(logistic_fwd), FAST(logistic_bwd), FAST(embedding_fwd), FAST(embedding_bwd), FAST(dropout_fwd),
-                         FAST(dropout_bwd),
+                         FAST(dropout_bwd), FAST(linear_attention_fwd), FAST(linear_attention_bwd), FAST(linear_attention_step),
+                        
                          {"raise_through", raise_through, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -31,3 +31,55 @@ def test_dropout_refusals():
         assert fwd(**bad) == EINVAL, bad
     assert L.cnn_dropout_bwd(nul, fake, 8, 0, 0.5, 1, 2, nul, nul) == EINVAL
     assert L.cnn_dropout_bwd(fake, fake, 8, 0, 2.0, 1, 2, nul, nul) == EINVAL
+
+
+def shape(B=2, T=5, H=4, Hk=2, Dk=32, Dv=64, type_=1):
+    return binding.LinearShape(B, T, H, Hk, Dk, Dv, type_)
+
+
+def heads(data=0x1000, batch=640, token=128, head=32):
+    return binding.Heads(data, batch, token, head)
+
+
+BAD_SHAPES = [{"B": 0}, {"T": 0}, {"H": 0}, {"Hk": 0}, {"Hk": 3}, {"Dk": 0}, {"Dk": 257}, {"Dv": 0}, {"Dv": 300}, {"type_": 3}, {"type_": -1},
+              {"B": 1 << 19, "H": 4}]
+BAD_HEADS = [None, heads(data=0), heads(data=0x1001), heads(batch=-1), heads(token=-128), heads(head=-1)]
+
+
+def test_linear_attention_refusals():
+    L = binding.lib()
+    fwd = lambda s=shape(), q=heads(), k=heads(), v=heads(), a=fake, n=nul, i=nul, o=fake, f=nul, ws=nul, b=0: L.cnn_linear_attention_fwd(  # noqa: E731
+        s, q, k, v, a, 1.0, n, i, o, f, ws, b, nul)
+    bwd = lambda s=shape(), q=heads(), d=heads(), a=fake, scale=1.0, i=nul, f=nul, dq=fake, dk=fake, dv=fake, ds=nul, ws=fake, b=1 << 40: (  # noqa: E731
+        L.cnn_linear_attention_bwd(s, q, heads(), heads(), a, d, scale, nul, i, f, dq, dk, dv, ds, ws, b, nul))
+    step = lambda s=shape(T=1), q=heads(), a=fake, state=fake, pool=2, slots=nul, o=fake: L.cnn_linear_attention_step(  # noqa: E731
+        s, q, heads(), heads(), a, 1.0, state, pool, slots, o, nul)
+    assert fwd(s=None) == bwd(s=None) == step(s=None) == EINVAL
+    for bad in BAD_SHAPES:
+        assert fwd(s=shape(**bad)) == EINVAL and bwd(s=shape(**bad)) == EINVAL, bad
+        assert L.cnn_linear_attention_fwd_workspace_bytes(shape(**bad)) == L.cnn_linear_attention_bwd_workspace_bytes(shape(**bad)) == 0, bad
+        if "T" not in bad:
+            assert step(s=shape(**{"T": 1, **bad})) == EINVAL, bad
+    for h in BAD_HEADS:
+        assert fwd(q=h) == fwd(k=h) == fwd(v=h) == bwd(q=h) == bwd(d=h) == step(q=h) == EINVAL
+    for bad in ({"a": nul}, {"o": nul}, {"a": odd}, {"o": odd}, {"n": odd}, {"i": odd}, {"f": odd}, {"ws": odd}):
+        assert fwd(**bad) == EINVAL, bad
+    for bad in ({"a": nul}, {"dq": nul}, {"dk": nul}, {"dv": nul}, {"dv": odd}, {"ds": odd}, {"f": odd}, {"scale": 0.0, "f": fake},
+                {"scale": float("nan"), "ds": fake}, {"scale": float("inf"), "ds": fake}):
+        assert bwd(**bad) == EINVAL, bad
+    for bad in ({"a": nul}, {"state": nul}, {"o": nul}, {"state": odd}, {"slots": odd}, {"pool": 0}, {"pool": 1}, {"s": shape(T=2)}):
+        assert step(**bad) == EINVAL, bad
+
+
+def test_linear_attention_workspaces():
+    """None where one pass does; states of the pieces of long sequences; partial gradients of shared heads."""
+    L = binding.lib()
+    fwd, bwd = L.cnn_linear_attention_fwd_workspace_bytes, L.cnn_linear_attention_bwd_workspace_bytes
+    assert fwd(shape()) == 0 and fwd(shape(B=64, T=10000, H=16, Hk=16)) == 0 and fwd(None) == 0
+    long = shape(B=1, T=8192)
+    need = fwd(long)
+    assert 0 < need and need % (4 * 32 * 64) == 0  # one state for every segment
+    assert L.cnn_linear_attention_fwd(long, heads(), heads(), heads(), fake, 1.0, nul, nul, fake, nul, nul, 0, nul) == EWS
+    assert L.cnn_linear_attention_fwd(long, heads(), heads(), heads(), fake, 1.0, nul, nul, fake, nul, fake, need - 1, nul) == EWS
+    assert bwd(shape(Hk=4)) == 0
+    assert bwd(shape(Hk=2)) >= 2 * 5 * 4 * (32 + 64) * 4
