@@ -13,15 +13,18 @@
 // width of its q and k, DV that of its v and out.
 //
 // A workgroup takes a block of DV columns of one sequence and head, and walks the chunks of its segment of the time axis; the
-// state stays in the accumulators of the matrix instructions, fp32, each wave holding 16 NW columns.  Where there are too few
+// state stays in the accumulators of the matrix instructions, fp32, each wave holding 32 columns.  Where there are too few
 // heads to fill the GPU the time axis is cut into segments: a first pass finds what each segment adds to the state, a scan over
 // the segments turns that into the state that each starts from, and the second pass runs them side by side.
 //
 // Operands are bfloat16 pieces (x = h + m + l, eight bits each): a bfloat16 is one piece, a half two, a float three, and products
 // of two pieces are left out where they are below the last bit kept (2^-16 of the result for halves, 2^-24 for floats).
-// What the kernel computes itself is not rounded to the input's type: state and scores are cut into two pieces (three for floats),
-// a^{C-1-s} v_s into three, so that the state is exact to fp32 sums for every type.
+// What the kernel computes itself is not rounded to the input's type: state and scores are cut into two pieces (2^-17 of each is
+// lost, of results that are rounded to 2^-9 or 2^-12), three for floats; a^{C-1-s} v_s into three, so that the state is exact to fp32
+// sums for every type, or two in the second pass over segments, whose own state is no result.
 #pragma once
+
+#include <type_traits>
 
 #include "cnn_common.h"
 #include "cnn_types.h"
@@ -34,6 +37,7 @@ using bf2 = __bf16 __attribute__((ext_vector_type(2)));
 using f4 = float __attribute__((ext_vector_type(4)));
 using f2 = float __attribute__((ext_vector_type(2)));
 using s4 = short __attribute__((ext_vector_type(4)));
+using bf4 = __bf16 __attribute__((ext_vector_type(4)));
 
 struct Operand {  // [batch][token][head][width], strides in elements, the last one is 1
   const void* data;
@@ -46,7 +50,7 @@ struct Role {
   void* out;  // [batch][token][head][DV], contiguous; float where `wide`, else of the element type
   const float* first;  // state before the sequence, nullable: element (i, j) of unit u at u * DK * DV + i * first_i + j * first_j
   float* last;         // state after it, nullable, [unit][DK][DV]
-  float* carry;        // [unit][segment][DK][DV]
+  float* carry;        // [unit][segment], states in the order of the kernel's registers
   int first_i, first_j;
   int DK, DV, blocks;  // blocks of columns
   float scale, first_by, last_by;
@@ -62,6 +66,18 @@ struct Args {
   int64_t units, T, segment_length;  // units: sequences times heads
   int heads, segments;
 };
+
+// Tokens of a sequence, and of one of its segments: these end where the sequence does, the first of them may be short or empty.
+__device__ __forceinline__ int64_t length_of(const Args& a, int64_t batch) {
+  if (!a.lengths) return a.T;
+  const int64_t n = a.lengths[batch];
+  return n < 0 ? 0 : n < a.T ? n : a.T;
+}
+__device__ __forceinline__ int64_t segment_end(const Args& a, int64_t n, int segment) {
+  const int64_t e = n - (a.segments - 1 - segment) * a.segment_length;
+  return e > 0 ? e : 0;
+}
+__device__ __forceinline__ int64_t segment_begin(const Args& a, int64_t n, int segment) { return segment_end(a, n, segment - 1); }
 
 template <class T>
 constexpr int PIECES = sizeof(T) == 4 ? 3 : 2;
@@ -110,51 +126,78 @@ __device__ __forceinline__ bf8 joined(s4 a, s4 b) {
   return __builtin_bit_cast(bf8, s8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
 }
 
-// Shape of a kernel: DKP columns of q and k (DK padded with zeros), chunks of 16 CT tokens, WAVES waves of 16 NW columns each.
-template <class T, int DKP, int CT, int WAVES, int NW>
+// Shape of a kernel: DKP columns of q and k (DK padded with zeros), WAVES waves of 32 columns of v (NW tiles of 16), chunks of 32
+// tokens: products over the tokens of a chunk are one step of the matrix instruction, and the scores are three of its tiles, which
+// every wave computes for itself.
+constexpr int C = 32, NW = 2;
+template <class T, int DKP, int WAVES>
 struct Shape {
-  static constexpr int C = 16 * CT, DVC = WAVES * 16 * NW, THREADS = 64 * WAVES;
+  static constexpr int DVC = WAVES * 16 * NW, THREADS = 64 * WAVES;
   static constexpr int NP = PIECES<T>, MP = at_least_two(NP);  // pieces of the inputs, and of state and scores
   // rows of q and k are read sixteen bytes to a lane, of v and k also four rows to a lane: the padding spreads them over the banks
   static constexpr int QS = DKP + 8, VS = DVC + 16;
-  static constexpr int K = 0, V = K + NP * C * QS, Q = V + NP * C * VS, P = Q + NP * C * QS;  // offsets of the tiles in LDS
-  static constexpr int TILES = CT * (CT + 1) / 2;  // of the scores, on and below the diagonal
-  static constexpr int ALL = P + TILES * MP * 256;
+  static constexpr int K = 0, V = K + NP * C * QS, Q = V + NP * C * VS, ALL = Q + NP * C * QS;  // offsets of the tiles in LDS
+  // two sets of tiles, and one barrier a chunk, where eight waves of a compute unit have room for them
+  static constexpr int SETS = 2 * ALL * 2 <= 20 * 1024 * WAVES ? 2 : 1;
 };
 
-// Units of eight elements of a tile that a thread brings from memory to LDS.
+// Units of eight elements of a tile that a thread brings from memory to LDS: one column of units, every STEP-th row.
 template <class T, int ROWS, int WIDTH, int THREADS>
 struct Stage {
-  static constexpr int UNITS = ROWS * WIDTH / 8, EACH = (UNITS + THREADS - 1) / THREADS;
+  static constexpr int COLUMNS = WIDTH / 8, STEP = THREADS / COLUMNS, EACH = (ROWS + STEP - 1) / STEP;
+  static_assert(THREADS % COLUMNS == 0, "threads to a row");
   Pack<T, 8> u[EACH];
 
-  // rows t0 .. of a sequence of n tokens; zeros past it and past `width`
-  __device__ __forceinline__ void load(const T* base, int64_t stride, int64_t t0, int64_t n, int width, bool reversed, bool packed) {
+  // Rows pad .. ROWS - 1, of `width` elements; `low` is where row 0 is or would be, or, in reversed order, the last row.  Rows
+  // before `pad` repeat row pad, so that the loads need no branches.
+  template <bool PACKED>
+  __device__ __forceinline__ void load(const T* low, int64_t stride, int pad, int width, bool reversed) {
+    const int c = threadIdx.x % COLUMNS * 8, row0 = threadIdx.x / COLUMNS;
+    const auto row_of = [&](int e) {
+      const int row = ROWS % STEP && row0 + e * STEP >= ROWS ? ROWS - 1 : row0 + e * STEP;
+      return reversed ? ROWS - 1 - row : row;
+    };
+    // (in reversed order the rows before pad are the last ones)
+    const auto kept = [&](int row) { return reversed ? (row < ROWS - pad ? row : ROWS - pad - 1) : (row > pad ? row : pad); };
+    if (c >= width) {
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      const int i = e * THREADS + threadIdx.x, c = i % (WIDTH / 8) * 8;
-      const int64_t t = t0 + i / (WIDTH / 8);
+      for (int e = 0; e < EACH; ++e)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) u[e].v[j] = (T)0.0f;
-      if (i >= UNITS || t >= n || c >= width) continue;
-      const T* row = base + (reversed ? n - 1 - t : t) * stride + c;
-      if (packed) {
-        u[e] = *reinterpret_cast<const Pack<T, 8>*>(row);
-      } else {
+        for (int j = 0; j < 8; ++j) u[e].v[j] = (T)0.0f;
+      return;
+    }
+    if constexpr (PACKED) {  // a chunk's rows are less than 2^31 bytes apart
+      const uint32_t step = (uint32_t)stride * (uint32_t)sizeof(T);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j < width) u[e].v[j] = row[j];
+      for (int e = 0; e < EACH; ++e)
+        u[e] = *reinterpret_cast<const Pack<T, 8>*>(reinterpret_cast<const char*>(low) + (__umul24(kept(row_of(e)), step) + c * (uint32_t)sizeof(T)));
+    } else {
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) {
+        const T* row = low + kept(row_of(e)) * stride + c;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[e].v[j] = c + j < width ? row[j] : (T)0.0f;
       }
     }
   }
 
+  // Rows before `pad` as zeros.
+  __device__ __forceinline__ void clear(int pad) {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if ((int)threadIdx.x / COLUMNS + e * STEP < pad) u[e].v[j] = (T)0.0f;
+  }
+
   template <int STRIDE>
-  __device__ __forceinline__ void store(__bf16* tile) const {  // NP planes of [ROWS][STRIDE]
+  __device__ __forceinline__ void store(__bf16* tile) const {  // planes of [ROWS][STRIDE], one to a piece
     constexpr int NP = PIECES<T>;
+    const int c = threadIdx.x % COLUMNS * 8, row0 = threadIdx.x / COLUMNS;
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
-      const int i = e * THREADS + threadIdx.x, at = i / (WIDTH / 8) * STRIDE + i % (WIDTH / 8) * 8;
-      if (i >= UNITS) continue;
+      const int row = row0 + e * STEP;
+      if (ROWS % STEP && row >= ROWS) continue;
       bf8 piece[NP];
       if constexpr (NP == 1) {
         piece[0] = __builtin_bit_cast(bf8, u[e]);
@@ -165,7 +208,7 @@ struct Stage {
         cut<NP>(x, piece);
       }
 #pragma unroll
-      for (int p = 0; p < NP; ++p) *reinterpret_cast<bf8*>(tile + p * ROWS * STRIDE + at) = piece[p];
+      for (int p = 0; p < NP; ++p) *reinterpret_cast<bf8*>(tile + (p * ROWS + row) * STRIDE + c) = piece[p];
     }
   }
 };
@@ -177,258 +220,311 @@ __device__ __forceinline__ float log2_decay(float a) {
 }
 __device__ __forceinline__ float power(float log2a, int e) { return __builtin_amdgcn_exp2f(log2a * (float)e); }
 
-template <class T, int DKP, int CT, int WAVES, int NW, bool STATE_ONLY>
-__global__ __launch_bounds__(64 * WAVES) void scan_kernel(Args args) {
-  using S = Shape<T, DKP, CT, WAVES, NW>;
-  constexpr int C = S::C, THREADS = S::THREADS, NP = S::NP, MP = S::MP, KS = CT / 2, M = DKP / 16;
-  __shared__ __align__(16) __bf16 tile[STATE_ONLY ? S::Q : S::ALL];
+// Keeps operands read from LDS for a later step from taking registers now.
+__device__ __forceinline__ void in_steps() { __builtin_amdgcn_sched_barrier(0); }
+// A number that the compiler takes for a new one, so that nothing computed from it is held through the loop before.
+__device__ __forceinline__ int anew(int x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+
+// Where a state's register i of tile m of a wave's lane stands.  A pair of tiles is an operand of a product over 32 rows as it is.
+__device__ __forceinline__ int state_row(int m, int lane, int i) { return 32 * (m >> 1) + 8 * (lane >> 4) + 4 * (m & 1) + i; }
+__device__ __forceinline__ int state_column(int tile, int lane) { return 16 * tile + (lane & 15); }  // tile: of sixteen columns
+
+constexpr int waves_wanted(int DKP) { return DKP <= 128 ? 2 : 1; }  // to a SIMD
+
+// STATE_ONLY: the first pass.  EXACT: the state is a result, not only what the segment's own tokens see.
+template <class T, int DKP, int WAVES, bool PACKED, bool STATE_ONLY, bool EXACT>
+__global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Args args) {
+  using S = Shape<T, DKP, WAVES>;
+  constexpr int THREADS = S::THREADS, NP = S::NP, MP = S::MP, WP = EXACT ? 3 : MP, M = DKP / 16;
+  constexpr int SET = STATE_ONLY ? S::Q : S::ALL;
+  __shared__ __align__(16) __bf16 tiles[S::SETS * SET];
   const Role& R = args.role[blockIdx.y];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
 
   const int64_t job = blockIdx.x / R.blocks, unit = job / args.segments;
   const int segment = (int)(job % args.segments), block = (int)(blockIdx.x % R.blocks);
   if (unit >= args.units) return;  // (a role of fewer column blocks has fewer workgroups)
   const int64_t batch = unit / args.heads;
   const int head = (int)(unit % args.heads), dv0 = block * S::DVC;
-  const int64_t n = args.lengths ? (args.lengths[batch] < 0 ? 0 : args.lengths[batch] < args.T ? args.lengths[batch] : args.T) : args.T;
-  const int64_t begin = segment * args.segment_length, end = begin + args.segment_length < args.T ? begin + args.segment_length : args.T;
+  const int64_t n = length_of(args, batch), end = segment_end(args, n, segment), begin = segment_begin(args, n, segment);
   const int DK = R.DK, DV = R.DV, width = DV - dv0 < S::DVC ? DV - dv0 : S::DVC;
-  const bool reversed = R.reversed, packed = R.packed;
-  const auto base = [&](const Operand& o) { return static_cast<const T*>(o.data) + batch * o.batch + head / o.share * o.head; };
-  const T *q = base(R.q), *k = base(R.k), *v = base(R.v) + dv0;
-  const float log2a = log2_decay(args.decay[head]);
+  const bool reversed = R.reversed;
 
-  // S: tile m of sixteen rows, register i: row 32 (m / 2) + 8 g + 4 (m % 2) + i, so that a pair of tiles is the second operand of a
-  // product over 32 rows as it is; column 16 (NW wave + w) + r
-  const auto row_of = [&](int m, int i) { return 32 * (m >> 1) + 8 * g + 4 * (m & 1) + i; };
-  const auto column_of = [&](int w) { return 16 * (NW * wave + w) + r; };
+  // Chunks end where the segment does; the first one may begin before it, with `pad` rows that are no tokens.
+  int pad = (int)((C - (end - begin) % C) % C);
+  Stage<T, C, DKP, THREADS> q_in, k_in;
+  Stage<T, C, S::DVC, THREADS> v_in;
+  const int64_t low = reversed ? n - (begin - pad) - C : begin - pad, advance = reversed ? -C : C;  // in tokens
+  const auto base = [&](const Operand& o) { return static_cast<const T*>(o.data) + batch * o.batch + head / o.share * o.head + low * o.token; };
+  const T *q = base(R.q), *k = base(R.k), *v = base(R.v) + dv0;
+  const int64_t q_step = advance * R.q.token, k_step = advance * R.k.token, v_step = advance * R.v.token;
+  const auto load = [&](int pad) {
+    k_in.template load<PACKED>(k, R.k.token, pad, DK, reversed);
+    v_in.template load<PACKED>(v, R.v.token, pad, width, reversed);
+    if (!STATE_ONLY) q_in.template load<PACKED>(q, R.q.token, pad, DK, reversed);
+    q += q_step, k += k_step, v += v_step;
+  };
+  const auto store = [&](__bf16* tile) {
+    k_in.template store<S::QS>(tile + S::K);
+    v_in.template store<S::VS>(tile + S::V);
+    if (!STATE_ONLY) q_in.template store<S::QS>(tile + S::Q);
+  };
+  if (begin < end) load(pad);
+
   f4 state[M][NW];
   const bool whole = args.segments == 1;
+  const int64_t carry_size = (int64_t)DKP * R.blocks * S::DVC;  // [tile of columns][tile of rows][lane][4]
+  f4* carry = reinterpret_cast<f4*>(R.carry + (unit * args.segments + segment) * carry_size) + (block * WAVES + wave) * NW * M * 64 + lane;
 #pragma unroll
   for (int m = 0; m < M; ++m)
 #pragma unroll
-    for (int w = 0; w < NW; ++w)
+    for (int w = 0; w < NW; ++w) state[m][w] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (!STATE_ONLY && !whole) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = row_of(m, i), col = dv0 + column_of(w);
-        float x = 0.0f;
-        if (!STATE_ONLY && row < DK && col < DV) {
-          if (!whole) x = R.carry[((unit * args.segments + segment) * DK + row) * DV + col];
-          else if (R.first) x = R.first[unit * DK * DV + (int64_t)row * R.first_i + (int64_t)col * R.first_j] * R.first_by;
-        }
-        state[m][w][i] = x;
-      }
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int w = 0; w < NW; ++w) state[m][w] = carry[(w * M + m) * 64];
+  } else if (!STATE_ONLY && R.first) {
+    const float* from = R.first + unit * DK * DV;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const int column = state_column(NW * wave + w, lane), at_column = (dv0 + column) * R.first_j;
+#pragma unroll
+      for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (state_row(m, lane, i) < DK && column < width) state[m][w][i] = from[(uint32_t)(state_row(m, lane, i) * R.first_i + at_column)];
+      in_steps();
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int w = 0; w < NW; ++w) state[m][w] *= R.first_by;
+  }
   int shift = reversed && begin == 0 ? 0 : 1;  // powers of a between the state before the chunk and the chunk's first token
 
-  Stage<T, C, DKP, THREADS> q_in, k_in;
-  Stage<T, C, S::DVC, THREADS> v_in;
-  const auto load = [&](int64_t t0) {
-    if (!STATE_ONLY) q_in.load(q, R.q.token, t0, n, DK, reversed, packed);
-    k_in.load(k, R.k.token, t0, n, DK, reversed, packed);
-    v_in.load(v, R.v.token, t0, n, width, reversed, packed);
-  };
-  const int64_t busy = end < n ? end : n;  // where the sequence, or the segment, ends
-  if (begin < busy) load(begin);
-  for (int64_t t0 = begin; t0 < busy; t0 += C) {
-    const int count = busy - t0 < C ? (int)(busy - t0) : C;
-    if (!STATE_ONLY) q_in.template store<S::QS>(tile + S::Q);
-    k_in.template store<S::QS>(tile + S::K);
-    v_in.template store<S::VS>(tile + S::V);
-    __syncthreads();
-    if (t0 + C < busy) load(t0 + C);
+  const float log2a = log2_decay(args.decay[head]);
+  // weights of the scores, by t - s = 16 (t's tile - s's tile) + r - 4 g - i, and of the tokens in the state at the chunk's end
+  float on_diagonal[4], below[4], follow[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int e = r - 4 * g - i;
+    on_diagonal[i] = power(log2a, e > 0 ? e : 0);
+    below[i] = power(log2a, 16 + e);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) follow[j] = power(log2a, C - 1 - 16 * (j >> 2) - (j & 3) - 4 * g);
 
-    f4 acc[CT][NW];
+  // out: rows of a chunk are tokens, columns 4 g + i of a tile of sixteen
+  const int out_stride = args.heads * DV, out_column = 16 * NW * wave + 4 * g;
+  int64_t out = ((batch * args.T + low) * args.heads + head) * DV + dv0;
+  const int64_t out_step = advance * out_stride;
+
+  __bf16* tile = tiles;
+  if (begin < end) {
+    if (pad) k_in.clear(pad);  // what is no token adds nothing
+    store(tile);
+    __syncthreads();
+  }
+  for (int64_t t0 = begin - pad; t0 < end; t0 += C) {
+    const bool more = t0 + C < end;
+    if (more) load(0);
+
+    f4 acc[2][NW];  // of the result, transposed: rows are columns 4 g + i of out, column r is token r
+    bf8 score[2][MP];
     if constexpr (!STATE_ONLY) {
-      // scores, transposed: columns t, rows s; four consecutive s to a lane are half an operand of the product with V
-      for (int i = wave; i < S::TILES; i += WAVES) {
-        const int tt = i < 1 ? 0 : i < 3 ? 1 : i < 6 ? 2 : 3, st = i - tt * (tt + 1) / 2;
-        f4 p{0.0f, 0.0f, 0.0f, 0.0f};
+      // Q S, and the scores, transposed: columns t, rows s, so that a pair of tiles is an operand of the product with V
+      f4 p00{0.0f, 0.0f, 0.0f, 0.0f}, p01 = p00, p11 = p00;  // [s][t]
 #pragma unroll
-        for (int s = 0; s < DKP / 32; ++s) {
-          bf8 a[NP], b[NP];
-#pragma unroll
-          for (int z = 0; z < NP; ++z) {
-            a[z] = *reinterpret_cast<const bf8*>(tile + S::K + (z * C + 16 * st + r) * S::QS + 32 * s + 8 * g);
-            b[z] = *reinterpret_cast<const bf8*>(tile + S::Q + (z * C + 16 * tt + r) * S::QS + 32 * s + 8 * g);
-          }
-          p = product(a, b, p);
-        }
-        const int e = 16 * (tt - st) + r - 4 * g;  // t - s of register 0
-        float rest[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) rest[j] = e >= j ? p[j] * power(log2a, e - j) : 0.0f;
-#pragma unroll
-        for (int z = 0; z < MP; ++z) {
-          const bf2 h0 = __builtin_convertvector(f2{rest[0], rest[1]}, bf2), h1 = __builtin_convertvector(f2{rest[2], rest[3]}, bf2);
-          *reinterpret_cast<bf2*>(tile + S::P + ((i * MP + z) * 64 + lane) * 4) = h0;
-          *reinterpret_cast<bf2*>(tile + S::P + ((i * MP + z) * 64 + lane) * 4 + 2) = h1;
-          rest[0] -= (float)h0[0], rest[1] -= (float)h0[1], rest[2] -= (float)h1[0], rest[3] -= (float)h1[1];
-        }
-      }
-      // Q S
-#pragma unroll
-      for (int t = 0; t < CT; ++t)
-#pragma unroll
-        for (int w = 0; w < NW; ++w) acc[t][w] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int w = 0; w < NW; ++w) acc[0][w] = acc[1][w] = p00;
 #pragma unroll
       for (int s = 0; s < M / 2; ++s) {
-        bf8 b[NW][MP];
+        bf8 row[2][NP], query[2][NP];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int z = 0; z < NP; ++z) {
+            query[t][z] = *reinterpret_cast<const bf8*>(tile + S::Q + (z * C + 16 * t + r) * S::QS + 32 * s + 8 * g);
+            row[t][z] = *reinterpret_cast<const bf8*>(tile + S::K + (z * C + 16 * t + r) * S::QS + 32 * s + 8 * g);
+          }
+        p00 = product(row[0], query[0], p00);
+        p01 = product(row[0], query[1], p01);
+        p11 = product(row[1], query[1], p11);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
           const f4 lo = state[2 * s][w], hi = state[2 * s + 1][w];
           const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-          cut<MP>(x, b[w]);
+          bf8 a[MP];
+          cut<MP>(x, a);
+          acc[0][w] = product(a, query[0], acc[0][w]);
+          acc[1][w] = product(a, query[1], acc[1][w]);
         }
-#pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          bf8 a[NP];
-#pragma unroll
-          for (int z = 0; z < NP; ++z) a[z] = *reinterpret_cast<const bf8*>(tile + S::Q + (z * C + 16 * t + r) * S::QS + 32 * s + 8 * g);
-#pragma unroll
-          for (int w = 0; w < NW; ++w) acc[t][w] = product(a, b[w], acc[t][w]);
-        }
+        if (NP > 1 || (s & 1)) in_steps();
       }
 #pragma unroll
-      for (int t = 0; t < CT; ++t)
+      for (int t = 0; t < 2; ++t) {
+        const int e = 16 * t + r - pad + shift;
+        const float by = power(log2a, e > 0 ? e : 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float by = power(log2a, 16 * t + 4 * g + i + shift);
-#pragma unroll
-          for (int w = 0; w < NW; ++w) acc[t][w][i] *= by;
-        }
-      __syncthreads();  // the scores are there
-    }
-
-    // the state: decayed, and the chunk's products added
-    const float by = power(log2a, count + shift - 1);
-#pragma unroll
-    for (int m = 0; m < M; ++m)
-#pragma unroll
-      for (int w = 0; w < NW; ++w)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) state[m][w][i] *= by;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      bf8 b[NW][3];
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        bf8 raw[NP];
-#pragma unroll
-        for (int z = 0; z < NP; ++z) {
-          const __bf16* p = tile + S::V + (z * C + 32 * s + 4 * g + (r >> 2)) * S::VS + 16 * (NW * wave + w) + 4 * (r & 3);
-          raw[z] = joined(read_transposed(p), read_transposed(p + 16 * S::VS));
-        }
-        if constexpr (!STATE_ONLY) {
-          // scores times V; the tile above the diagonal is zero
-#pragma unroll
-          for (int t = 2 * s; t < CT; ++t) {
-            bf8 a[MP];
-#pragma unroll
-            for (int z = 0; z < MP; ++z) {
-              const int i = t * (t + 1) / 2 + 2 * s;
-              const s4 lo = *reinterpret_cast<const s4*>(tile + S::P + ((i * MP + z) * 64 + lane) * 4);
-              s4 hi{0, 0, 0, 0};
-              if (2 * s + 1 <= t) hi = *reinterpret_cast<const s4*>(tile + S::P + (((i + 1) * MP + z) * 64 + lane) * 4);
-              a[z] = joined(lo, hi);
-            }
-            acc[t][w] = product(a, raw, acc[t][w]);
-          }
-        }
+        for (int w = 0; w < NW; ++w) acc[t][w] *= by;
         float x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          x[j] = 0.0f;
-#pragma unroll
-          for (int z = NP - 1; z >= 0; --z) x[j] += (float)raw[z][j];
-          const int e = count - 1 - (32 * s + 16 * (j >> 2) + 4 * g + (j & 3));  // tokens that follow in the chunk
-          x[j] = e >= 0 ? x[j] * power(log2a, e) : 0.0f;
+        for (int j = 0; j < 4; ++j) {
+          const bool on = r >= 4 * g + j;
+          x[j] = t ? p01[j] * below[j] : on ? p00[j] * on_diagonal[j] : 0.0f;
+          x[4 + j] = t && on ? p11[j] * on_diagonal[j] : 0.0f;
         }
-        cut<3>(x, b[w]);
-      }
-#pragma unroll
-      for (int m = 0; m < M; ++m) {
-        bf8 a[NP];
-#pragma unroll
-        for (int z = 0; z < NP; ++z) {
-          const __bf16* p = tile + S::K + (z * C + 32 * s + 4 * g + (r >> 2)) * S::QS + 32 * (m >> 1) + 8 * (r & 3) + 4 * (m & 1);
-          a[z] = joined(read_transposed(p), read_transposed(p + 16 * S::QS));
-        }
-#pragma unroll
-        for (int w = 0; w < NW; ++w) state[m][w] = product(a, b[w], state[m][w]);
+        cut<MP>(x, score[t]);
       }
     }
+
+    // the scores' product with V; the state: decayed, and the chunk's products added
+    const float by = power(log2a, C - pad + shift - 1);
+    bf8 weighted[NW][WP];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      bf8 raw[NP];
+#pragma unroll
+      for (int z = 0; z < NP; ++z) {
+        const __bf16* p = tile + S::V + (z * C + 4 * g + (r >> 2)) * S::VS + 16 * (NW * wave + w) + 4 * (r & 3);
+        raw[z] = joined(read_transposed(p), read_transposed(p + 16 * S::VS));
+      }
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[j] = 0.0f;
+#pragma unroll
+        for (int z = NP - 1; z >= 0; --z) x[j] += (float)raw[z][j];
+        x[j] *= follow[j];
+      }
+      cut<WP>(x, weighted[w]);
+      if constexpr (!STATE_ONLY) {
+        acc[0][w] = product(raw, score[0], acc[0][w]);
+        acc[1][w] = product(raw, score[1], acc[1][w]);
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      bf8 a[NP];
+#pragma unroll
+      for (int z = 0; z < NP; ++z) {
+        const __bf16* p = tile + S::K + (z * C + 4 * g + (r >> 2)) * S::QS + 32 * (m >> 1) + 8 * (r & 3) + 4 * (m & 1);
+        a[z] = joined(read_transposed(p), read_transposed(p + 16 * S::QS));
+      }
+#pragma unroll
+      for (int w = 0; w < NW; ++w) state[m][w] = product(a, weighted[w], state[m][w] * by);
+      if ((m & 3) == 3 || (NP > 1 && (m & 1))) in_steps();
+    }
+
     if constexpr (!STATE_ONLY) {
 #pragma unroll
-      for (int t = 0; t < CT; ++t)
+      for (int t = 0; t < 2; ++t) {
+        const int at = 16 * t + r, row = reversed ? C - 1 - at : at;
+        if (at < pad) continue;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at = 16 * t + 4 * g + i;
-          if (at >= count) continue;
-          const int64_t token = reversed ? n - 1 - (t0 + at) : t0 + at;
-          const int64_t row = ((batch * args.T + token) * args.heads + head) * DV;
+        for (int w = 0; w < NW; ++w) {
+          const f4 y = acc[t][w] * R.scale;
+          const int column = out_column + 16 * w;
+          if constexpr (PACKED) {  // whole packs, so width is a multiple of eight; the chunk's rows are less than 2^31 bytes apart
+            if (column >= width) continue;
+            const uint32_t e = (uint32_t)(row * out_stride + column);
+            if (R.wide) *reinterpret_cast<f4*>(static_cast<float*>(R.out) + out + e) = y;
+            else *reinterpret_cast<Pack<T, 4>*>(static_cast<T*>(R.out) + out + e) = Pack<T, 4>{{(T)y[0], (T)y[1], (T)y[2], (T)y[3]}};
+          } else {
+            const int64_t e = out + (int64_t)row * out_stride + column;
 #pragma unroll
-          for (int w = 0; w < NW; ++w) {
-            const int col = column_of(w);
-            if (col >= width) continue;
-            const float x = acc[t][w][i] * R.scale;
-            if (R.wide) static_cast<float*>(R.out)[row + dv0 + col] = x;
-            else static_cast<T*>(R.out)[row + dv0 + col] = (T)x;
+            for (int i = 0; i < 4; ++i) {
+              if (column + i >= width) continue;
+              if (R.wide) static_cast<float*>(R.out)[e + i] = y[i];
+              else static_cast<T*>(R.out)[e + i] = (T)y[i];
+            }
           }
         }
+      }
+      out += out_step;
     }
-    shift = 1;
-    __syncthreads();  // the tiles may be overwritten
+    shift = 1, pad = 0;
+    if constexpr (S::SETS == 1) __syncthreads();  // the tiles may be overwritten
+    else tile = tile == tiles ? tiles + SET : tiles;
+    if (more) store(tile);
+    __syncthreads();
   }
 
-  if constexpr (!STATE_ONLY) {  // rows past the sequence are zero
-    const int64_t from = begin > n ? begin : n;
-    for (int64_t i = threadIdx.x; i < (end - from) * width; i += THREADS) {
-      const int64_t at = ((batch * args.T + from + i / width) * args.heads + head) * DV + dv0 + i % width;
+  if constexpr (!STATE_ONLY) {  // rows past the sequence are zero; the segments share them out
+    const int64_t first = n + (args.T - n) * segment / args.segments, last = n + (args.T - n) * (segment + 1) / args.segments;
+    for (int64_t i = threadIdx.x; i < (last - first) * width; i += THREADS) {
+      const int64_t at = ((batch * args.T + first + i / width) * args.heads + head) * DV + dv0 + i % width;
       if (R.wide) static_cast<float*>(R.out)[at] = 0.0f;
       else static_cast<T*>(R.out)[at] = (T)0.0f;
     }
   }
-  if (STATE_ONLY || (whole && R.last)) {
-    // a reversed sequence's state stands at its first token; one decay more and the scale make it the error of the state before it
-    const float by = STATE_ONLY || n == 0 ? 1.0f : R.last_by * (reversed ? args.decay[head] : 1.0f);
-    float* to = STATE_ONLY ? R.carry + (unit * args.segments + segment) * DK * DV : R.last + unit * DK * DV;
+  if constexpr (STATE_ONLY) {
 #pragma unroll
     for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int w = 0; w < NW; ++w) carry[(w * M + m) * 64] = state[m][w];
+  } else if (whole && R.last) {
+    // a reversed sequence's state stands at its first token; one decay more and the scale make it the error of the state before it
+    const float by = R.last_by * (reversed ? args.decay[head] : 1.0f);
+    float* to = R.last + unit * DK * DV;
+    const float* from = R.first ? R.first + unit * DK * DV : nullptr;
+    const int rows = anew(DK), stride = anew(DV);
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
 #pragma unroll
       for (int w = 0; w < NW; ++w)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int row = row_of(m, i), col = dv0 + column_of(w);
-          if (row >= DK || col >= DV) continue;
+          const int row = state_row(m, lane, i), column = dv0 + state_column(NW * wave + w, lane);
+          if (row >= rows || column >= stride) continue;
           float x = state[m][w][i] * by;
-          if (!STATE_ONLY && n == 0) x = R.first ? R.first[unit * DK * DV + (int64_t)row * R.first_i + (int64_t)col * R.first_j] : 0.0f;
-          to[(int64_t)row * DV + col] = x;
+          if (n == 0) x = from ? from[(uint32_t)(row * R.first_i + column * R.first_j)] : 0.0f;  // as it was given
+          to[(uint32_t)(row * stride + column)] = x;
         }
+      in_steps();
+    }
   }
 }
 
 // ---- launches, one translation unit to each element type ---------------------------------------------------------------
 constexpr int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-// Columns of a workgroup: all of a narrow role's, else 128, or 64 where the state has 256 rows, so that it takes 64 registers.
-constexpr int block_columns(int DK, int DV) { return DV <= 32 ? 32 : DV <= 64 || DK > 128 ? 64 : 128; }
+// Columns of a workgroup, 32 to a wave.  (One wave brings in the rows of at most 64 columns of q and k by itself.)
+constexpr int block_columns(int DK, int DV) { return DV <= 32 && DK <= 64 ? 32 : DV <= 64 && DK <= 128 ? 64 : 128; }
+constexpr int blocks_of(int DK, int DV) { return (DV + block_columns(DK, DV) - 1) / block_columns(DK, DV); }
+// Floats of a state as the kernel holds it.
+constexpr int64_t carry_floats(int DK, int DV) { return (int64_t)padded(DK) * blocks_of(DK, DV) * block_columns(DK, DV); }
 
-template <class T, int DKP, int WAVES, int NW>
+template <class T, int DKP, int WAVES>
 int launch_scan(const Args& a, int roles, bool state_only, hipStream_t st) {
-  constexpr int CT = sizeof(T) == 2 && PIECES<T> == 1 ? 4 : 2;  // chunks of 64 tokens of one piece, of 32 of more
   int blocks = 1;
   for (int r = 0; r < roles; ++r) blocks = a.role[r].blocks > blocks ? a.role[r].blocks : blocks;
   const dim3 grid((unsigned)(a.units * a.segments * blocks), (unsigned)roles);
-  if (state_only) scan_kernel<T, DKP, CT, WAVES, NW, true><<<grid, 64 * WAVES, 0, st>>>(a);
-  else scan_kernel<T, DKP, CT, WAVES, NW, false><<<grid, 64 * WAVES, 0, st>>>(a);
+  const auto launch = [&](auto packed, auto only, auto exact) {
+    scan_kernel<T, DKP, WAVES, decltype(packed)::value, decltype(only)::value, decltype(exact)::value><<<grid, 64 * WAVES, 0, st>>>(a);
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  const std::bool_constant<PIECES<T> == 3> floats;  // (their pieces are three either way)
+  const auto any_exact = [&](auto packed) {
+    if (state_only) launch(packed, yes, yes);
+    else if (a.segments == 1) launch(packed, no, yes);
+    else launch(packed, no, floats);
+  };
+  if (a.role[0].packed) any_exact(yes);
+  else any_exact(no);
   return launch_status();
 }
 
 template <class T, int DKP>
 int launch_scan(const Args& a, int roles, int columns, bool state_only, hipStream_t st) {
-  if (columns == 32) return launch_scan<T, DKP, 2, 1>(a, roles, state_only, st);
-  if constexpr (DKP < 256)
-    if (columns == 128) return launch_scan<T, DKP, 4, 2>(a, roles, state_only, st);
-  return launch_scan<T, DKP, 4, 1>(a, roles, state_only, st);
+  if constexpr (DKP <= 64)
+    if (columns == 32) return launch_scan<T, DKP, 1>(a, roles, state_only, st);
+  if constexpr (DKP <= 128)
+    if (columns == 64) return launch_scan<T, DKP, 2>(a, roles, state_only, st);
+  return launch_scan<T, DKP, 4>(a, roles, state_only, st);
 }
 
 // One pass of all roles; those of one shape in one launch.

@@ -10,28 +10,47 @@ namespace {
 constexpr int CARRY_THREADS = 256;
 __global__ __launch_bounds__(CARRY_THREADS) void carry_kernel(Args args) {
   const Role& R = args.role[blockIdx.y];
-  const int64_t size = (int64_t)R.DK * R.DV, groups = (size + CARRY_THREADS - 1) / CARRY_THREADS;
+  const int64_t size = carry_floats(R.DK, R.DV) / 4, groups = (size + CARRY_THREADS - 1) / CARRY_THREADS;
   const int64_t unit = blockIdx.x / groups, at = blockIdx.x % groups * CARRY_THREADS + threadIdx.x;
   if (unit >= args.units || at >= size) return;
-  const int64_t batch = unit / args.heads, asked = args.lengths ? args.lengths[batch] : args.T;
-  const int64_t n = asked < 0 ? 0 : asked < args.T ? asked : args.T;
+  const int64_t n = length_of(args, unit / args.heads);
   const float a = args.decay[unit % args.heads];
+  // [tile of columns][tile of rows][lane]
+  const int tiles = padded(R.DK) / 16, lane = (int)(at & 63), row = state_row((int)((at >> 6) % tiles), lane, 0);
+  const int column = state_column((int)((at >> 6) / tiles), lane);
+  f4 raw{0.0f, 0.0f, 0.0f, 0.0f};
+  if (R.first && column < R.DV)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (row + i < R.DK) raw[i] = R.first[unit * R.DK * R.DV + (row + i) * R.first_i + column * R.first_j];
+  f4 run = raw * R.first_by;
+  f4* carry = reinterpret_cast<f4*>(R.carry) + unit * args.segments * size + at;
   const double log2a = log2((double)a);
   const auto power_of = [&](int64_t e) { return e > 0 ? (float)exp2(log2a * (double)e) : 1.0f; };
-  const float raw = R.first ? R.first[unit * size + at / R.DV * R.first_i + at % R.DV * R.first_j] : 0.0f;
-  float run = raw * R.first_by;
-  float* carry = R.carry + unit * args.segments * size + at;
   const float full = power_of(args.segment_length);
-  for (int j = 0; j < args.segments; ++j) {
-    const int64_t left = n - j * args.segment_length;
-    const float added = carry[j * size];
-    carry[j * size] = run;
-    if (left <= 0) continue;
-    const int64_t count = left < args.segment_length ? left : args.segment_length;
-    const float by = j == 0 && R.reversed ? power_of(count - 1) : count == args.segment_length ? full : power_of(count);
-    run = run * by + added;
+  constexpr int AHEAD = 8;
+  for (int j0 = 0; j0 < args.segments; j0 += AHEAD) {
+    f4 added[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (j0 + i < args.segments) added[i] = carry[(j0 + i) * size];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int j = j0 + i;
+      if (j >= args.segments) break;
+      carry[j * size] = run;
+      const int64_t begin = segment_begin(args, n, j), count = segment_end(args, n, j) - begin;
+      if (count == 0) continue;
+      const float by = begin == 0 ? power_of(R.reversed ? count - 1 : count) : full;
+      run = run * by + added[i];
+    }
   }
-  if (R.last) R.last[unit * size + at] = n == 0 ? raw : run * (R.last_by * (R.reversed ? a : 1.0f));
+  if (R.last && column < R.DV) {
+    run = n == 0 ? raw : run * (R.last_by * (R.reversed ? a : 1.0f));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (row + i < R.DK) R.last[(unit * R.DK + row + i) * R.DV + column] = run[i];
+  }
 }
 
 // ---- gradients of shared heads -----------------------------------------------------------------------------------------
@@ -136,8 +155,12 @@ bool heads_ok(const cnn_heads* h, int type) {
 // Rows made of whole packs at aligned addresses, whatever token, head and sequence.
 bool packed_ok(const cnn_heads* h, int width, int type) {
   const int64_t unit = 16 / (int64_t)type_bytes(type);
-  return aligned16(h->data) && width % 8 == 0 && h->batch % unit == 0 && h->token % unit == 0 && h->head % unit == 0;
+  return aligned16(h->data) && width % 8 == 0 && h->batch % unit == 0 && h->token % unit == 0 && h->head % unit == 0 &&
+         h->token * (int64_t)type_bytes(type) < 1 << 24;  // (the kernel multiplies by it in 24 bits)
 }
+
+// Results whose rows of one chunk lie less than 2^31 bytes apart.
+bool near_ok(const cnn_linear_shape* s) { return (int64_t)s->H * (s->Dk > s->Dv ? s->Dk : s->Dv) < 1 << 23; }
 
 Operand operand_of(const cnn_heads* h, int share) { return {h->data, h->batch, h->token, h->head, share}; }
 
@@ -150,19 +173,22 @@ struct Plan {
 
 size_t rounded(size_t b) { return (b + 255) & ~(size_t)255; }
 
-constexpr int64_t JOBS = 512, SEGMENT = 256;  // workgroups wanted; tokens to a segment, at least
+constexpr int64_t WAVES_WANTED = 2048;  // two to a SIMD
 
 Plan plan_of(const cnn_linear_shape& s, int roles) {
   Plan p{};
   const int64_t units = (int64_t)s.B * s.H;
-  const auto blocks = [](int dk, int dv) { return (dv + block_columns(dk, dv) - 1) / block_columns(dk, dv); };
-  const int64_t jobs = roles == 1 ? units * blocks(s.Dk, s.Dv) : units * (blocks(s.Dk, s.Dv) + 2 * blocks(s.Dv, s.Dk));
-  int64_t n = (JOBS + jobs - 1) / jobs, most = s.T / SEGMENT;
+  const auto waves = [](int dk, int dv) { return (int64_t)blocks_of(dk, dv) * block_columns(dk, dv) / (16 * NW); };
+  const int64_t at_once = units * (roles == 1 ? waves(s.Dk, s.Dv) : waves(s.Dk, s.Dv) + 2 * waves(s.Dv, s.Dk));
+  // Segments until the waves fill the GPU, but none whose state, written and read twice, is more to move than its tokens.
+  const int64_t least = 16 * (int64_t)s.Dk * s.Dv / (2 * (s.Dk + s.Dv) * (int64_t)type_bytes(s.type));
+  int64_t n = (WAVES_WANTED + at_once - 1) / at_once, most = s.T / (least > 2 * C ? least : 2 * C);
   n = n < most ? n : most;
   n = n < 1 ? 1 : n;
-  p.length = ((s.T + n - 1) / n + 63) / 64 * 64;
+  p.length = ((s.T + n - 1) / n + C - 1) / C * C;
   p.segments = (int)((s.T + p.length - 1) / p.length);
-  p.state_bytes = p.segments > 1 ? rounded((size_t)units * p.segments * s.Dk * s.Dv * 4) : 0;
+  const int64_t floats = carry_floats(s.Dk, s.Dv) > carry_floats(s.Dv, s.Dk) || roles == 1 ? carry_floats(s.Dk, s.Dv) : carry_floats(s.Dv, s.Dk);
+  p.state_bytes = p.segments > 1 ? rounded((size_t)units * p.segments * floats * 4) : 0;
   p.bytes = p.state_bytes * roles;
   if (roles > 1 && s.H != s.Hk) {
     p.wide_k = p.bytes;
@@ -182,11 +208,15 @@ Args args_of(const cnn_linear_shape& s, const Plan& p, const float* decay, const
 
 int run(Args& a, int type, int roles, hipStream_t st) {
   const auto scan = type == CNN_F32 ? run_scan_f32 : type == CNN_BF16 ? run_scan_bf16 : run_scan_f16;
-  for (int r = 0; r < roles; ++r) a.role[r].blocks = (a.role[r].DV + block_columns(a.role[r].DK, a.role[r].DV) - 1) / block_columns(a.role[r].DK, a.role[r].DV);
+  for (int r = 0; r < roles; ++r) a.role[r].blocks = blocks_of(a.role[r].DK, a.role[r].DV);
   if (a.segments > 1) {
     const int rc = scan(a, roles, true, st);
     if (rc != CNN_OK) return rc;
-    const int64_t groups = ((int64_t)a.role[0].DK * a.role[0].DV + CARRY_THREADS - 1) / CARRY_THREADS;
+    int64_t groups = 0;
+    for (int r = 0; r < roles; ++r) {
+      const int64_t g = (carry_floats(a.role[r].DK, a.role[r].DV) / 4 + CARRY_THREADS - 1) / CARRY_THREADS;
+      groups = g > groups ? g : groups;
+    }
     carry_kernel<<<dim3((unsigned)(a.units * groups), (unsigned)roles), CARRY_THREADS, 0, st>>>(a);
     if (launch_status() != CNN_OK) return CNN_EHIP;
   }
@@ -220,7 +250,7 @@ int cnn_linear_attention_fwd(const cnn_linear_shape* s, const cnn_heads* q, cons
   r.out = o, r.first = initial_state, r.last = final_state, r.carry = static_cast<float*>(workspace);
   r.first_i = s->Dv, r.first_j = 1, r.DK = s->Dk, r.DV = s->Dv;
   r.scale = scale, r.first_by = r.last_by = 1.0f;
-  r.packed = packed_ok(q, s->Dk, s->type) && packed_ok(k, s->Dk, s->type) && packed_ok(v, s->Dv, s->type);
+  r.packed = near_ok(s) && packed_ok(q, s->Dk, s->type) && packed_ok(k, s->Dk, s->type) && packed_ok(v, s->Dv, s->type);
   return run(a, s->type, 1, (hipStream_t)hip_stream);
 }
 
@@ -243,7 +273,7 @@ int cnn_linear_attention_bwd(const cnn_linear_shape* s, const cnn_heads* q, cons
   const int share = s->H / s->Hk;
   const Operand Q = operand_of(q, 1), K = operand_of(k, share), V = operand_of(v, share), D = operand_of(d_o, 1);
   const bool shared = share > 1;
-  const bool packed = packed_ok(q, s->Dk, s->type) && packed_ok(k, s->Dk, s->type) && packed_ok(v, s->Dv, s->type) && packed_ok(d_o, s->Dv, s->type);
+  const bool packed = near_ok(s) && packed_ok(q, s->Dk, s->type) && packed_ok(k, s->Dk, s->type) && packed_ok(v, s->Dv, s->type) && packed_ok(d_o, s->Dv, s->type);
   for (int i = 0; i < 3; ++i) {
     Role& r = a.role[i];
     r.carry = reinterpret_cast<float*>(ws + i * p.state_bytes);
