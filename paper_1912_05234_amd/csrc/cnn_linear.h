@@ -142,42 +142,45 @@ struct Shape {
 };
 
 // Units of eight elements of a tile that a thread brings from memory to LDS: one column of units, every STEP-th row.
+//
+// Rows that are no tokens (before `pad`, in a sequence's first chunk) and columns past the width repeat others, so that the loads
+// need no branches; what they add to a result is zero because k's are zeros in LDS: clear() and blank() see to that.
 template <class T, int ROWS, int WIDTH, int THREADS>
 struct Stage {
   static constexpr int COLUMNS = WIDTH / 8, STEP = THREADS / COLUMNS, EACH = (ROWS + STEP - 1) / STEP;
   static_assert(THREADS % COLUMNS == 0, "threads to a row");
   Pack<T, 8> u[EACH];
+  uint32_t at[EACH];  // PACKED: bytes from the chunk's lowest address, which is row 0's, or in reversed order the last row's
+  int width, stride;  // in elements
 
-  // Rows pad .. ROWS - 1, of `width` elements; `low` is where row 0 is or would be, or, in reversed order, the last row.  Rows
-  // before `pad` repeat row pad, so that the loads need no branches.
-  template <bool PACKED>
-  __device__ __forceinline__ void load(const T* low, int64_t stride, int pad, int width, bool reversed) {
-    const int c = threadIdx.x % COLUMNS * 8, row0 = threadIdx.x / COLUMNS;
-    const auto row_of = [&](int e) {
-      const int row = ROWS % STEP && row0 + e * STEP >= ROWS ? ROWS - 1 : row0 + e * STEP;
-      return reversed ? ROWS - 1 - row : row;
-    };
-    // (in reversed order the rows before pad are the last ones)
-    const auto kept = [&](int row) { return reversed ? (row < ROWS - pad ? row : ROWS - pad - 1) : (row > pad ? row : pad); };
-    if (c >= width) {
+  __device__ __forceinline__ int column() const { return threadIdx.x % COLUMNS * 8; }
+  __device__ __forceinline__ int row(int e) const {
+    const int r = threadIdx.x / COLUMNS + e * STEP;
+    return ROWS % STEP && r >= ROWS ? ROWS - 1 : r;
+  }
+  __device__ __forceinline__ int place(int row, int pad, bool reversed) const {
+    row = row > pad ? row : pad;
+    return reversed ? ROWS - 1 - row : row;
+  }
+  __device__ __forceinline__ void set(int columns, int64_t token_stride, int pad, bool reversed) {
+    width = columns, stride = (int)token_stride;
+    const int c = column() < width ? column() : 0;
 #pragma unroll
-      for (int e = 0; e < EACH; ++e)
+    for (int e = 0; e < EACH; ++e)  // (rows of a chunk are less than 2^31 bytes apart)
+      at[e] = __umul24(place(row(e), pad, reversed), (uint32_t)stride * (uint32_t)sizeof(T)) + c * (uint32_t)sizeof(T);
+  }
+  __device__ __forceinline__ void load(const T* low) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) u[e].v[j] = (T)0.0f;
-      return;
-    }
-    if constexpr (PACKED) {  // a chunk's rows are less than 2^31 bytes apart
-      const uint32_t step = (uint32_t)stride * (uint32_t)sizeof(T);
+    for (int e = 0; e < EACH; ++e) u[e] = *reinterpret_cast<const Pack<T, 8>*>(reinterpret_cast<const char*>(low) + at[e]);
+  }
+  // the same element by element, for any width, stride and alignment
+  __device__ __forceinline__ void load_any(const T* low, int64_t token_stride, int columns, int pad, bool reversed) {
+    const int c = column();
 #pragma unroll
-      for (int e = 0; e < EACH; ++e)
-        u[e] = *reinterpret_cast<const Pack<T, 8>*>(reinterpret_cast<const char*>(low) + (__umul24(kept(row_of(e)), step) + c * (uint32_t)sizeof(T)));
-    } else {
+    for (int e = 0; e < EACH; ++e) {
+      const T* from = low + place(row(e), pad, reversed) * token_stride;
 #pragma unroll
-      for (int e = 0; e < EACH; ++e) {
-        const T* row = low + kept(row_of(e)) * stride + c;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) u[e].v[j] = c + j < width ? row[j] : (T)0.0f;
-      }
+      for (int j = 0; j < 8; ++j) u[e].v[j] = c + j < columns ? from[c + j] : (T)0.0f;
     }
   }
 
@@ -190,14 +193,15 @@ struct Stage {
         if ((int)threadIdx.x / COLUMNS + e * STEP < pad) u[e].v[j] = (T)0.0f;
   }
 
+  // planes of [ROWS][STRIDE], one to a piece; `all`: columns past the width too
   template <int STRIDE>
-  __device__ __forceinline__ void store(__bf16* tile) const {  // planes of [ROWS][STRIDE], one to a piece
+  __device__ __forceinline__ void store(__bf16* tile, bool all) const {
     constexpr int NP = PIECES<T>;
-    const int c = threadIdx.x % COLUMNS * 8, row0 = threadIdx.x / COLUMNS;
+    if (!all && column() >= width) return;
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
-      const int row = row0 + e * STEP;
-      if (ROWS % STEP && row >= ROWS) continue;
+      const int r = threadIdx.x / COLUMNS + e * STEP;
+      if (ROWS % STEP && r >= ROWS) continue;
       bf8 piece[NP];
       if constexpr (NP == 1) {
         piece[0] = __builtin_bit_cast(bf8, u[e]);
@@ -208,8 +212,14 @@ struct Stage {
         cut<NP>(x, piece);
       }
 #pragma unroll
-      for (int p = 0; p < NP; ++p) *reinterpret_cast<bf8*>(tile + (p * ROWS + row) * STRIDE + c) = piece[p];
+      for (int p = 0; p < NP; ++p) *reinterpret_cast<bf8*>(tile + (p * ROWS + r) * STRIDE + column()) = piece[p];
     }
+  }
+  // columns past the width as zeros, once
+  template <int STRIDE>
+  __device__ __forceinline__ void blank(__bf16* tile) const {
+    if (column() < width) return;
+    for (int r = threadIdx.x / COLUMNS; r < PIECES<T> * ROWS; r += STEP) *reinterpret_cast<bf8*>(tile + r * STRIDE + column()) = bf8{};
   }
 };
 
@@ -262,17 +272,29 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
   const T *q = base(R.q), *k = base(R.k), *v = base(R.v) + dv0;
   const int64_t q_step = advance * R.q.token, k_step = advance * R.k.token, v_step = advance * R.v.token;
   const auto load = [&](int pad) {
-    k_in.template load<PACKED>(k, R.k.token, pad, DK, reversed);
-    v_in.template load<PACKED>(v, R.v.token, pad, width, reversed);
-    if (!STATE_ONLY) q_in.template load<PACKED>(q, R.q.token, pad, DK, reversed);
+    if constexpr (PACKED) {
+      k_in.load(k), v_in.load(v);
+      if (!STATE_ONLY) q_in.load(q);
+    } else {
+      k_in.load_any(k, R.k.token, DK, pad, reversed), v_in.load_any(v, R.v.token, width, pad, reversed);
+      if (!STATE_ONLY) q_in.load_any(q, R.q.token, DK, pad, reversed);
+    }
     q += q_step, k += k_step, v += v_step;
   };
   const auto store = [&](__bf16* tile) {
-    k_in.template store<S::QS>(tile + S::K);
-    v_in.template store<S::VS>(tile + S::V);
-    if (!STATE_ONLY) q_in.template store<S::QS>(tile + S::Q);
+    k_in.template store<S::QS>(tile + S::K, !PACKED);
+    v_in.template store<S::VS>(tile + S::V, true);
+    if (!STATE_ONLY) q_in.template store<S::QS>(tile + S::Q, true);
   };
+  const auto set = [&](int pad) {
+    k_in.set(DK, R.k.token, pad, reversed), v_in.set(width, R.v.token, pad, reversed);
+    if (!STATE_ONLY) q_in.set(DK, R.q.token, pad, reversed);
+  };
+  set(pad);
   if (begin < end) load(pad);
+  if (pad) set(0);
+  if (PACKED && DK < DKP)
+    for (int i = 0; i < S::SETS; ++i) k_in.template blank<S::QS>(tiles + i * SET + S::K);
 
   f4 state[M][NW];
   const bool whole = args.segments == 1;
@@ -322,6 +344,9 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
   const int out_stride = args.heads * DV, out_column = 16 * NW * wave + 4 * g;
   int64_t out = ((batch * args.T + low) * args.heads + head) * DV + dv0;
   const int64_t out_step = advance * out_stride;
+  const int out_at = (reversed ? C - 1 - r : r) * out_stride + out_column, out_next = reversed ? -16 * out_stride : 16 * out_stride;  // (of tile 1)
+  const float scale = R.scale;
+  const bool wide = R.wide;
 
   __bf16* tile = tiles;
   if (begin < end) {
@@ -422,23 +447,21 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
     if constexpr (!STATE_ONLY) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const int at = 16 * t + r, row = reversed ? C - 1 - at : at;
-        if (at < pad) continue;
+        if (16 * t + r < pad) continue;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          const f4 y = acc[t][w] * R.scale;
-          const int column = out_column + 16 * w;
+          const f4 y = acc[t][w] * scale;
           if constexpr (PACKED) {  // whole packs, so width is a multiple of eight; the chunk's rows are less than 2^31 bytes apart
-            if (column >= width) continue;
-            const uint32_t e = (uint32_t)(row * out_stride + column);
-            if (R.wide) *reinterpret_cast<f4*>(static_cast<float*>(R.out) + out + e) = y;
+            if (out_column + 16 * w >= width) continue;
+            const uint32_t e = (uint32_t)(out_at + t * out_next + 16 * w);
+            if (wide) *reinterpret_cast<f4*>(static_cast<float*>(R.out) + out + e) = y;
             else *reinterpret_cast<Pack<T, 4>*>(static_cast<T*>(R.out) + out + e) = Pack<T, 4>{{(T)y[0], (T)y[1], (T)y[2], (T)y[3]}};
           } else {
-            const int64_t e = out + (int64_t)row * out_stride + column;
+            const int64_t e = out + (int64_t)(reversed ? C - 1 - 16 * t - r : 16 * t + r) * args.heads * DV + out_column + 16 * w;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              if (column + i >= width) continue;
-              if (R.wide) static_cast<float*>(R.out)[e + i] = y[i];
+              if (out_column + 16 * w + i >= width) continue;
+              if (wide) static_cast<float*>(R.out)[e + i] = y[i];
               else static_cast<T*>(R.out)[e + i] = (T)y[i];
             }
           }
