@@ -5,7 +5,7 @@
 // A token outside [0, V) is padding: its output row is zero and its error goes nowhere.
 //
 // The gradient sorts the positions by token (a stable radix sort of eight bits a pass, padding left out in the first), cuts the
-// sorted list into tiles of equal length and lets one walker sum each tile's rows in order: a row whose tokens all lie in one
+// sorted list into tiles of equal length and lets one workgroup sum each tile's rows in order: a row whose tokens all lie in one
 // tile is finished there, the others leave partial sums that a second kernel adds tile by tile.  So every sum has a fixed order,
 // in fp32, whatever the distribution of the tokens: a token that a third of all positions hold costs what any other row costs.
 // (Adding into the table with atomics would be shorter, but its results change from run to run and bfloat16 has none.)
@@ -71,7 +71,8 @@ struct Entry {  // of the sorted list
 
 constexpr int RADIX = 256;
 constexpr int SORT_THREADS = 256, SORT_WAVES = SORT_THREADS / 64;
-constexpr int SORT_CHUNK = 2048;    // positions to a workgroup, at least
+constexpr int SORT_EACH = 8;        // positions that a lane holds at once, so that their loads are under way together
+constexpr int SORT_CHUNK = SORT_THREADS * SORT_EACH;  // positions to a workgroup, at least
 constexpr int SORT_GROUPS = 256;    // workgroups of a pass, at most: each adds up the counts of those before it
 constexpr int SMALL_THREADS = 1024, SMALL_WAVES = SMALL_THREADS / 64, SMALL_EACH = 4;
 constexpr int SMALL = SMALL_THREADS * SMALL_EACH;  // positions that one workgroup sorts in LDS
@@ -113,20 +114,37 @@ __device__ __forceinline__ bool entry_at(const SortArgs& a, int64_t i, int64_t e
   return (uint64_t)t < (uint64_t)a.V;
 }
 
+// Entries begin + 64 r + lane of a wave, r = 0 .. SORT_EACH - 1.
+template <class I, bool FIRST>
+__device__ __forceinline__ void entries_at(const SortArgs& a, int64_t begin, int64_t end, Entry (&e)[SORT_EACH], bool (&any)[SORT_EACH]) {
+#pragma unroll
+  for (int r = 0; r < SORT_EACH; ++r) {
+    e[r] = Entry{0, 0};
+    any[r] = entry_at<I, FIRST>(a, begin + 64 * r + (threadIdx.x & 63), end, e[r]);
+  }
+}
+
 template <class I, bool FIRST>
 __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(SortArgs a) {
   if ((int)blockIdx.x >= a.groups) return fill(a.clear, blockIdx.x - a.groups, gridDim.x - a.groups, SORT_THREADS);
-  __shared__ uint32_t count[RADIX];
-  count[threadIdx.x] = 0;
+  __shared__ uint32_t count[SORT_WAVES][RADIX];
+  const int wave = threadIdx.x >> 6;
+  for (int w = 0; w < SORT_WAVES; ++w) count[w][threadIdx.x] = 0;
   __syncthreads();
-  const int64_t begin = (int64_t)blockIdx.x * a.chunk, all = FIRST ? a.N : (int64_t)*a.total;
-  const int64_t end = begin + a.chunk < all ? begin + a.chunk : all;
-  for (int64_t i = begin + threadIdx.x; i < end; i += SORT_THREADS) {
-    Entry e;
-    if (entry_at<I, FIRST>(a, i, end, e)) atomicAdd(&count[e.token >> a.shift & (RADIX - 1)], 1u);
+  const int64_t all = FIRST ? a.N : (int64_t)*a.total, part = a.chunk / SORT_WAVES;
+  const int64_t begin = (int64_t)blockIdx.x * a.chunk + wave * part, end = begin + part < all ? begin + part : all;
+  for (int64_t i = begin; i < end; i += 64 * SORT_EACH) {
+    Entry e[SORT_EACH];
+    bool any[SORT_EACH];
+    entries_at<I, FIRST>(a, i, end, e, any);
+#pragma unroll
+    for (int r = 0; r < SORT_EACH; ++r)
+      if (any[r]) atomicAdd(&count[wave][e[r].token >> a.shift & (RADIX - 1)], 1u);
   }
   __syncthreads();
-  a.counts[(int64_t)blockIdx.x * RADIX + threadIdx.x] = count[threadIdx.x];
+  uint32_t sum = 0;
+  for (int w = 0; w < SORT_WAVES; ++w) sum += count[w][threadIdx.x];
+  a.counts[(int64_t)blockIdx.x * RADIX + threadIdx.x] = sum;
 }
 
 // Lanes of the wave that hold the same digit as this one, among those that hold any.
@@ -169,24 +187,29 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(SortArgs a) 
   if ((int)blockIdx.x >= a.groups) return fill(a.clear, blockIdx.x - a.groups, gridDim.x - a.groups, SORT_THREADS);
   __shared__ uint32_t place[SORT_WAVES][RADIX], sums[SORT_WAVES];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, digit = threadIdx.x;
+  const int64_t all = FIRST ? a.N : (int64_t)*a.total;
+  const int64_t part = a.chunk / SORT_WAVES;  // a multiple of 64 SORT_EACH
+  const int64_t begin = (int64_t)blockIdx.x * a.chunk + wave * part;
+  const int64_t end = begin + part < all ? begin + part : all;
+  Entry e[SORT_EACH];
+  bool any[SORT_EACH];
+  entries_at<I, FIRST>(a, begin, end, e, any);
   // entries of this thread's digit in earlier workgroups, and in all
   uint32_t before = 0, total = 0;
-#pragma unroll 8
+#pragma unroll 16
   for (int g = 0; g < a.groups; ++g) {
     const uint32_t c = a.counts[(int64_t)g * RADIX + digit];
-    if (g < (int)blockIdx.x) before += c;
+    before += g < (int)blockIdx.x ? c : 0;
     total += c;
   }
   for (int w = 0; w < SORT_WAVES; ++w) place[w][digit] = 0;
   const uint32_t base = before + exclusive_sum<SORT_WAVES>(total, sums);  // (its barrier also follows the clearing)
-  const int64_t all = FIRST ? a.N : (int64_t)*a.total;
   if (FIRST && blockIdx.x == 0 && threadIdx.x == RADIX - 1) *a.total = base - before + total;
-  const int64_t part = a.chunk / SORT_WAVES;  // a multiple of 64
-  const int64_t begin = (int64_t)blockIdx.x * a.chunk + wave * part;
-  const int64_t end = begin + part < all ? begin + part : all;
-  for (int64_t i = begin + lane; i < end; i += 64) {
-    Entry e;
-    if (entry_at<I, FIRST>(a, i, end, e)) atomicAdd(&place[wave][e.token >> a.shift & (RADIX - 1)], 1u);
+  for (int64_t i = begin; i < end; i += 64 * SORT_EACH) {
+    if (part > 64 * SORT_EACH) entries_at<I, FIRST>(a, i, end, e, any);
+#pragma unroll
+    for (int r = 0; r < SORT_EACH; ++r)
+      if (any[r]) atomicAdd(&place[wave][e[r].token >> a.shift & (RADIX - 1)], 1u);
   }
   __syncthreads();
   uint32_t next = base;
@@ -196,19 +219,21 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(SortArgs a) 
     next += c;
   }
   __syncthreads();
-  for (int64_t i = begin; i < end; i += 64) {  // (every lane of the wave makes every step)
-    Entry e{0, 0};
-    const bool any = entry_at<I, FIRST>(a, i + lane, end, e);
-    const uint32_t d = e.token >> a.shift & (RADIX - 1);
-    const uint64_t same = peers(d, any);
-    const int rank = __popcll(same & ((1ull << lane) - 1));
-    const uint32_t at = any ? place[wave][d] : 0;
-    wave_in_order();
-    if (any) {
-      if (rank == 0) place[wave][d] = at + (uint32_t)__popcll(same);
-      a.to[at + rank] = e;
+  for (int64_t i = begin; i < end; i += 64 * SORT_EACH) {  // (every lane of the wave makes every step)
+    if (part > 64 * SORT_EACH) entries_at<I, FIRST>(a, i, end, e, any);
+#pragma unroll
+    for (int r = 0; r < SORT_EACH; ++r) {
+      const uint32_t d = e[r].token >> a.shift & (RADIX - 1);
+      const uint64_t same = peers(d, any[r]);
+      const int rank = __popcll(same & ((1ull << lane) - 1));
+      const uint32_t at = any[r] ? place[wave][d] : 0;
+      wave_in_order();
+      if (any[r]) {
+        if (rank == 0) place[wave][d] = at + (uint32_t)__popcll(same);
+        a.to[at + rank] = e[r];
+      }
+      wave_in_order();
     }
-    wave_in_order();
   }
 }
 
@@ -278,9 +303,9 @@ struct SumArgs {
   void* d_table;
   const Entry* sorted;
   const uint32_t* total;
-  float* partial;  // [tile][2][columns rounded up to packs]: of the run that enters a tile, of the one that leaves it
+  float* partial;  // [tile][2][D]: of the run that enters a tile, of the one that leaves it
   int cols;        // of VN elements, per row
-  int lanes_log, tile;
+  int lanes_log, stretch, tile;  // entries of a walker, of a workgroup
   float scale;
 };
 
@@ -305,51 +330,79 @@ struct Sum {
   }
 };
 
-// A walker of 1 << lanes_log lanes takes a tile of the sorted list and 1 << lanes_log packs of the columns.
+// A walker of 1 << lanes_log lanes takes a stretch of the sorted list and 1 << lanes_log packs of the columns; a workgroup's walkers
+// take the stretches of one tile and add up, through LDS, the parts of rows that lie in more than one of them.
 constexpr int AHEAD = 8;
 template <class T, int VN>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(SumArgs a) {
   using P = Pack<T, VN>;
+  __shared__ float parts[2][EMBED_THREADS * VN];  // of the run that enters a stretch, of the one that leaves it
+  __shared__ bool through[EMBED_THREADS];         // by stretch: it is part of a run that goes on on both sides
   const P* d_out = static_cast<const P*>(a.d_out);
   T* d_table = static_cast<T*>(a.d_table);
-  const int64_t total = *a.total;
-  const int64_t tile = (int64_t)blockIdx.x * (EMBED_THREADS >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
-  const int c = (blockIdx.y << a.lanes_log) + (threadIdx.x & ((1 << a.lanes_log) - 1));
-  const int64_t begin = tile * a.tile, end = begin + a.tile < total ? begin + a.tile : total;
-  if (begin >= end || c >= a.cols) return;
-  const int64_t width = (int64_t)a.cols * VN;
-  uint32_t token = a.sorted[begin].token;
-  bool inside = begin == 0 || a.sorted[begin - 1].token != token;  // the present run began in this tile
+  const int64_t total = *a.total, width = (int64_t)a.cols * VN;
+  const int walkers = EMBED_THREADS >> a.lanes_log, walker = threadIdx.x >> a.lanes_log, lane = threadIdx.x & ((1 << a.lanes_log) - 1);
+  const int c = (blockIdx.y << a.lanes_log) + lane;
+  const int64_t begin = (int64_t)blockIdx.x * a.tile + (int64_t)walker * a.stretch;
+  const int64_t end = begin + a.stretch < total ? begin + a.stretch : total;
+  const bool busy = begin < end && c < a.cols;
+  uint32_t token = busy ? a.sorted[begin].token : 0;
+  const bool entered = busy && begin > 0 && a.sorted[begin - 1].token == token;
+  bool inside = !entered;  // the present run began in this stretch
   Sum<VN> sum;
   sum.clear();
-  for (int64_t i = begin; i < end; i += AHEAD) {
-    Entry e[AHEAD];
-    P row[AHEAD];
+  const auto keep = [&](int which) {
 #pragma unroll
-    for (int r = 0; r < AHEAD; ++r)
-      if (i + r < end) e[r] = a.sorted[i + r];
+    for (int j = 0; j < VN; ++j) parts[which][j * EMBED_THREADS + threadIdx.x] = sum.v[j];
+  };
+  if (busy)
+    for (int64_t i = begin; i < end; i += AHEAD) {
+      Entry e[AHEAD];
+      P row[AHEAD];
 #pragma unroll
-    for (int r = 0; r < AHEAD; ++r)
-      if (i + r < end) row[r] = d_out[(int64_t)e[r].position * a.cols + c];
+      for (int r = 0; r < AHEAD; ++r)
+        if (i + r < end) e[r] = a.sorted[i + r];
 #pragma unroll
-    for (int r = 0; r < AHEAD; ++r) {
-      if (i + r >= end) break;
-      if (e[r].token != token) {
-        if (inside)
-          sum.store(d_table + token * width, c, a.scale);
-        else
-          sum.store(a.partial + 2 * tile * width, c, 1.0f);
-        sum.clear();
-        token = e[r].token, inside = true;
+      for (int r = 0; r < AHEAD; ++r)
+        if (i + r < end) row[r] = d_out[(int64_t)e[r].position * a.cols + c];
+#pragma unroll
+      for (int r = 0; r < AHEAD; ++r) {
+        if (i + r >= end) break;
+        if (e[r].token != token) {
+          if (inside) sum.store(d_table + token * width, c, a.scale);
+          else keep(0);
+          sum.clear();
+          token = e[r].token, inside = true;
+        }
+        sum.add(row[r]);
       }
-      sum.add(row[r]);
     }
+  const bool leaves = busy && end < total && a.sorted[end].token == token;
+  if (busy && inside && !leaves) sum.store(d_table + token * width, c, a.scale);
+  else if (busy) keep(inside);
+  if (lane == 0) through[walker] = busy && !inside && leaves;  // (the first column of a block is never past the width)
+  __syncthreads();
+  // The run that leaves this stretch: the parts that entered the next ones, up to the stretch or the tile where it ends.
+  const auto follow = [&](int which) {
+#pragma unroll
+    for (int j = 0; j < VN; ++j) sum.v[j] = parts[which][j * EMBED_THREADS + threadIdx.x];
+    int w = walker;
+    bool on = which == 1 || through[w];
+    while (on && ++w < walkers) {
+#pragma unroll
+      for (int j = 0; j < VN; ++j) sum.v[j] += parts[0][j * EMBED_THREADS + (w << a.lanes_log) + lane];
+      on = through[w];
+    }
+    return on;  // it leaves the tile
+  };
+  if (busy && inside && leaves) {
+    if (follow(1)) sum.store(a.partial + (2 * (int64_t)blockIdx.x + 1) * width, c, 1.0f);
+    else sum.store(d_table + token * width, c, a.scale);
   }
-  const bool leaves = end < total && a.sorted[end].token == token;
-  if (inside && !leaves)
-    sum.store(d_table + token * width, c, a.scale);
-  else
-    sum.store(a.partial + (2 * tile + inside) * width, c, 1.0f);
+  if (walker == 0 && entered) {
+    follow(0);
+    sum.store(a.partial + 2 * (int64_t)blockIdx.x * width, c, 1.0f);
+  }
 }
 
 // Rows whose tokens lie in more than one tile: the part that left the tile where they began, then the parts that entered the
@@ -382,15 +435,6 @@ __global__ __launch_bounds__(JOIN_THREADS) void embed_join_kernel(SumArgs a) {
 #pragma unroll
         for (int j = 0; j < JOIN_FEW; ++j)
           if (parts == (uint32_t)j + 1 && at[j] == token) ++parts;
-        if (parts == JOIN_FEW + 1) {
-          int64_t low = end + 1, high = total;  // the first entry past the run
-          while (low < high) {
-            const int64_t mid = (low + high) >> 1;
-            if (a.sorted[mid].token == token) low = mid + 1;
-            else high = mid;
-          }
-          parts = (uint32_t)((low - 1) / a.tile - tile + 1);
-        }
       }
     }
     begun[threadIdx.x][0] = parts, begun[threadIdx.x][1] = token;
@@ -412,12 +456,19 @@ __global__ __launch_bounds__(JOIN_THREADS) void embed_join_kernel(SumArgs a) {
     sum.store(d_table + begun[k][1] * width, c, a.scale);
   }
   for (int k = 0; k < JOIN_TILES; ++k) {
-    const int64_t parts = begun[k][0];
-    if (parts <= JOIN_FEW) continue;  // (the same for the whole workgroup)
+    if (begun[k][0] <= JOIN_FEW) continue;  // (the same for the whole workgroup)
+    // tiles that begin with the row's token: every wave looks at 64 places at a time
+    int64_t low = first + k + JOIN_FEW, high = (total + a.tile - 1) / a.tile;  // the last one known, one past the last
+    while (high - low > 1) {
+      const int64_t step = (high - low + 63) / 64, at = low + step * ((threadIdx.x & 63) + 1);
+      low += step * __popcll(__ballot(at < high && a.sorted[at * a.tile].token == begun[k][1]));
+      high = low + step < high ? low + step : high;
+    }
+    const int64_t parts = low - (first + k) + 1;
     Sum<VN> sum;
     sum.clear();
     if (c < a.cols) {
-#pragma unroll 4
+#pragma unroll 8
       for (int64_t p = group; p < parts; p += groups) sum.add(part(first + k, p));
     }
 #pragma unroll
@@ -426,6 +477,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void embed_join_kernel(SumArgs a) {
     const int used = parts < groups ? (int)parts : groups;  // walkers that had a part
     for (int i = threadIdx.x; i < VN * lanes; i += JOIN_THREADS) {
       float s = 0.0f;
+#pragma unroll 8
       for (int g = 0; g < used; ++g) s += lds[g * VN * lanes + i];
       lds[i] = s;
     }
@@ -453,7 +505,7 @@ int lanes_log_for(int cols, int most) {
 }
 
 struct EmbedPlan {
-  int64_t groups, chunk, tiles, tile, columns;
+  int64_t groups, chunk, tiles, stretch, tile, columns;
   int pack, lanes_log, passes;
   bool small;
   size_t list, list_bytes, counts, partial, bytes;  // offsets and sizes in the workspace; the number of entries is at its start
@@ -473,9 +525,10 @@ EmbedPlan embed_plan(int64_t N, int64_t V, int D, int type) {
   const int cols = D / p.pack;
   p.lanes_log = lanes_log_for(cols, 6);
   p.columns = (cols + (1 << p.lanes_log) - 1) >> p.lanes_log;
-  // short tiles keep many loads in flight, long ones leave few partial sums
-  p.tile = 16;
-  while (p.tile < 512 && (N / p.tile * p.columns << p.lanes_log) / 64 > SUM_WAVES) p.tile *= 2;
+  // short stretches keep many loads in flight, long ones leave few partial sums
+  p.stretch = 16;
+  while (p.stretch < 512 && (N / p.stretch * p.columns << p.lanes_log) / 64 > SUM_WAVES) p.stretch *= 2;
+  p.tile = p.stretch * (EMBED_THREADS >> p.lanes_log);
   p.tiles = (N + p.tile - 1) / p.tile;
   const auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
   p.list = 256;
@@ -530,8 +583,7 @@ int sort_tokens(const EmbedPlan& p, SortArgs a, char* ws, size_t table_bytes, hi
 
 template <class T, int VN>
 int sum_rows(const EmbedPlan& p, const SumArgs& a, hipStream_t st) {
-  const int walkers = EMBED_THREADS >> p.lanes_log;
-  embed_sum_kernel<T, VN><<<dim3((unsigned)((p.tiles + walkers - 1) / walkers), (unsigned)p.columns), EMBED_THREADS, 0, st>>>(a);
+  embed_sum_kernel<T, VN><<<dim3((unsigned)p.tiles, (unsigned)p.columns), EMBED_THREADS, 0, st>>>(a);
   if (p.tiles > 1)
     embed_join_kernel<T, VN><<<dim3((unsigned)((p.tiles + JOIN_TILES - 1) / JOIN_TILES), (unsigned)p.columns), JOIN_THREADS, 0, st>>>(a);
   return launch_status();
@@ -598,7 +650,7 @@ int cnn_embedding_bwd(const void* d_out, const void* tokens, void* d_table, int6
   const int rc = wide_tokens ? sort_tokens<int64_t>(p, s, ws, table_bytes, st) : sort_tokens<int32_t>(p, s, ws, table_bytes, st);
   if (rc != CNN_OK) return rc;
   const SumArgs a{d_out, d_table, reinterpret_cast<Entry*>(ws + p.list), s.total, reinterpret_cast<float*>(ws + p.partial), D / p.pack,
-                  p.lanes_log, (int)p.tile, scale};
+                  p.lanes_log, (int)p.stretch, (int)p.tile, scale};
   return with_pack(type, p.pack, [&](auto t, auto n) { return sum_rows<decltype(t), decltype(n)::value>(p, a, st); });
 }
 

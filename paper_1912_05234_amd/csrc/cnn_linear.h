@@ -51,6 +51,7 @@ struct Role {
   const float* first;  // state before the sequence, nullable: element (i, j) of unit u at u * DK * DV + i * first_i + j * first_j
   float* last;         // state after it, nullable, [unit][DK][DV]
   float* carry;        // [unit][segment], states in the order of the kernel's registers
+  const float* flipped;  // instead: those of a role whose states are this one's transposed
   int first_i, first_j;
   int DK, DV, blocks;  // blocks of columns
   float scale, first_by, last_by;
@@ -136,7 +137,10 @@ struct Shape {
   static constexpr int NP = PIECES<T>, MP = at_least_two(NP);  // pieces of the inputs, and of state and scores
   // rows of q and k are read sixteen bytes to a lane, of v and k also four rows to a lane: the padding spreads them over the banks
   static constexpr int QS = DKP + 8, VS = DVC + 16;
-  static constexpr int K = 0, V = K + NP * C * QS, Q = V + NP * C * VS, ALL = Q + NP * C * QS;  // offsets of the tiles in LDS
+  // A single wave of narrow rows takes q from memory in the order of its operands: without it in LDS eight waves of floats fit a
+  // compute unit, not six.
+  static constexpr bool Q_DIRECT = WAVES == 1 && DKP == 32;
+  static constexpr int K = 0, V = K + NP * C * QS, Q = V + NP * C * VS, ALL = Q + (Q_DIRECT ? 0 : NP * C * QS);  // offsets of the tiles in LDS
   // two sets of tiles, and one barrier a chunk, where eight waves of a compute unit have room for them
   static constexpr int SETS = 2 * ALL * 2 <= 20 * 1024 * WAVES ? 2 : 1;
 };
@@ -223,6 +227,61 @@ struct Stage {
   }
 };
 
+__host__ __device__ constexpr int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+// Columns of a workgroup, 32 to a wave.  (One wave brings in the rows of at most 64 columns of q and k by itself.)
+__host__ __device__ constexpr int block_columns(int DK, int DV) { return DV <= 32 && DK <= 64 ? 32 : DV <= 64 && DK <= 128 ? 64 : 128; }
+__host__ __device__ constexpr int blocks_of(int DK, int DV) { return (DV + block_columns(DK, DV) - 1) / block_columns(DK, DV); }
+// Floats of a state as the kernel holds it.
+__host__ __device__ constexpr int64_t carry_floats(int DK, int DV) { return (int64_t)padded(DK) * blocks_of(DK, DV) * block_columns(DK, DV); }
+
+// Rows of q of a single wave, as operands of its products: row 16 t + lane % 16, columns 32 s + 8 (lane / 16) .. + 7.
+template <class T, int DKP>
+struct Direct {
+  static constexpr int ST = DKP / 32;
+  Pack<T, 8> u[2][ST];
+  uint32_t at[2];
+  int column;  // as far as it is one; a column past the width meets zeros of k
+
+  __device__ __forceinline__ int place(int t, int pad, bool reversed) const {
+    int row = 16 * t + (threadIdx.x & 15);
+    row = row > pad ? row : pad;
+    return reversed ? C - 1 - row : row;
+  }
+  __device__ __forceinline__ void set(int width, int64_t token_stride, int pad, bool reversed) {
+    column = threadIdx.x / 16 % 4 * 8 < width ? threadIdx.x / 16 % 4 * 8 : 0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) at[t] = __umul24(place(t, pad, reversed), (uint32_t)token_stride * (uint32_t)sizeof(T)) + column * (uint32_t)sizeof(T);
+  }
+  __device__ __forceinline__ void load(const T* low) {
+    static_assert(ST == 1, "columns of one step");
+#pragma unroll
+    for (int t = 0; t < 2; ++t) u[t][0] = *reinterpret_cast<const Pack<T, 8>*>(reinterpret_cast<const char*>(low) + at[t]);
+  }
+  __device__ __forceinline__ void load_any(const T* low, int64_t token_stride, int width, int pad, bool reversed) {
+    const int c = threadIdx.x / 16 % 4 * 8;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const T* from = low + place(t, pad, reversed) * token_stride;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) u[t][0].v[j] = c + j < width ? from[c + j] : (T)0.0f;
+    }
+  }
+  template <int NP>
+  __device__ __forceinline__ void pieces(bf8 (&out)[2][NP]) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if constexpr (NP == 1) {
+        out[t][0] = __builtin_bit_cast(bf8, u[t][0]);
+      } else {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = (float)u[t][0].v[j];
+        cut<NP>(x, out[t]);
+      }
+    }
+  }
+};
+
 // log2 of a decay, finite also for a = 0 (a^0 = 1 and a^n = 0 then come out right), to fp32 also next to 1.
 __device__ __forceinline__ float log2_decay(float a) {
   const double l = log2((double)a);
@@ -241,6 +300,11 @@ __device__ __forceinline__ int anew(int x) {
 // Where a state's register i of tile m of a wave's lane stands.  A pair of tiles is an operand of a product over 32 rows as it is.
 __device__ __forceinline__ int state_row(int m, int lane, int i) { return 32 * (m >> 1) + 8 * (lane >> 4) + 4 * (m & 1) + i; }
 __device__ __forceinline__ int state_column(int tile, int lane) { return 16 * tile + (lane & 15); }  // tile: of sixteen columns
+// The other way: index of an element in a state of `tiles` tiles of rows to a tile of columns.
+__device__ __forceinline__ uint32_t state_index(int row, int column, int tiles) {
+  const int m = 2 * (row >> 5) + (row >> 2 & 1), lane = 16 * (row >> 3 & 3) + (column & 15);
+  return (uint32_t)((((column >> 4) * tiles + m) * 64 + lane) * 4 + (row & 3));
+}
 
 constexpr int waves_wanted(int DKP) { return DKP <= 128 ? 2 : 1; }  // to a SIMD
 
@@ -265,8 +329,10 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
 
   // Chunks end where the segment does; the first one may begin before it, with `pad` rows that are no tokens.
   int pad = (int)((C - (end - begin) % C) % C);
-  Stage<T, C, DKP, THREADS> q_in, k_in;
+  std::conditional_t<S::Q_DIRECT, Direct<T, 32>, Stage<T, C, DKP, THREADS>> q_in;
+  Stage<T, C, DKP, THREADS> k_in;
   Stage<T, C, S::DVC, THREADS> v_in;
+  bf8 direct[2][NP];  // q's operands of the present chunk, where they do not pass through LDS
   const int64_t low = reversed ? n - (begin - pad) - C : begin - pad, advance = reversed ? -C : C;  // in tokens
   const auto base = [&](const Operand& o) { return static_cast<const T*>(o.data) + batch * o.batch + head / o.share * o.head + low * o.token; };
   const T *q = base(R.q), *k = base(R.k), *v = base(R.v) + dv0;
@@ -284,7 +350,9 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
   const auto store = [&](__bf16* tile) {
     k_in.template store<S::QS>(tile + S::K, !PACKED);
     v_in.template store<S::VS>(tile + S::V, true);
-    if (!STATE_ONLY) q_in.template store<S::QS>(tile + S::Q, true);
+    if constexpr (STATE_ONLY) return;
+    else if constexpr (S::Q_DIRECT) q_in.pieces(direct);
+    else q_in.template store<S::QS>(tile + S::Q, true);
   };
   const auto set = [&](int pad) {
     k_in.set(DK, R.k.token, pad, reversed), v_in.set(width, R.v.token, pad, reversed);
@@ -304,7 +372,20 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
   for (int m = 0; m < M; ++m)
 #pragma unroll
     for (int w = 0; w < NW; ++w) state[m][w] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-  if (!STATE_ONLY && !whole) {
+  if (!STATE_ONLY && !whole && R.flipped) {
+    const float* from = R.flipped + (unit * args.segments + segment) * carry_floats(DV, DK);
+    const int tiles = padded(DV) / 16;
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+#pragma unroll
+      for (int w = 0; w < NW; ++w)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = state_row(m, lane, i), column = dv0 + state_column(NW * wave + w, lane);
+          if (row < DK && column < DV) state[m][w][i] = from[state_index(column, row, tiles)];
+        }
+    }
+  } else if (!STATE_ONLY && !whole) {
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
@@ -372,7 +453,8 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int z = 0; z < NP; ++z) {
-            query[t][z] = *reinterpret_cast<const bf8*>(tile + S::Q + (z * C + 16 * t + r) * S::QS + 32 * s + 8 * g);
+            if constexpr (S::Q_DIRECT) query[t][z] = direct[t][z];
+            else query[t][z] = *reinterpret_cast<const bf8*>(tile + S::Q + (z * C + 16 * t + r) * S::QS + 32 * s + 8 * g);
             row[t][z] = *reinterpret_cast<const bf8*>(tile + S::K + (z * C + 16 * t + r) * S::QS + 32 * s + 8 * g);
           }
         p00 = product(row[0], query[0], p00);
@@ -513,13 +595,6 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
 }
 
 // ---- launches, one translation unit to each element type ---------------------------------------------------------------
-constexpr int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-// Columns of a workgroup, 32 to a wave.  (One wave brings in the rows of at most 64 columns of q and k by itself.)
-constexpr int block_columns(int DK, int DV) { return DV <= 32 && DK <= 64 ? 32 : DV <= 64 && DK <= 128 ? 64 : 128; }
-constexpr int blocks_of(int DK, int DV) { return (DV + block_columns(DK, DV) - 1) / block_columns(DK, DV); }
-// Floats of a state as the kernel holds it.
-constexpr int64_t carry_floats(int DK, int DV) { return (int64_t)padded(DK) * blocks_of(DK, DV) * block_columns(DK, DV); }
-
 template <class T, int DKP, int WAVES>
 int launch_scan(const Args& a, int roles, bool state_only, hipStream_t st) {
   int blocks = 1;

@@ -54,14 +54,34 @@ __global__ __launch_bounds__(CARRY_THREADS) void carry_kernel(Args args) {
 }
 
 // ---- gradients of shared heads -----------------------------------------------------------------------------------------
-// out[row][h][d] = sum over the query heads of h of part[row][head][d], part in fp32.
-template <class T>
-__global__ __launch_bounds__(256) void share_kernel(const float* part, T* out, int64_t total, int share, int width) {
+// out[row][h][d] = sum over the query heads of h of part[row][head][d], part in fp32; for d_k and d_v.
+struct ShareArgs {
+  const float* part[2];
+  void* out[2];
+  int64_t rows;  // times key heads
+  int width[2], share;
+};
+
+template <class T, int VN>
+__global__ __launch_bounds__(256) void share_kernel(ShareArgs a) {
+  using P = Pack<float, VN>;
+  const int width = a.width[blockIdx.y] / VN, share = a.share;
+  const P* part = reinterpret_cast<const P*>(a.part[blockIdx.y]);
+  Pack<T, VN>* out = static_cast<Pack<T, VN>*>(a.out[blockIdx.y]);
+  const int64_t total = a.rows * width;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const float* p = part + i / width * share * width + i % width;
-    float s = 0.0f;
-    for (int h = 0; h < share; ++h) s += p[(int64_t)h * width];
-    out[i] = (T)s;
+    const int64_t row = total < (int64_t)1 << 32 ? (uint32_t)i / (uint32_t)width : i / width;
+    const P* p = part + row * share * width + (i - row * width);
+    P sum = p[0];
+    for (int h = 1; h < share; ++h) {
+      const P q = p[(int64_t)h * width];
+#pragma unroll
+      for (int j = 0; j < VN; ++j) sum.v[j] += q.v[j];
+    }
+    Pack<T, VN> r;
+#pragma unroll
+    for (int j = 0; j < VN; ++j) r.v[j] = (T)sum.v[j];
+    out[i] = r;
   }
 }
 
@@ -189,7 +209,7 @@ Plan plan_of(const cnn_linear_shape& s, int roles) {
   p.segments = (int)((s.T + p.length - 1) / p.length);
   const int64_t floats = carry_floats(s.Dk, s.Dv) > carry_floats(s.Dv, s.Dk) || roles == 1 ? carry_floats(s.Dk, s.Dv) : carry_floats(s.Dv, s.Dk);
   p.state_bytes = p.segments > 1 ? rounded((size_t)units * p.segments * floats * 4) : 0;
-  p.bytes = p.state_bytes * roles;
+  p.bytes = p.state_bytes * (roles > 1 ? 2 : 1);  // (d_k's states are d_v's transposed)
   if (roles > 1 && s.H != s.Hk) {
     p.wide_k = p.bytes;
     p.wide_v = p.wide_k + rounded((size_t)units * s.T * s.Dk * 4);
@@ -210,14 +230,18 @@ int run(Args& a, int type, int roles, hipStream_t st) {
   const auto scan = type == CNN_F32 ? run_scan_f32 : type == CNN_BF16 ? run_scan_bf16 : run_scan_f16;
   for (int r = 0; r < roles; ++r) a.role[r].blocks = blocks_of(a.role[r].DK, a.role[r].DV);
   if (a.segments > 1) {
-    const int rc = scan(a, roles, true, st);
-    if (rc != CNN_OK) return rc;
+    Args own = a;  // the roles that have states of their own
+    int count = 0;
     int64_t groups = 0;
     for (int r = 0; r < roles; ++r) {
+      if (a.role[r].flipped) continue;
+      own.role[count++] = a.role[r];
       const int64_t g = (carry_floats(a.role[r].DK, a.role[r].DV) / 4 + CARRY_THREADS - 1) / CARRY_THREADS;
       groups = g > groups ? g : groups;
     }
-    carry_kernel<<<dim3((unsigned)(a.units * groups), (unsigned)roles), CARRY_THREADS, 0, st>>>(a);
+    const int rc = scan(own, count, true, st);
+    if (rc != CNN_OK) return rc;
+    carry_kernel<<<dim3((unsigned)(a.units * groups), (unsigned)count), CARRY_THREADS, 0, st>>>(own);
     if (launch_status() != CNN_OK) return CNN_EHIP;
   }
   return scan(a, roles, false, st);
@@ -276,7 +300,7 @@ int cnn_linear_attention_bwd(const cnn_linear_shape* s, const cnn_heads* q, cons
   const bool packed = near_ok(s) && packed_ok(q, s->Dk, s->type) && packed_ok(k, s->Dk, s->type) && packed_ok(v, s->Dv, s->type) && packed_ok(d_o, s->Dv, s->type);
   for (int i = 0; i < 3; ++i) {
     Role& r = a.role[i];
-    r.carry = reinterpret_cast<float*>(ws + i * p.state_bytes);
+    r.carry = reinterpret_cast<float*>(ws + (i ? p.state_bytes : 0));
     r.scale = scale, r.packed = packed, r.first_by = r.last_by = 1.0f;
     r.reversed = i > 0, r.wide = i > 0 && shared;
     r.DK = i < 2 ? s->Dv : s->Dk, r.DV = i < 2 ? s->Dk : s->Dv;
@@ -288,17 +312,19 @@ int cnn_linear_attention_bwd(const cnn_linear_shape* s, const cnn_heads* q, cons
   a.role[1].q = V, a.role[1].k = D, a.role[1].v = Q, a.role[1].out = shared ? ws + p.wide_k : d_k;
   a.role[2].q = K, a.role[2].k = Q, a.role[2].v = D, a.role[2].out = shared ? ws + p.wide_v : d_v;
   a.role[2].last = d_initial_state;
+  if (p.segments > 1) a.role[1].flipped = a.role[2].carry;
   hipStream_t st = (hipStream_t)hip_stream;
   const int rc = run(a, s->type, 3, st);
   if (rc != CNN_OK || !shared) return rc;
   return with_type(s->type, [&](auto t) {
     using T = decltype(t);
-    for (int i = 0; i < 2; ++i) {
-      const int width = i ? s->Dv : s->Dk;
-      const int64_t total = (int64_t)s->B * s->T * s->Hk * width, groups = (total + 255) / 256;
-      share_kernel<T><<<(unsigned)(groups < 8192 ? groups : 8192), 256, 0, st>>>(reinterpret_cast<const float*>(ws + (i ? p.wide_v : p.wide_k)),
-                                                                                static_cast<T*>(i ? d_v : d_k), total, share, width);
-    }
+    const ShareArgs g{{reinterpret_cast<const float*>(ws + p.wide_k), reinterpret_cast<const float*>(ws + p.wide_v)}, {d_k, d_v},
+                      (int64_t)s->B * s->T * s->Hk, {s->Dk, s->Dv}, share};
+    const bool fours = s->Dk % 4 == 0 && s->Dv % 4 == 0;
+    const int64_t groups = (g.rows * (s->Dk > s->Dv ? s->Dk : s->Dv) / (fours ? 4 : 1) + 255) / 256;
+    const dim3 grid((unsigned)(groups < 4096 ? groups : 4096), 2);
+    if (fours) share_kernel<T, 4><<<grid, 256, 0, st>>>(g);
+    else share_kernel<T, 1><<<grid, 256, 0, st>>>(g);
     return launch_status();
   });
 }
