@@ -136,7 +136,7 @@ struct Shape {
   static constexpr int DVC = WAVES * 16 * NW, THREADS = 64 * WAVES;
   static constexpr int NP = PIECES<T>, MP = at_least_two(NP);  // pieces of the inputs, and of state and scores
   // rows of q and k are read sixteen bytes to a lane, of v and k also four rows to a lane: the padding spreads them over the banks
-  static constexpr int QS = DKP + 8, VS = DVC + 16;
+  static constexpr int QS = DKP + 8, VS = DVC + (WAVES == 1 ? 8 : 16);
   // A single wave of narrow rows takes q from memory in the order of its operands: without it in LDS eight waves of floats fit a
   // compute unit, not six.
   static constexpr bool Q_DIRECT = WAVES == 1 && DKP == 32;
@@ -489,7 +489,8 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
     }
 
     // the scores' product with V; the state: decayed, and the chunk's products added
-    const float by = power(log2a, C - pad + shift - 1);
+    // (the first pass leaves the state as it is and weights each token by what is left of its segment: fewer products)
+    const float by = power(log2a, STATE_ONLY ? (int)(end - t0 - C) : C - pad + shift - 1);
     bf8 weighted[NW][WP];
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
@@ -505,7 +506,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
         x[j] = 0.0f;
 #pragma unroll
         for (int z = NP - 1; z >= 0; --z) x[j] += (float)raw[z][j];
-        x[j] *= follow[j];
+        x[j] *= STATE_ONLY ? follow[j] * by : follow[j];
       }
       cut<WP>(x, weighted[w]);
       if constexpr (!STATE_ONLY) {
@@ -522,7 +523,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
         a[z] = joined(read_transposed(p), read_transposed(p + 16 * S::QS));
       }
 #pragma unroll
-      for (int w = 0; w < NW; ++w) state[m][w] = product(a, weighted[w], state[m][w] * by);
+      for (int w = 0; w < NW; ++w) state[m][w] = product(a, weighted[w], STATE_ONLY ? state[m][w] : state[m][w] * by);
       if ((m & 3) == 3 || (NP > 1 && (m & 1))) in_steps();
     }
 
@@ -559,11 +560,21 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
   }
 
   if constexpr (!STATE_ONLY) {  // rows past the sequence are zero; the segments share them out
-    const int64_t first = n + (args.T - n) * segment / args.segments, last = n + (args.T - n) * (segment + 1) / args.segments;
-    for (int64_t i = threadIdx.x; i < (last - first) * width; i += THREADS) {
-      const int64_t at = ((batch * args.T + first + i / width) * args.heads + head) * DV + dv0 + i % width;
-      if (R.wide) static_cast<float*>(R.out)[at] = 0.0f;
-      else static_cast<T*>(R.out)[at] = (T)0.0f;
+    const int64_t past = args.T - n, first = n + past * segment / args.segments, last = n + past * (segment + 1) / args.segments;
+    constexpr int LANES = S::DVC / 4, ROWS = THREADS / LANES;
+    const int column = threadIdx.x % LANES * 4;
+    for (int64_t t = first + threadIdx.x / LANES; t < last; t += ROWS) {
+      const int64_t at = ((batch * args.T + t) * args.heads + head) * DV + dv0 + column;
+      if (PACKED && column < width) {
+        if (wide) *reinterpret_cast<f4*>(static_cast<float*>(R.out) + at) = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        else *reinterpret_cast<Pack<T, 4>*>(static_cast<T*>(R.out) + at) = Pack<T, 4>{};
+      }
+      if (!PACKED)
+        for (int i = 0; i < 4; ++i) {
+          if (column + i >= width) continue;
+          if (wide) static_cast<float*>(R.out)[at + i] = 0.0f;
+          else static_cast<T*>(R.out)[at + i] = (T)0.0f;
+        }
     }
   }
   if constexpr (STATE_ONLY) {
