@@ -193,19 +193,38 @@ struct Plan {
 
 size_t rounded(size_t b) { return (b + 255) & ~(size_t)255; }
 
-constexpr int64_t WAVES_WANTED = 2048;  // two to a SIMD
+// How long the passes take that cut the time axis into segments of `length` tokens, in chunks of one wave that a SIMD works through
+// (about 2 us).  Waves of a SIMD share it, and one alone leaves it waiting a third of the time; a wave's states, brought in and
+// written, cost it as much as a chunk and a half.
+double cost_of(const cnn_linear_shape& s, int roles, int64_t length) {
+  constexpr int64_t CUS = 256;
+  const int64_t segments = (s.T + length - 1) / length, units = (int64_t)s.B * s.H;
+  const auto pass = [&](int dk, int dv, int same) {
+    const int waves = block_columns(dk, dv) / (16 * NW);  // of a workgroup
+    const int64_t to_cu = (units * segments * blocks_of(dk, dv) * same + CUS - 1) / CUS, to_simd = (to_cu * waves + 3) / 4;
+    return (to_simd > 1 ? (double)to_simd : 1.5) * ((double)(length / C) + 1.5);
+  };
+  const auto alike = [&] { return padded(s.Dk) == padded(s.Dv) && block_columns(s.Dk, s.Dv) == block_columns(s.Dv, s.Dk); };
+  const double all = roles == 1 ? pass(s.Dk, s.Dv, 1) : alike() ? pass(s.Dk, s.Dv, 3) : pass(s.Dv, s.Dk, 2) + pass(s.Dk, s.Dv, 1);
+  if (segments == 1) return all;
+  const double states = roles == 1 ? pass(s.Dk, s.Dv, 1) : alike() ? pass(s.Dk, s.Dv, 2) : pass(s.Dv, s.Dk, 1) + pass(s.Dk, s.Dv, 1);
+  const double moved = 8.0 * (double)(units * segments * (roles == 1 ? 1 : 2)) * (double)carry_floats(s.Dk, s.Dv);  // by the kernel between them
+  return all + 0.45 * states + 2.5 + moved * 1.0e-7;  // (10 MB take as long as a chunk)
+}
 
 Plan plan_of(const cnn_linear_shape& s, int roles) {
   Plan p{};
   const int64_t units = (int64_t)s.B * s.H;
-  const auto waves = [](int dk, int dv) { return (int64_t)blocks_of(dk, dv) * block_columns(dk, dv) / (16 * NW); };
-  const int64_t at_once = units * (roles == 1 ? waves(s.Dk, s.Dv) : waves(s.Dk, s.Dv) + 2 * waves(s.Dv, s.Dk));
-  // Segments until the waves fill the GPU, but none whose state, written and read twice, is more to move than its tokens.
+  // No segments whose state, written and read twice, is more to move than its tokens.
   const int64_t least = 16 * (int64_t)s.Dk * s.Dv / (2 * (s.Dk + s.Dv) * (int64_t)type_bytes(s.type));
-  int64_t n = (WAVES_WANTED + at_once - 1) / at_once, most = s.T / (least > 2 * C ? least : 2 * C);
-  n = n < most ? n : most;
-  n = n < 1 ? 1 : n;
-  p.length = ((s.T + n - 1) / n + C - 1) / C * C;
+  const int64_t most = s.T / (least > 2 * C ? least : 2 * C);
+  p.length = ((int64_t)s.T + C - 1) / C * C;
+  double best = cost_of(s, roles, p.length);
+  for (int64_t n = 2; n <= most && n <= 256; ++n) {
+    const int64_t length = ((s.T + n - 1) / n + C - 1) / C * C;
+    const double cost = cost_of(s, roles, length);
+    if (cost < best) best = cost, p.length = length;
+  }
   p.segments = (int)((s.T + p.length - 1) / p.length);
   const int64_t floats = carry_floats(s.Dk, s.Dv) > carry_floats(s.Dv, s.Dk) || roles == 1 ? carry_floats(s.Dk, s.Dv) : carry_floats(s.Dv, s.Dk);
   p.state_bytes = p.segments > 1 ? rounded((size_t)units * p.segments * floats * 4) : 0;
