@@ -325,7 +325,7 @@ int cnn_linear_attention_bwd(const cnn_linear_shape* s, const cnn_heads* q, cons
     r.DK = i < 2 ? s->Dv : s->Dk, r.DV = i < 2 ? s->Dk : s->Dv;
     r.first = i == 0 ? initial_state : d_final_state;
     r.first_i = i < 2 ? 1 : s->Dv, r.first_j = i < 2 ? s->Dv : 1;  // the first two hold the state transposed
-    if (i > 0) r.first_by = 1.0f / scale, r.last_by = scale;
+    if (i > 0 && (d_final_state || d_initial_state)) r.first_by = 1.0f / scale, r.last_by = scale;  // (else any scale, zero too)
   }
   a.role[0].q = D, a.role[0].k = V, a.role[0].v = K, a.role[0].out = d_q;
   a.role[1].q = V, a.role[1].k = D, a.role[1].v = Q, a.role[1].out = shared ? ws + p.wide_k : d_k;

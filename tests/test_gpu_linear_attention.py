@@ -222,6 +222,15 @@ def test_other_stream_and_graph():
         assert all(torch.equal(x, y) for x, y in zip(want, got)) and torch.equal(state, eager), i
 
 
+@pytest.mark.parametrize("T", [40, 900])
+def test_a_scale_of_zero_gives_gradients_of_zero(T):
+    """Without states' errors any scale is allowed; 900 tokens are cut into segments."""
+    q, k, v, decay, d_o, _, _, _ = make((1, T, 2, 1, 32, 48, None, False, True), "fp32")
+    for scale in (0.0, 2.0 ** -140):
+        for g in binding.linear_attention_bwd(q, k, v, decay, d_o, scale)[:3]:
+            assert torch.isfinite(g).all() and (g.abs() <= 2.0 ** -100).all()
+
+
 def test_refusals():
     q, k, v = (torch.zeros(2, 3, 4, 8, device=DEV) for _ in range(3))
     decay, fwd = torch.ones(4, device=DEV), binding.linear_attention_fwd
