@@ -70,7 +70,7 @@ __global__ __launch_bounds__(DROP_THREADS) void dropout_kernel(DropArgs a) {
   const T *x = static_cast<const T*>(a.x), *res = static_cast<const T*>(a.residual);
   T* y = static_cast<T*>(a.y);
   const uint64_t offset = a.offset + (a.step ? (uint64_t)*a.step : 0);
-  const size_t first = (size_t)blockIdx.x * (DROP_THREADS * DROP_BLOCKS) + threadIdx.x;
+  const size_t first = (size_t)workgroup() * (DROP_THREADS * DROP_BLOCKS) + threadIdx.x;
   Pack<T, 8> in[DROP_BLOCKS], add[DROP_BLOCKS];
 #pragma unroll
   for (int i = 0; i < DROP_BLOCKS; ++i) {
@@ -112,9 +112,9 @@ int dropout(const void* x, const void* residual, void* y, size_t n, int type, do
   const size_t groups = (n + DROP_THREADS * DROP_BLOCKS * 8 - 1) / (DROP_THREADS * DROP_BLOCKS * 8);
   return with_type(type, [&](auto t) {
     if (residual)
-      dropout_kernel<decltype(t), true><<<(unsigned)groups, DROP_THREADS, 0, (hipStream_t)hip_stream>>>(a);
+      dropout_kernel<decltype(t), true><<<grid_of((int64_t)groups), DROP_THREADS, 0, (hipStream_t)hip_stream>>>(a);
     else
-      dropout_kernel<decltype(t), false><<<(unsigned)groups, DROP_THREADS, 0, (hipStream_t)hip_stream>>>(a);
+      dropout_kernel<decltype(t), false><<<grid_of((int64_t)groups), DROP_THREADS, 0, (hipStream_t)hip_stream>>>(a);
     return launch_status();
   });
 }

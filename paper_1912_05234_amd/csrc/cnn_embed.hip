@@ -40,7 +40,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_fwd_kernel(EmbedArgs a) {
   const P* table = static_cast<const P*>(a.table);
   P* out = static_cast<P*>(a.out);
   const int lanes = 1 << a.lanes_log, groups = EMBED_THREADS >> a.lanes_log;
-  const int64_t row0 = (int64_t)blockIdx.x * (groups * ROWS) + (threadIdx.x >> a.lanes_log);
+  const int64_t row0 = workgroup() * (groups * ROWS) + (threadIdx.x >> a.lanes_log);
   int64_t token[ROWS];
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
@@ -593,7 +593,7 @@ template <class T, int VN>
 int lookup(const EmbedArgs& a, bool wide, hipStream_t st) {
   constexpr int ROWS = 4;
   const int64_t per = (int64_t)(EMBED_THREADS >> a.lanes_log) * ROWS;
-  const unsigned grid = (unsigned)((a.N + per - 1) / per);
+  const dim3 grid = grid_of((a.N + per - 1) / per);
   if (wide) embed_fwd_kernel<T, VN, int64_t, ROWS><<<grid, EMBED_THREADS, 0, st>>>(a);
   else embed_fwd_kernel<T, VN, int32_t, ROWS><<<grid, EMBED_THREADS, 0, st>>>(a);
   return launch_status();

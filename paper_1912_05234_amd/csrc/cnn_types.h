@@ -25,6 +25,13 @@ auto with_type(int type, FN fn) {
   return fn(_Float16{});
 }
 
+// Workgroups 0 .. n - 1, and perhaps some more, as a grid of two dimensions: one of them holds less than 2^32 threads.
+inline dim3 grid_of(int64_t n) {
+  const int64_t x = n < 1 << 22 ? n : 1 << 22;
+  return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
+}
+__device__ __forceinline__ int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 inline int launch_status() {
   if (hipGetLastError() != hipSuccess) return CNN_EHIP;
   return CNN_OK;

@@ -46,6 +46,18 @@ def test_lookup(N, V, D, spread, type_):
         ref.near(out, want, 2.0 ** -24 * np.abs(want), dtype, "lookup %s" % type_)  # the product is rounded to fp32 first
 
 
+def test_lookup_of_more_rows_than_one_dimension_of_a_grid_holds():
+    """Four rows to a workgroup of 256 threads: past 2^26 rows there are 2^32 threads."""
+    N, V, D = (1 << 26) + 5, 7, 129
+    table = torch.randn(V, D, generator=torch.Generator().manual_seed(0)).to(DEV, torch.bfloat16)
+    tokens = (torch.arange(N, dtype=torch.int32, device=DEV) % 11) - 2
+    out = binding.embedding_fwd(table, tokens, 2.0)
+    padded = torch.cat([table * 2, torch.zeros(1, D, device=DEV, dtype=table.dtype)])
+    for first in range(0, N, 1 << 24):  # (a product with a power of two is exact)
+        t = tokens[first:first + (1 << 24)].long()
+        assert torch.equal(out[first:first + (1 << 24)], padded[torch.where((t < 0) | (t >= V), V, t)]), first
+
+
 @pytest.mark.parametrize("type_", list(ref.TYPES))
 @pytest.mark.parametrize("N,V,D,spread", CASES)
 def test_gradient(N, V, D, spread, type_):
