@@ -136,11 +136,14 @@ struct Shape {
   static constexpr int DVC = WAVES * 16 * NW, THREADS = 64 * WAVES;
   static constexpr int NP = PIECES<T>, MP = at_least_two(NP);  // pieces of the inputs, and of state and scores
   // rows of q and k are read sixteen bytes to a lane, of v and k also four rows to a lane: the padding spreads them over the banks
-  static constexpr int QS = DKP + 8, VS = DVC + (WAVES == 1 ? 8 : 16);
+  static constexpr int QS = DKP + 8, VS = DVC + 16;
   // A single wave of narrow rows takes q from memory in the order of its operands: without it in LDS eight waves of floats fit a
   // compute unit, not six.
   static constexpr bool Q_DIRECT = WAVES == 1 && DKP == 32;
-  static constexpr int K = 0, V = K + NP * C * QS, Q = V + NP * C * VS, ALL = Q + (Q_DIRECT ? 0 : NP * C * QS);  // offsets of the tiles in LDS
+  // Columns of v belong to one wave each.  Floats come from memory in the order of its operands; elements of 16 bits pass through LDS,
+  // whose reads turn the tile, and are cut after that: the uncut number is wanted too.
+  static constexpr bool V_DIRECT = sizeof(T) == 4;
+  static constexpr int K = 0, V = K + NP * C * QS, Q = V + (V_DIRECT ? 0 : C * VS), ALL = Q + (Q_DIRECT ? 0 : NP * C * QS);  // offsets of the tiles in LDS
   // two sets of tiles, and one barrier a chunk, where eight waves of a compute unit have room for them
   static constexpr int SETS = 2 * ALL * 2 <= 20 * 1024 * WAVES ? 2 : 1;
 };
@@ -197,10 +200,10 @@ struct Stage {
         if ((int)threadIdx.x / COLUMNS + e * STEP < pad) u[e].v[j] = (T)0.0f;
   }
 
-  // planes of [ROWS][STRIDE], one to a piece; `all`: columns past the width too
-  template <int STRIDE>
+  // planes of [ROWS][STRIDE], one to a piece, or one of uncut elements of 16 bits; `all`: columns past the width too
+  template <int STRIDE, bool UNCUT = false>
   __device__ __forceinline__ void store(__bf16* tile, bool all) const {
-    constexpr int NP = PIECES<T>;
+    constexpr int NP = UNCUT ? 1 : PIECES<T>;
     if (!all && column() >= width) return;
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
@@ -282,6 +285,40 @@ struct Direct {
   }
 };
 
+// Columns of v of one wave as operands: eight tokens, 16 (j / 4) + 4 (lane / 16) + j % 4, of column lane % 16 of each of its tiles.
+template <class T>
+struct Columns {
+  T u[NW][8];
+  uint32_t at[NW];  // bytes from the row that its place in the wave does not change
+
+  __device__ __forceinline__ int column(int w) const { return (threadIdx.x >> 6) * 16 * NW + 16 * w + (threadIdx.x & 15); }
+  __device__ __forceinline__ static int group() { return threadIdx.x >> 4 & 3; }
+  __device__ __forceinline__ void set(int width, int64_t token_stride, bool reversed) {
+    const uint32_t row = __umul24(reversed ? 12 - 4 * group() : 4 * group(), (uint32_t)token_stride * (uint32_t)sizeof(T));
+#pragma unroll
+    for (int w = 0; w < NW; ++w) at[w] = row + (column(w) < width ? column(w) : 0) * (uint32_t)sizeof(T);
+  }
+  __device__ __forceinline__ void load(const T* low, int64_t token_stride, bool reversed) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int place = 16 * (j >> 2) + (j & 3);
+      const char* row = reinterpret_cast<const char*>(low + (reversed ? 19 - place : place) * token_stride);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) u[w][j] = *reinterpret_cast<const T*>(row + at[w]);
+    }
+  }
+  __device__ __forceinline__ void load_any(const T* low, int64_t token_stride, int width, int pad, bool reversed) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      int row = 16 * (j >> 2) + 4 * group() + (j & 3);
+      row = row > pad ? row : pad;
+      const T* from = low + (reversed ? C - 1 - row : row) * token_stride;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) u[w][j] = column(w) < width ? from[column(w)] : (T)0.0f;
+    }
+  }
+};
+
 // log2 of a decay, finite also for a = 0 (a^0 = 1 and a^n = 0 then come out right), to fp32 also next to 1.
 __device__ __forceinline__ float log2_decay(float a) {
   const double l = log2((double)a);
@@ -306,7 +343,8 @@ __device__ __forceinline__ uint32_t state_index(int row, int column, int tiles) 
   return (uint32_t)((((column >> 4) * tiles + m) * 64 + lane) * 4 + (row & 3));
 }
 
-constexpr int waves_wanted(int DKP) { return DKP <= 128 ? 2 : 1; }  // to a SIMD
+// Waves to a SIMD, which bound the registers of a kernel.  (Three would spill: the pixel sequences' gradients took 105 us, not 71.)
+constexpr int waves_wanted(int DKP) { return DKP <= 128 ? 2 : 1; }
 
 // STATE_ONLY: the first pass.  EXACT: the state is a result, not only what the segment's own tokens see.
 template <class T, int DKP, int WAVES, bool PACKED, bool STATE_ONLY, bool EXACT>
@@ -331,35 +369,51 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
   int pad = (int)((C - (end - begin) % C) % C);
   std::conditional_t<S::Q_DIRECT, Direct<T, 32>, Stage<T, C, DKP, THREADS>> q_in;
   Stage<T, C, DKP, THREADS> k_in;
-  Stage<T, C, S::DVC, THREADS> v_in;
+  std::conditional_t<S::V_DIRECT, Columns<T>, Stage<T, C, S::DVC, THREADS>> v_in;
   bf8 direct[2][NP];  // q's operands of the present chunk, where they do not pass through LDS
   const int64_t low = reversed ? n - (begin - pad) - C : begin - pad, advance = reversed ? -C : C;  // in tokens
-  const auto base = [&](const Operand& o) { return static_cast<const T*>(o.data) + batch * o.batch + head / o.share * o.head + low * o.token; };
+  const auto base = [&](const Operand& o) __attribute__((always_inline)) { return static_cast<const T*>(o.data) + batch * o.batch + head / o.share * o.head + low * o.token; };
   const T *q = base(R.q), *k = base(R.k), *v = base(R.v) + dv0;
   const int64_t q_step = advance * R.q.token, k_step = advance * R.k.token, v_step = advance * R.v.token;
-  const auto load = [&](int pad) {
+  const auto load_v = [&](int pad, bool first) __attribute__((always_inline)) {
+    if constexpr (S::V_DIRECT) {
+      if (PACKED && !first) v_in.load(v, R.v.token, reversed);
+      else v_in.load_any(v, R.v.token, width, pad, reversed);
+    } else {
+      if (PACKED) v_in.load(v);
+      else v_in.load_any(v, R.v.token, width, pad, reversed);
+    }
+    v += v_step;
+  };
+  const auto load = [&](int pad) __attribute__((always_inline)) {
     if constexpr (PACKED) {
-      k_in.load(k), v_in.load(v);
+      k_in.load(k);
       if (!STATE_ONLY) q_in.load(q);
     } else {
-      k_in.load_any(k, R.k.token, DK, pad, reversed), v_in.load_any(v, R.v.token, width, pad, reversed);
+      k_in.load_any(k, R.k.token, DK, pad, reversed);
       if (!STATE_ONLY) q_in.load_any(q, R.q.token, DK, pad, reversed);
     }
-    q += q_step, k += k_step, v += v_step;
+    q += q_step, k += k_step;
+    if constexpr (!S::V_DIRECT) load_v(pad, false);
   };
-  const auto store = [&](__bf16* tile) {
+  const auto store = [&](__bf16* tile) __attribute__((always_inline)) {
     k_in.template store<S::QS>(tile + S::K, !PACKED);
-    v_in.template store<S::VS>(tile + S::V, true);
+    if constexpr (!S::V_DIRECT) v_in.template store<S::VS, true>(tile + S::V, true);
     if constexpr (STATE_ONLY) return;
     else if constexpr (S::Q_DIRECT) q_in.pieces(direct);
     else q_in.template store<S::QS>(tile + S::Q, true);
   };
-  const auto set = [&](int pad) {
-    k_in.set(DK, R.k.token, pad, reversed), v_in.set(width, R.v.token, pad, reversed);
+  const auto set = [&](int pad) __attribute__((always_inline)) {
+    k_in.set(DK, R.k.token, pad, reversed);
+    if constexpr (!S::V_DIRECT) v_in.set(width, R.v.token, pad, reversed);
     if (!STATE_ONLY) q_in.set(DK, R.q.token, pad, reversed);
   };
   set(pad);
-  if (begin < end) load(pad);
+  if constexpr (S::V_DIRECT) v_in.set(width, R.v.token, reversed);
+  if (begin < end) {
+    load(pad);
+    if constexpr (S::V_DIRECT) load_v(pad, true);
+  }
   if (pad) set(0);
   if (PACKED && DK < DKP)
     for (int i = 0; i < S::SETS; ++i) k_in.template blank<S::QS>(tiles + i * SET + S::K);
@@ -495,25 +549,29 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       bf8 raw[NP];
-#pragma unroll
-      for (int z = 0; z < NP; ++z) {
-        const __bf16* p = tile + S::V + (z * C + 4 * g + (r >> 2)) * S::VS + 16 * (NW * wave + w) + 4 * (r & 3);
-        raw[z] = joined(read_transposed(p), read_transposed(p + 16 * S::VS));
-      }
       float x[8];
+      if constexpr (S::V_DIRECT) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        x[j] = 0.0f;
+        for (int j = 0; j < 8; ++j) x[j] = (float)v_in.u[w][j];
+        cut<NP>(x, raw);
+      } else {
+        const __bf16* p = tile + S::V + (4 * g + (r >> 2)) * S::VS + 16 * (NW * wave + w) + 4 * (r & 3);
+        raw[0] = joined(read_transposed(p), read_transposed(p + 16 * S::VS));
+        const auto uncut = __builtin_bit_cast(Pack<T, 8>, raw[0]);
 #pragma unroll
-        for (int z = NP - 1; z >= 0; --z) x[j] += (float)raw[z][j];
-        x[j] *= STATE_ONLY ? follow[j] * by : follow[j];
+        for (int j = 0; j < 8; ++j) x[j] = (float)uncut.v[j];
+        if constexpr (NP > 1) cut<NP>(x, raw);
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= STATE_ONLY ? follow[j] * by : follow[j];
       cut<WP>(x, weighted[w]);
       if constexpr (!STATE_ONLY) {
         acc[0][w] = product(raw, score[0], acc[0][w]);
         acc[1][w] = product(raw, score[1], acc[1][w]);
       }
     }
+    if constexpr (S::V_DIRECT)
+      if (more) load_v(0, false);
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       bf8 a[NP];
