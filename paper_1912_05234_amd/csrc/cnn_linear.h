@@ -426,18 +426,24 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
   for (int m = 0; m < M; ++m)
 #pragma unroll
     for (int w = 0; w < NW; ++w) state[m][w] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+  // Rows 32 m + 8 g + j, j < 8, of a column are registers j % 4 of its tiles 2 m + j / 4.
+  const int rows = DK - 8 * g;  // of the state from 8 g on
   if (!STATE_ONLY && !whole && R.flipped) {
-    const float* from = R.flipped + (unit * args.segments + segment) * carry_floats(DV, DK);
+    // their columns are rows here: an element's place in their registers, taken apart into what depends on the lane and what does not
     const int tiles = padded(DV) / 16;
+    const float* from = R.flipped + (unit * args.segments + segment) * carry_floats(DV, DK);
 #pragma unroll
-    for (int m = 0; m < M; ++m) {
+    for (int w = 0; w < NW; ++w) {
+      const int column = dv0 + state_column(NW * wave + w, lane);
+      if (column >= padded(DV)) continue;
+      const float* p = from + state_index(column, 8 * g, tiles);
 #pragma unroll
-      for (int w = 0; w < NW; ++w)
+      for (int m = 0; m < M / 2; ++m) {
+        if (PACKED && 32 * m >= rows) continue;  // (their columns past the width hold something)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int row = state_row(m, lane, i), column = dv0 + state_column(NW * wave + w, lane);
-          if (row < DK && column < DV) state[m][w][i] = from[state_index(column, row, tiles)];
-        }
+        for (int j = 0; j < 8; ++j)
+          if (PACKED || 32 * m + j < rows) state[2 * m + (j >> 2)][w][j & 3] = p[4 * j + m * 512 * tiles];
+      }
     }
   } else if (!STATE_ONLY && !whole) {
 #pragma unroll
@@ -448,13 +454,21 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
     const float* from = R.first + unit * DK * DV;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const int column = state_column(NW * wave + w, lane), at_column = (dv0 + column) * R.first_j;
+      const int column = state_column(NW * wave + w, lane);
+      if (column >= width) continue;
+      const float* p = from + 8 * g * R.first_i + (dv0 + column) * R.first_j;
 #pragma unroll
-      for (int m = 0; m < M; ++m)
+      for (int m = 0; m < M / 2; ++m) {
+        if (PACKED && 32 * m >= rows) continue;  // whole packs of rows
+        if (PACKED && R.first_i == 1) {
+          state[2 * m][w] = *reinterpret_cast<const f4*>(p + 32 * m);
+          state[2 * m + 1][w] = *reinterpret_cast<const f4*>(p + 32 * m + 4);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (state_row(m, lane, i) < DK && column < width) state[m][w][i] = from[(uint32_t)(state_row(m, lane, i) * R.first_i + at_column)];
-      in_steps();
+          for (int j = 0; j < 8; ++j)
+            if (PACKED || 32 * m + j < rows) state[2 * m + (j >> 2)][w][j & 3] = p[(32 * m + j) * R.first_i];
+        }
+      }
     }
 #pragma unroll
     for (int m = 0; m < M; ++m)
@@ -641,24 +655,31 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
 #pragma unroll
       for (int w = 0; w < NW; ++w) carry[(w * M + m) * 64] = state[m][w];
   } else if (whole && R.last) {
+    float* to = R.last + unit * DK * DV + dv0;
+    if (n == 0) {  // as it was given
+      const float* from = R.first ? R.first + unit * DK * DV : nullptr;
+      for (int i = threadIdx.x; i < DK * width; i += THREADS) {
+        const int row = i / width, column = i % width;
+        to[row * DV + column] = from ? from[row * R.first_i + (dv0 + column) * R.first_j] : 0.0f;
+      }
+      return;
+    }
     // a reversed sequence's state stands at its first token; one decay more and the scale make it the error of the state before it
     const float by = R.last_by * (reversed ? args.decay[head] : 1.0f);
-    float* to = R.last + unit * DK * DV;
-    const float* from = R.first ? R.first + unit * DK * DV : nullptr;
-    const int rows = anew(DK), stride = anew(DV);
+    const int left = anew(DK) - 8 * g, stride = anew(DV);
 #pragma unroll
-    for (int m = 0; m < M; ++m) {
+    for (int w = 0; w < NW; ++w) {
+      const int column = state_column(NW * wave + w, lane);
+      if (column >= width) continue;
+      float* p = to + 8 * g * stride + column;
 #pragma unroll
-      for (int w = 0; w < NW; ++w)
+      for (int m = 0; m < M / 2; ++m) {
+        if (PACKED && 32 * m >= left) continue;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int row = state_row(m, lane, i), column = dv0 + state_column(NW * wave + w, lane);
-          if (row >= rows || column >= stride) continue;
-          float x = state[m][w][i] * by;
-          if (n == 0) x = from ? from[(uint32_t)(row * R.first_i + column * R.first_j)] : 0.0f;  // as it was given
-          to[(uint32_t)(row * stride + column)] = x;
-        }
-      in_steps();
+        for (int j = 0; j < 8; ++j)
+          if (PACKED || 32 * m + j < left) p[(32 * m + j) * stride] = state[2 * m + (j >> 2)][w][j & 3] * by;
+        in_steps();
+      }
     }
   }
 }
