@@ -155,7 +155,8 @@ struct Shape {
 template <class T, int ROWS, int WIDTH, int THREADS>
 struct Stage {
   static constexpr int COLUMNS = WIDTH / 8, STEP = THREADS / COLUMNS, EACH = (ROWS + STEP - 1) / STEP;
-  static_assert(THREADS % COLUMNS == 0, "threads to a row");
+  // Threads past STEP whole rows bring in the next row's units a second time; rows past the last are left out.
+  static constexpr bool PAST = ROWS % STEP != 0 || THREADS % COLUMNS != 0;
   Pack<T, 8> u[EACH];
   uint32_t at[EACH];  // PACKED: bytes from the chunk's lowest address, which is row 0's, or in reversed order the last row's
   int width, stride;  // in elements
@@ -163,7 +164,7 @@ struct Stage {
   __device__ __forceinline__ int column() const { return threadIdx.x % COLUMNS * 8; }
   __device__ __forceinline__ int row(int e) const {
     const int r = threadIdx.x / COLUMNS + e * STEP;
-    return ROWS % STEP && r >= ROWS ? ROWS - 1 : r;
+    return PAST && r >= ROWS ? ROWS - 1 : r;
   }
   __device__ __forceinline__ int place(int row, int pad, bool reversed) const {
     row = row > pad ? row : pad;
@@ -208,7 +209,7 @@ struct Stage {
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
       const int r = threadIdx.x / COLUMNS + e * STEP;
-      if (ROWS % STEP && r >= ROWS) continue;
+      if (PAST && r >= ROWS) continue;
       bf8 piece[NP];
       if constexpr (NP == 1) {
         piece[0] = __builtin_bit_cast(bf8, u[e]);
@@ -230,9 +231,14 @@ struct Stage {
   }
 };
 
-__host__ __device__ constexpr int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-// Columns of a workgroup, 32 to a wave.  (One wave brings in the rows of at most 64 columns of q and k by itself.)
-__host__ __device__ constexpr int block_columns(int DK, int DV) { return DV <= 32 && DK <= 64 ? 32 : DV <= 64 && DK <= 128 ? 64 : 128; }
+__host__ __device__ constexpr int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
+// Columns of a workgroup, 32 to a wave, as few as the number of workgroups allows.  (One wave brings in the rows of at most 64
+// columns of q and k by itself, two of 128.)
+__host__ __device__ constexpr int block_columns(int DK, int DV) {
+  if (DV <= 32 && DK <= 64) return 32;
+  if (DV <= 64 && DK <= 128) return 64;
+  return DK <= 128 && (DV + 95) / 96 == (DV + 127) / 128 ? 96 : 128;
+}
 __host__ __device__ constexpr int blocks_of(int DK, int DV) { return (DV + block_columns(DK, DV) - 1) / block_columns(DK, DV); }
 // Floats of a state as the kernel holds it.
 __host__ __device__ constexpr int64_t carry_floats(int DK, int DV) { return (int64_t)padded(DK) * blocks_of(DK, DV) * block_columns(DK, DV); }
@@ -712,6 +718,8 @@ int launch_scan(const Args& a, int roles, int columns, bool state_only, hipStrea
     if (columns == 32) return launch_scan<T, DKP, 1>(a, roles, state_only, st);
   if constexpr (DKP <= 128)
     if (columns == 64) return launch_scan<T, DKP, 2>(a, roles, state_only, st);
+  if constexpr (DKP <= 128)
+    if (columns == 96) return launch_scan<T, DKP, 3>(a, roles, state_only, st);
   return launch_scan<T, DKP, 4>(a, roles, state_only, st);
 }
 
@@ -729,6 +737,7 @@ int run_scan(const Args& all, int roles, bool state_only, hipStream_t st) {
     }
     const int rc = dk == 32    ? launch_scan<T, 32>(a, same, columns, state_only, st)
                    : dk == 64  ? launch_scan<T, 64>(a, same, columns, state_only, st)
+                   : dk == 96  ? launch_scan<T, 96>(a, same, columns, state_only, st)
                    : dk == 128 ? launch_scan<T, 128>(a, same, columns, state_only, st)
                                : launch_scan<T, 256>(a, same, columns, state_only, st);
     if (rc != CNN_OK) return rc;

@@ -87,6 +87,19 @@ def test_backward(case, type_):
     assert again[3] is None and all(torch.equal(x, y) for x, y in zip(again[:3], got[:3]))
 
 
+# widths of three tiles of 32, and blocks of 96 columns
+THREES = [(2, 45, 2, 1, 96, 96, [45, 3], True, True), (1, 333, 2, 2, 80, 96, None, True, True), (1, 100, 3, 1, 77, 90, [99], True, False),
+          (1, 700, 1, 1, 96, 160, None, True, False), (2, 640, 2, 1, 64, 88, [600, 33], False, True), (1, 70, 1, 1, 200, 96, None, True, True),
+          (1, 65, 1, 1, 24, 72, None, False, False), (1, 390, 1, 1, 128, 192, [388], True, True)]
+
+
+@pytest.mark.parametrize("type_", list(ref.TYPES))
+@pytest.mark.parametrize("case", THREES, ids=[str(c[:6]) for c in THREES])
+def test_widths_of_three_tiles(case, type_):
+    test_forward(case, type_)
+    test_backward(case, type_)
+
+
 def test_backward_against_differences_of_the_forward_call():
     """The loss sum(o w) + sum(state u) in fp32, perturbed along random directions: the slope is the gradient's product with them."""
     case = (2, 90, 2, 1, 20, 24, [90, 51], True, False)
