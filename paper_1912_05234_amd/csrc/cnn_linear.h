@@ -53,7 +53,9 @@ struct Role {
   float* carry;        // [unit][segment], states in the order of the kernel's registers
   const float* flipped;  // instead: those of a role whose states are this one's transposed
   int first_i, first_j;
-  int DK, DV, blocks;  // blocks of columns
+  int DK, DV, DKP, columns, blocks;  // DK padded, columns of a workgroup, workgroups to a state
+  int flipped_rows;                  // DKP of that role
+  int64_t flipped_floats;            // of one of its states
   float scale, first_by, last_by;
   int reversed;  // the last token of a sequence comes first; the first state then already stands at the first token
   int wide, packed;  // packed: rows are made of whole packs of eight elements at addresses that are multiples of 16 bytes
@@ -239,9 +241,8 @@ __host__ __device__ constexpr int block_columns(int DK, int DV) {
   if (DV <= 64 && DK <= 128) return 64;
   return DK <= 128 && (DV + 95) / 96 == (DV + 127) / 128 ? 96 : 128;
 }
-__host__ __device__ constexpr int blocks_of(int DK, int DV) { return (DV + block_columns(DK, DV) - 1) / block_columns(DK, DV); }
 // Floats of a state as the kernel holds it.
-__host__ __device__ constexpr int64_t carry_floats(int DK, int DV) { return (int64_t)padded(DK) * blocks_of(DK, DV) * block_columns(DK, DV); }
+__host__ __device__ inline int64_t carry_floats(const Role& r) { return (int64_t)r.DKP * r.blocks * r.columns; }
 
 // Rows of q of a single wave, as operands of its products: row 16 t + lane % 16, columns 32 s + 8 (lane / 16) .. + 7.
 template <class T, int DKP>
@@ -436,12 +437,12 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
   const int rows = DK - 8 * g;  // of the state from 8 g on
   if (!STATE_ONLY && !whole && R.flipped) {
     // their columns are rows here: an element's place in their registers, taken apart into what depends on the lane and what does not
-    const int tiles = padded(DV) / 16;
-    const float* from = R.flipped + (unit * args.segments + segment) * carry_floats(DV, DK);
+    const int tiles = R.flipped_rows / 16;
+    const float* from = R.flipped + (unit * args.segments + segment) * R.flipped_floats;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       const int column = dv0 + state_column(NW * wave + w, lane);
-      if (column >= padded(DV)) continue;
+      if (column >= R.flipped_rows) continue;
       const float* p = from + state_index(column, 8 * g, tiles);
 #pragma unroll
       for (int m = 0; m < M / 2; ++m) {
@@ -728,13 +729,9 @@ template <class T>
 int run_scan(const Args& all, int roles, bool state_only, hipStream_t st) {
   for (int r = 0; r < roles;) {
     Args a = all;
-    const int dk = padded(all.role[r].DK), columns = block_columns(all.role[r].DK, all.role[r].DV);
+    const int dk = all.role[r].DKP, columns = all.role[r].columns;
     int same = 0;
-    for (; r + same < roles; ++same) {
-      const Role& o = all.role[r + same];
-      if (padded(o.DK) != dk || block_columns(o.DK, o.DV) != columns) break;
-      a.role[same] = o;
-    }
+    for (; r + same < roles && all.role[r + same].DKP == dk && all.role[r + same].columns == columns; ++same) a.role[same] = all.role[r + same];
     const int rc = dk == 32    ? launch_scan<T, 32>(a, same, columns, state_only, st)
                    : dk == 64  ? launch_scan<T, 64>(a, same, columns, state_only, st)
                    : dk == 96  ? launch_scan<T, 96>(a, same, columns, state_only, st)

@@ -10,13 +10,13 @@ namespace {
 constexpr int CARRY_THREADS = 256;
 __global__ __launch_bounds__(CARRY_THREADS) void carry_kernel(Args args) {
   const Role& R = args.role[blockIdx.y];
-  const int64_t size = carry_floats(R.DK, R.DV) / 4, groups = (size + CARRY_THREADS - 1) / CARRY_THREADS;
+  const int64_t size = carry_floats(R) / 4, groups = (size + CARRY_THREADS - 1) / CARRY_THREADS;
   const int64_t unit = blockIdx.x / groups, at = blockIdx.x % groups * CARRY_THREADS + threadIdx.x;
   if (unit >= args.units || at >= size) return;
   const int64_t n = length_of(args, unit / args.heads);
   const float a = args.decay[unit % args.heads];
   // [tile of columns][tile of rows][lane]
-  const int tiles = padded(R.DK) / 16, lane = (int)(at & 63), row = state_row((int)((at >> 6) % tiles), lane, 0);
+  const int tiles = R.DKP / 16, lane = (int)(at & 63), row = state_row((int)((at >> 6) % tiles), lane, 0);
   const int column = state_column((int)((at >> 6) / tiles), lane);
   f4 raw{0.0f, 0.0f, 0.0f, 0.0f};
   if (R.first && column < R.DV)
@@ -184,31 +184,36 @@ bool near_ok(const cnn_linear_shape* s) { return (int64_t)s->H * (s->Dk > s->Dv 
 
 Operand operand_of(const cnn_heads* h, int share) { return {h->data, h->batch, h->token, h->head, share}; }
 
+struct Form {  // of a role's kernel
+  int DKP, columns, blocks;
+  int64_t floats() const { return (int64_t)DKP * columns * blocks; }
+};
+
 struct Plan {
   int segments;
   int64_t length;
+  Form form[2];        // of the role d_v, and of forward; of the other two roles
   size_t state_bytes;  // of one role's states, all segments
   size_t wide_k, wide_v, bytes;
 };
 
 size_t rounded(size_t b) { return (b + 255) & ~(size_t)255; }
 
-// How long the passes take that cut the time axis into segments of `length` tokens, in chunks of one wave that a SIMD works through
-// (about 2 us).  Waves of a SIMD share it, and one alone leaves it waiting a third of the time; a wave's states, brought in and
-// written, cost it as much as a chunk and a half.
-double cost_of(const cnn_linear_shape& s, int roles, int64_t length) {
+// How long the passes take that cut the time axis into segments of `length` tokens, in chunks of one wave of 128 x 32 that a SIMD
+// works through (about 2 us).  Waves of a SIMD share it, and one alone leaves it waiting a third of the time (those of 256 columns are
+// alone: their registers fill it); a wave's states, brought in and written, cost it as much as a chunk and a half.
+double cost_of(const cnn_linear_shape& s, const Plan& p, int roles, int64_t length) {
   constexpr int64_t CUS = 256;
   const int64_t segments = (s.T + length - 1) / length, units = (int64_t)s.B * s.H;
-  const auto pass = [&](int dk, int dv, int same) {
-    const int waves = block_columns(dk, dv) / (16 * NW);  // of a workgroup
-    const int64_t to_cu = (units * segments * blocks_of(dk, dv) * same + CUS - 1) / CUS, to_simd = (to_cu * waves + 3) / 4;
-    return (to_simd > 1 ? (double)to_simd : 1.5) * ((double)(length / C) + 1.5);
+  const auto pass = [&](const Form& f, int same) {
+    const int64_t to_cu = (units * segments * f.blocks * same + CUS - 1) / CUS, to_simd = (to_cu * (f.columns / (16 * NW)) + 3) / 4;
+    return (f.DKP > 128 ? 1.5 * (double)to_simd : to_simd > 1 ? (double)to_simd : 1.5) * ((double)(length / C) + 1.5) * (f.DKP + 64) / 192.0;
   };
-  const auto alike = [&] { return padded(s.Dk) == padded(s.Dv) && block_columns(s.Dk, s.Dv) == block_columns(s.Dv, s.Dk); };
-  const double all = roles == 1 ? pass(s.Dk, s.Dv, 1) : alike() ? pass(s.Dk, s.Dv, 3) : pass(s.Dv, s.Dk, 2) + pass(s.Dk, s.Dv, 1);
+  const bool joint = p.form[0].DKP == p.form[1].DKP && p.form[0].columns == p.form[1].columns;  // in one launch
+  const double all = roles == 1 ? pass(p.form[0], 1) : joint ? pass(p.form[0], 3) : pass(p.form[1], 2) + pass(p.form[0], 1);
   if (segments == 1) return all;
-  const double states = roles == 1 ? pass(s.Dk, s.Dv, 1) : alike() ? pass(s.Dk, s.Dv, 2) : pass(s.Dv, s.Dk, 1) + pass(s.Dk, s.Dv, 1);
-  const double moved = 8.0 * (double)(units * segments * (roles == 1 ? 1 : 2)) * (double)carry_floats(s.Dk, s.Dv);  // by the kernel between them
+  const double states = roles == 1 ? pass(p.form[0], 1) : joint ? pass(p.form[0], 2) : pass(p.form[1], 1) + pass(p.form[0], 1);
+  const double moved = 8.0 * (double)(units * segments) * (double)(p.form[0].floats() + (roles == 1 ? 0 : p.form[1].floats()));  // between them
   return all + 0.45 * states + 2.5 + moved * 1.0e-7;  // (10 MB take as long as a chunk)
 }
 
@@ -218,15 +223,30 @@ Plan plan_of(const cnn_linear_shape& s, int roles) {
   // No segments whose state, written and read twice, is more to move than its tokens.
   const int64_t least = 16 * (int64_t)s.Dk * s.Dv / (2 * (s.Dk + s.Dv) * (int64_t)type_bytes(s.type));
   const int64_t most = s.T / (least > 2 * C ? least : 2 * C);
-  p.length = ((int64_t)s.T + C - 1) / C * C;
-  double best = cost_of(s, roles, p.length);
-  for (int64_t n = 2; n <= most && n <= 256; ++n) {
-    const int64_t length = ((s.T + n - 1) / n + C - 1) / C * C;
-    const double cost = cost_of(s, roles, length);
-    if (cost < best) best = cost, p.length = length;
+  double best = 0.0;
+  // Each role in its own form, or all in one that holds them, which is one launch for two: 2 x 11 tokens of 12 heads of 80 x 128 (fp16)
+  // take 7 us so and 15 us the other way.
+  for (int joint = 0; joint < (roles == 1 ? 1 : 2); ++joint) {
+    Plan now{};
+    for (int f = 0; f < 2; ++f) {
+      const int dk = f ? s.Dv : s.Dk, dv = f ? s.Dk : s.Dv;
+      Form& form = now.form[f];
+      form.DKP = padded(dk), form.columns = block_columns(dk, dv);
+      if (joint) {
+        const int other = block_columns(dv, dk);
+        form.DKP = padded(dk > dv ? dk : dv);
+        form.columns = form.columns > other ? form.columns : other;
+      }
+      form.blocks = (dv + form.columns - 1) / form.columns;
+    }
+    for (int64_t n = 1; n == 1 || (n <= most && n <= 256); ++n) {
+      now.length = ((s.T + n - 1) / n + C - 1) / C * C;
+      const double cost = cost_of(s, now, roles, now.length);
+      if (best == 0.0 || cost < best) best = cost, p = now;
+    }
   }
   p.segments = (int)((s.T + p.length - 1) / p.length);
-  const int64_t floats = carry_floats(s.Dk, s.Dv) > carry_floats(s.Dv, s.Dk) || roles == 1 ? carry_floats(s.Dk, s.Dv) : carry_floats(s.Dv, s.Dk);
+  const int64_t floats = roles == 1 || p.form[0].floats() > p.form[1].floats() ? p.form[0].floats() : p.form[1].floats();
   p.state_bytes = p.segments > 1 ? rounded((size_t)units * p.segments * floats * 4) : 0;
   p.bytes = p.state_bytes * (roles > 1 ? 2 : 1);  // (d_k's states are d_v's transposed)
   if (roles > 1 && s.H != s.Hk) {
@@ -245,9 +265,10 @@ Args args_of(const cnn_linear_shape& s, const Plan& p, const float* decay, const
   return a;
 }
 
+void set_form(Role& r, const Form& f) { r.DKP = f.DKP, r.columns = f.columns, r.blocks = f.blocks; }
+
 int run(Args& a, int type, int roles, hipStream_t st) {
   const auto scan = type == CNN_F32 ? run_scan_f32 : type == CNN_BF16 ? run_scan_bf16 : run_scan_f16;
-  for (int r = 0; r < roles; ++r) a.role[r].blocks = blocks_of(a.role[r].DK, a.role[r].DV);
   if (a.segments > 1) {
     Args own = a;  // the roles that have states of their own
     int count = 0;
@@ -255,7 +276,7 @@ int run(Args& a, int type, int roles, hipStream_t st) {
     for (int r = 0; r < roles; ++r) {
       if (a.role[r].flipped) continue;
       own.role[count++] = a.role[r];
-      const int64_t g = (carry_floats(a.role[r].DK, a.role[r].DV) / 4 + CARRY_THREADS - 1) / CARRY_THREADS;
+      const int64_t g = (carry_floats(a.role[r]) / 4 + CARRY_THREADS - 1) / CARRY_THREADS;
       groups = g > groups ? g : groups;
     }
     const int rc = scan(own, count, true, st);
@@ -292,6 +313,7 @@ int cnn_linear_attention_fwd(const cnn_linear_shape* s, const cnn_heads* q, cons
   r.q = operand_of(q, 1), r.k = operand_of(k, share), r.v = operand_of(v, share);
   r.out = o, r.first = initial_state, r.last = final_state, r.carry = static_cast<float*>(workspace);
   r.first_i = s->Dv, r.first_j = 1, r.DK = s->Dk, r.DV = s->Dv;
+  set_form(r, p.form[0]);
   r.scale = scale, r.first_by = r.last_by = 1.0f;
   r.packed = near_ok(s) && packed_ok(q, s->Dk, s->type) && packed_ok(k, s->Dk, s->type) && packed_ok(v, s->Dv, s->type);
   return run(a, s->type, 1, (hipStream_t)hip_stream);
@@ -323,6 +345,7 @@ int cnn_linear_attention_bwd(const cnn_linear_shape* s, const cnn_heads* q, cons
     r.scale = scale, r.packed = packed, r.first_by = r.last_by = 1.0f;
     r.reversed = i > 0, r.wide = i > 0 && shared;
     r.DK = i < 2 ? s->Dv : s->Dk, r.DV = i < 2 ? s->Dk : s->Dv;
+    set_form(r, p.form[i < 2]);
     r.first = i == 0 ? initial_state : d_final_state;
     r.first_i = i < 2 ? 1 : s->Dv, r.first_j = i < 2 ? s->Dv : 1;  // the first two hold the state transposed
     if (i > 0 && (d_final_state || d_initial_state)) r.first_by = 1.0f / scale, r.last_by = scale;  // (else any scale, zero too)
@@ -331,7 +354,7 @@ int cnn_linear_attention_bwd(const cnn_linear_shape* s, const cnn_heads* q, cons
   a.role[1].q = V, a.role[1].k = D, a.role[1].v = Q, a.role[1].out = shared ? ws + p.wide_k : d_k;
   a.role[2].q = K, a.role[2].k = Q, a.role[2].v = D, a.role[2].out = shared ? ws + p.wide_v : d_v;
   a.role[2].last = d_initial_state;
-  if (p.segments > 1) a.role[1].flipped = a.role[2].carry;
+  if (p.segments > 1) a.role[1].flipped = a.role[2].carry, a.role[1].flipped_rows = p.form[0].DKP, a.role[1].flipped_floats = p.form[0].floats();
   hipStream_t st = (hipStream_t)hip_stream;
   const int rc = run(a, s->type, 3, st);
   if (rc != CNN_OK || !shared) return rc;
