@@ -341,6 +341,12 @@ __device__ __forceinline__ int anew(int x) {
   return x;
 }
 
+using Bytes = __attribute__((address_space(1))) char;  // memory of the GPU
+// Waits for the loads from memory that are under way.  The compiler's own waits in a loop allow for what may be pending on any way to
+// them: without this one before the loop the products with the state waited in every chunk for the next chunk's rows, and without the
+// one before rows are stored to LDS, which some lanes skip, the next loads waited for all stores to memory.
+__device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // (vmcnt 0, the other counters at their most)
+
 // Where a state's register i of tile m of a wave's lane stands.  A pair of tiles is an operand of a product over 32 rows as it is.
 __device__ __forceinline__ int state_row(int m, int lane, int i) { return 32 * (m >> 1) + 8 * (lane >> 4) + 4 * (m & 1) + i; }
 __device__ __forceinline__ int state_column(int tile, int lane) { return 16 * tile + (lane & 15); }  // tile: of sixteen columns
@@ -497,14 +503,17 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
   for (int j = 0; j < 8; ++j) follow[j] = power(log2a, C - 1 - 16 * (j >> 2) - (j & 3) - 4 * g);
 
   // out: rows of a chunk are tokens, columns 4 g + i of a tile of sixteen
-  const int out_stride = args.heads * DV, out_column = 16 * NW * wave + 4 * g;
-  int64_t out = ((batch * args.T + low) * args.heads + head) * DV + dv0;
-  const int64_t out_step = advance * out_stride;
-  const int out_at = (reversed ? C - 1 - r : r) * out_stride + out_column, out_next = reversed ? -16 * out_stride : 16 * out_stride;  // (of tile 1)
-  const float scale = R.scale;
   const bool wide = R.wide;
+  const int out_column = 16 * NW * wave + 4 * g, out_size = wide ? 4 : (int)sizeof(T);
+  const int64_t out_stride = (int64_t)args.heads * DV * out_size, out_step = advance * out_stride;  // in bytes
+  Bytes* out = (Bytes*)R.out + (((batch * args.T + low) * args.heads + head) * DV + dv0) * out_size;
+  uint32_t out_at[2];  // PACKED: rows of a chunk are less than 2^31 bytes apart
+#pragma unroll
+  for (int t = 0; t < 2; ++t) out_at[t] = (uint32_t)((reversed ? C - 1 - 16 * t - r : 16 * t + r) * (int)out_stride + out_column * out_size);
+  const float scale = R.scale;
 
   __bf16* tile = tiles;
+  loads_done();
   if (begin < end) {
     if (pad) k_in.clear(pad);  // what is no token adds nothing
     store(tile);
@@ -606,6 +615,10 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
       if ((m & 3) == 3 || (NP > 1 && (m & 1))) in_steps();
     }
 
+    __bf16* const next = S::SETS == 1 || tile != tiles ? tiles : tiles + SET;
+    if constexpr (S::SETS == 1) __syncthreads();  // the tiles may be overwritten
+    loads_done();
+    if (more) store(next);
     if constexpr (!STATE_ONLY) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -613,28 +626,26 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
           const f4 y = acc[t][w] * scale;
-          if constexpr (PACKED) {  // whole packs, so width is a multiple of eight; the chunk's rows are less than 2^31 bytes apart
+          if constexpr (PACKED) {  // whole packs, so width is a multiple of eight
             if (out_column + 16 * w >= width) continue;
-            const uint32_t e = (uint32_t)(out_at + t * out_next + 16 * w);
-            if (wide) *reinterpret_cast<f4*>(static_cast<float*>(R.out) + out + e) = y;
-            else *reinterpret_cast<Pack<T, 4>*>(static_cast<T*>(R.out) + out + e) = Pack<T, 4>{{(T)y[0], (T)y[1], (T)y[2], (T)y[3]}};
+            using Four = std::conditional_t<sizeof(T) == 4, f4, f2>;
+            const Four narrow = __builtin_bit_cast(Four, Pack<T, 4>{{(T)y[0], (T)y[1], (T)y[2], (T)y[3]}});
+            if (wide) *(__attribute__((address_space(1))) f4*)(out + out_at[t] + 64 * w) = y;
+            else *(__attribute__((address_space(1))) Four*)(out + out_at[t] + 16 * w * (int)sizeof(T)) = narrow;
           } else {
-            const int64_t e = out + (int64_t)(reversed ? C - 1 - 16 * t - r : 16 * t + r) * args.heads * DV + out_column + 16 * w;
+            Bytes* const to = out + (reversed ? C - 1 - 16 * t - r : 16 * t + r) * out_stride + (out_column + 16 * w) * out_size;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               if (out_column + 16 * w + i >= width) continue;
-              if (wide) static_cast<float*>(R.out)[e + i] = y[i];
-              else static_cast<T*>(R.out)[e + i] = (T)y[i];
+              if (wide) ((__attribute__((address_space(1))) float*)to)[i] = y[i];
+              else ((__attribute__((address_space(1))) T*)to)[i] = (T)y[i];
             }
           }
         }
       }
       out += out_step;
     }
-    shift = 1, pad = 0;
-    if constexpr (S::SETS == 1) __syncthreads();  // the tiles may be overwritten
-    else tile = tile == tiles ? tiles + SET : tiles;
-    if (more) store(tile);
+    shift = 1, pad = 0, tile = next;
     __syncthreads();
   }
 
