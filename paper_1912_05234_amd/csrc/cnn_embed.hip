@@ -71,7 +71,7 @@ struct Entry {  // of the sorted list
 
 constexpr int RADIX = 256;
 constexpr int SORT_THREADS = 256, SORT_WAVES = SORT_THREADS / 64;
-constexpr int SORT_EACH = 8;        // positions that a lane holds at once, so that their loads are under way together
+constexpr int SORT_EACH = 4;        // positions that a lane holds at once, so that their loads are under way together (8: 64 us for 60 below)
 constexpr int SORT_CHUNK = SORT_THREADS * SORT_EACH;  // positions to a workgroup, at least
 constexpr int SORT_GROUPS = 256;    // workgroups of a pass, at most: each adds up the counts of those before it
 constexpr int SMALL_THREADS = 1024, SMALL_WAVES = SMALL_THREADS / 64, SMALL_EACH = 4;
