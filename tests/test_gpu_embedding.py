@@ -46,6 +46,18 @@ def test_lookup(N, V, D, spread, type_):
         ref.near(out, want, 2.0 ** -24 * np.abs(want), dtype, "lookup %s" % type_)  # the product is rounded to fp32 first
 
 
+@pytest.mark.parametrize("type_,D", [("bf16", 1024), ("fp32", 224)])
+def test_lookup_of_a_long_output(type_, D):
+    """Past 96 MB of whole lines of 128 bytes the output goes past the caches; and the row before that."""
+    row = D * (4 if type_ == "fp32" else 2)
+    for N in ((96 << 20) // row, (96 << 20) // row + 3, 120011):
+        table = torch.randn(301, D, generator=torch.Generator().manual_seed(N)).to(DEV, ref.TYPES[type_])
+        tokens = (torch.arange(N, device=DEV) * 7919) % 303 - 1
+        out = binding.embedding_fwd(table, tokens, 0.5)
+        padded = torch.cat([table * 0.5, torch.zeros(1, D, device=DEV, dtype=table.dtype)])
+        assert torch.equal(out, padded[torch.where((tokens < 0) | (tokens >= 301), 301, tokens)])
+
+
 def test_lookup_of_more_rows_than_one_dimension_of_a_grid_holds():
     """Four rows to a workgroup of 256 threads: past 2^26 rows there are 2^32 threads."""
     N, V, D = (1 << 26) + 5, 7, 129
