@@ -12,7 +12,7 @@
 // k' = q, v' = d_o, the last two with time reversed), so one kernel serves all four.  Below, q, k, v are a role's, DK is the
 // width of its q and k, DV that of its v and out.
 //
-// A workgroup takes a block of DV columns of one sequence and head, and walks the chunks of its segment of the time axis; the
+// A workgroup takes a block of DV columns (32 to 128, a wave to 32) of one sequence and head, and walks the chunks of its segment of the time axis; the
 // state stays in the accumulators of the matrix instructions, fp32, each wave holding 32 columns.  Where there are too few
 // heads to fill the GPU the time axis is cut into segments: a first pass finds what each segment adds to the state, a scan over
 // the segments turns that into the state that each starts from, and the second pass runs them side by side.
@@ -22,6 +22,12 @@
 // What the kernel computes itself is not rounded to the input's type: state and scores are cut into two pieces (2^-17 of each is
 // lost, of results that are rounded to 2^-9 or 2^-12), three for floats; a^{C-1-s} v_s into three, so that the state is exact to fp32
 // sums for every type, or two in the second pass over segments, whose own state is no result.
+//
+// Measured (MI355X; in brackets the bytes that have to be moved at a copy's 5.15 TB/s): 8192 tokens of 2 x 16 heads of 128 (bf16) 120 us
+// (53): 33 for the first pass, 14 for the scan over 16 segments, 71 for the second pass, in which a SIMD's two waves issue vector
+// instructions, most of them cutting and decaying the state, 60 % of the time and matrix instructions 33 %.  100 x 2 heads of 784 tokens,
+// 32 wide (fp32): 33 us forward on uneven lengths (10), 72 us backward (27), bound by the cutting of floats, some 700 vector instructions
+// for 32 tokens.  3 x 12 heads of 2047 tokens, 64 and 96 wide (fp16), backward: 107 us (10), of six dependent launches.
 #pragma once
 
 #include <type_traits>
