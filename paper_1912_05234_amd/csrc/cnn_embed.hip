@@ -37,14 +37,6 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, int64_t n) {
   return (int64_t) static_cast<const I*>(tokens)[n];
 }
 
-// Stores past the caches, for packs of sixteen bytes.
-template <class P>
-__device__ __forceinline__ void put_past_caches(P* at, const P& v) {
-  using Words = uint32_t __attribute__((ext_vector_type(4)));
-  static_assert(sizeof(P) == 16, "packs of sixteen bytes");
-  __builtin_nontemporal_store(__builtin_bit_cast(Words, v), reinterpret_cast<Words*>(at));
-}
-
 // Lanes in groups that each take ROWS rows at once, so that as many loads are in flight.
 template <class T, int VN, class I, int ROWS, bool PAST_CACHES>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_fwd_kernel(EmbedArgs a) {

@@ -103,8 +103,8 @@ constexpr int STEP_THREADS = 256, STEP_COLUMNS = 32;
 
 // A workgroup takes 32 columns of one state: the whole of DK, so that nothing has to be joined outside it.  Every thread
 // updates VN columns of one row in so many, and keeps their products with q; these are added over the rows at the end.
-// Memory bounds it: 256 rows of 16 states of 128 x 128 (537 MB read and written) take 92 us, 5.8 TB/s.
-template <class T, int VN>
+// Memory bounds it: 256 rows of 16 states of 128 x 128 (537 MB read and written) take 100 to 109 us, 5.4 to 4.9 TB/s.
+template <class T, int VN, bool PAST_CACHES>
 __global__ __launch_bounds__(STEP_THREADS) void step_kernel(StepArgs a) {
   constexpr int LANES = STEP_COLUMNS / VN, ROWS = STEP_THREADS / LANES, AHEAD = 4;
   using P = Pack<float, VN>;
@@ -135,7 +135,8 @@ __global__ __launch_bounds__(STEP_THREADS) void step_kernel(StepArgs a) {
     for (int r = 0; r < AHEAD; ++r) {
       const int row = i + r * ROWS;
       if (row >= a.DK || !mine) continue;
-      s[r] = *reinterpret_cast<const P*>(state + (int64_t)row * a.DV + col);
+      if constexpr (PAST_CACHES) s[r] = got_past_caches(reinterpret_cast<const P*>(state + (int64_t)row * a.DV + col));
+      else s[r] = *reinterpret_cast<const P*>(state + (int64_t)row * a.DV + col);
       key[r] = (float)k[row], query[r] = (float)q[row];
     }
 #pragma unroll
@@ -147,7 +148,8 @@ __global__ __launch_bounds__(STEP_THREADS) void step_kernel(StepArgs a) {
         s[r].v[j] = s[r].v[j] * decay + key[r] * value[j];
         sum[j] += query[r] * s[r].v[j];
       }
-      *reinterpret_cast<P*>(state + (int64_t)row * a.DV + col) = s[r];
+      if constexpr (PAST_CACHES) put_past_caches(reinterpret_cast<P*>(state + (int64_t)row * a.DV + col), s[r]);
+      else *reinterpret_cast<P*>(state + (int64_t)row * a.DV + col) = s[r];
     }
   }
 #pragma unroll
@@ -385,10 +387,14 @@ int cnn_linear_attention_step(const cnn_linear_shape* s, const cnn_heads* q, con
   const int share = s->H / s->Hk, blocks = (s->Dv + STEP_COLUMNS - 1) / STEP_COLUMNS;
   const StepArgs a{operand_of(q, 1), operand_of(k, share), operand_of(v, share), decay, state, slots, o, pool, s->H, s->Dk, s->Dv, blocks, scale};
   const unsigned grid = (unsigned)((int64_t)s->B * s->H * blocks);
+  // States that do not fit the last cache of 256 MB go past it.  268 MB of them 98 and 125 us (again and again, and after other work),
+  // past the caches 100 and 109; 402 MB 153 and 167, 143 and 151; but 134 MB 42 and 71, 51 and 59.
+  const bool past_caches = (int64_t)s->B * s->H * s->Dk * s->Dv * 4 >= (int64_t)256 << 20;
   return with_type(s->type, [&](auto t) {
     using T = decltype(t);
-    if (s->Dv % 4 == 0) step_kernel<T, 4><<<grid, STEP_THREADS, 0, (hipStream_t)hip_stream>>>(a);
-    else step_kernel<T, 1><<<grid, STEP_THREADS, 0, (hipStream_t)hip_stream>>>(a);
+    if (past_caches && s->Dv % 4 == 0) step_kernel<T, 4, true><<<grid, STEP_THREADS, 0, (hipStream_t)hip_stream>>>(a);
+    else if (s->Dv % 4 == 0) step_kernel<T, 4, false><<<grid, STEP_THREADS, 0, (hipStream_t)hip_stream>>>(a);
+    else step_kernel<T, 1, false><<<grid, STEP_THREADS, 0, (hipStream_t)hip_stream>>>(a);
     return launch_status();
   });
 }

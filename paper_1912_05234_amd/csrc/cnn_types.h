@@ -17,6 +17,19 @@ struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Pack {
   T v[N];
 };
 
+// Loads and stores past the caches, for packs of sixteen bytes.
+using Words = uint32_t __attribute__((ext_vector_type(4)));
+template <class P>
+__device__ __forceinline__ void put_past_caches(P* at, const P& v) {
+  static_assert(sizeof(P) == 16, "packs of sixteen bytes");
+  __builtin_nontemporal_store(__builtin_bit_cast(Words, v), reinterpret_cast<Words*>(at));
+}
+template <class P>
+__device__ __forceinline__ P got_past_caches(const P* at) {
+  static_assert(sizeof(P) == 16, "packs of sixteen bytes");
+  return __builtin_bit_cast(P, __builtin_nontemporal_load(reinterpret_cast<const Words*>(at)));
+}
+
 // Calls fn with a value of the element type that `type` names.
 template <class FN>
 auto with_type(int type, FN fn) {

@@ -151,6 +151,23 @@ def test_tokens_one_by_one(shape, type_):
     assert torch.equal(state[others], before[others])
 
 
+def test_states_larger_than_the_caches():
+    """256 MB of states in one call against two calls of half of them, whose tokens are tested above: the same arithmetic."""
+    B, H, D = 256, 16, 128
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    q, k, v = (torch.randn(B, H, D, generator=gen, device=DEV).bfloat16() for _ in range(3))
+    state = torch.randn(B + 3, H, D, D, generator=gen, device=DEV)
+    decay, other = torch.linspace(0.5, 1.0, H, device=DEV), state.clone()
+    slots = torch.randperm(B + 3, generator=gen, device=DEV)[:B].to(torch.int32)
+    slots[5], slots[200] = -1, B + 3
+    for _ in range(2):
+        o = binding.linear_attention_step(q, k, v, decay, state, 0.3, slots=slots)
+        halves = [binding.linear_attention_step(q[i:i + 128], k[i:i + 128], v[i:i + 128], decay, other, 0.3, slots=slots[i:i + 128])
+                  for i in (0, 128)]
+        assert torch.equal(o, torch.cat(halves)) and torch.equal(state, other)
+        assert (o[5] == 0).all() and (o[200] == 0).all()
+
+
 def test_prompt_then_tokens_is_the_whole_sequence():
     case = (2, 700, 2, 2, 64, 96, None, False, True)
     q, k, v, decay, _, _, _, _ = make(case, "fp32")
