@@ -17,17 +17,25 @@ struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Pack {
   T v[N];
 };
 
-// Loads and stores past the caches, for packs of sixteen bytes.
+// Loads and stores past the caches, for packs of whole sixteen bytes.
 using Words = uint32_t __attribute__((ext_vector_type(4)));
 template <class P>
+struct Sixteens {
+  static_assert(sizeof(P) % 16 == 0, "packs of whole sixteen bytes");
+  Words w[sizeof(P) / 16];
+};
+template <class P>
 __device__ __forceinline__ void put_past_caches(P* at, const P& v) {
-  static_assert(sizeof(P) == 16, "packs of sixteen bytes");
-  __builtin_nontemporal_store(__builtin_bit_cast(Words, v), reinterpret_cast<Words*>(at));
+  const Sixteens<P> words = __builtin_bit_cast(Sixteens<P>, v);
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(P) / 16); ++i) __builtin_nontemporal_store(words.w[i], reinterpret_cast<Words*>(at) + i);
 }
 template <class P>
 __device__ __forceinline__ P got_past_caches(const P* at) {
-  static_assert(sizeof(P) == 16, "packs of sixteen bytes");
-  return __builtin_bit_cast(P, __builtin_nontemporal_load(reinterpret_cast<const Words*>(at)));
+  Sixteens<P> words;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(P) / 16); ++i) words.w[i] = __builtin_nontemporal_load(reinterpret_cast<const Words*>(at) + i);
+  return __builtin_bit_cast(P, words);
 }
 
 // Calls fn with a value of the element type that `type` names.

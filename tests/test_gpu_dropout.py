@@ -36,6 +36,19 @@ def test_against_definition(n, p, type_):
     ref.near(both, total, 2.0 ** -23 * np.abs(want) + 2.0 ** -24 * np.abs(total), dtype, "with residual %s" % type_)
 
 
+@pytest.mark.parametrize("type_", ["bf16", "fp16"])
+def test_more_than_the_last_cache_holds(type_):
+    """Past 256 MB read and written, against the same elements as floats, whose kernel is another: one mask, values exact for p = 1/2."""
+    n, dtype = (256 << 20) // 4 + 1003, ref.TYPES[type_]
+    x = torch.randn(n, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).to(dtype)
+    res = x.flip(0)
+    want = binding.dropout_fwd(x.float(), 0.5, 11, 12)
+    assert torch.equal(binding.dropout_fwd(x, 0.5, 11, 12), want.to(dtype))
+    assert torch.equal(binding.dropout_fwd(x, 0.5, 11, 12, residual=res), (want + res.float()).to(dtype))
+    small = binding.dropout_fwd(x[:100003].contiguous(), 0.5, 11, 12)
+    assert torch.equal(small, want[:100003].to(dtype))
+
+
 def test_every_bit_of_the_limit_counts():
     """Elements whose high sixteen bits equal the limit's are decided by the low ones: limits around the numbers drawn themselves."""
     n = 4096
