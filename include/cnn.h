@@ -311,7 +311,8 @@ int cnn_linear_attention_fwd(const cnn_linear_shape* shape, const cnn_heads* q, 
 /* Gradients for the error d_o of o and (nullable) d_final_state of the final state: d_q, d_k, d_v and (nullable) d_initial_state.
  * With G_t the error of S_t: G_t = scale q_t d_o_t^T + a G_{t+1} (d_final_state past the end), d_q_t = scale S_t d_o_t,
  * d_k_t = G_t v_t, d_v_t = G_t^T k_t, summed over the query heads of a shared head; d_initial_state = a G_0, or d_final_state for a
- * sequence of length 0; it must not be the memory of an input.  With a state's error given or wanted, 2^-100 <= |scale| <= 2^100. */
+ * sequence of length 0; it must not be the memory of an input.  With a state's error given or wanted, 2^-100 <= |scale| <= 2^100; any d_final_state below
+ * 2^127 is then taken, however far from the scale.  (Given one, G itself is held, else G over the scale.) */
 size_t cnn_linear_attention_bwd_workspace_bytes(const cnn_linear_shape* shape);
 int cnn_linear_attention_bwd(const cnn_linear_shape* shape, const cnn_heads* q, const cnn_heads* k, const cnn_heads* v,
                              const float* decay, const cnn_heads* d_o, float scale, const int32_t* lengths,

@@ -62,7 +62,9 @@ struct Role {
   int DK, DV, DKP, columns, blocks;  // DK padded, columns of a workgroup, workgroups to a state
   int flipped_rows;                  // DKP of that role
   int64_t flipped_floats;            // of one of its states
-  float scale, first_by, last_by;
+  float scale;    // of out
+  float inside;   // of what the tokens add to the state: the scale where the state before the sequence already holds it
+  float last_by;  // of the state after it: the scale where neither the tokens nor the state before them hold it
   int reversed;  // the last token of a sequence comes first; the first state then already stands at the first token
   int wide, packed;  // packed: rows are made of whole packs of eight elements at addresses that are multiples of 16 bytes
 };
@@ -489,10 +491,6 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
         }
       }
     }
-#pragma unroll
-    for (int m = 0; m < M; ++m)
-#pragma unroll
-      for (int w = 0; w < NW; ++w) state[m][w] *= R.first_by;
   }
   int shift = reversed && begin == 0 ? 0 : 1;  // powers of a between the state before the chunk and the chunk's first token
 
@@ -507,6 +505,12 @@ __global__ __launch_bounds__(64 * WAVES, waves_wanted(DKP)) void scan_kernel(Arg
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) follow[j] = power(log2a, C - 1 - 16 * (j >> 2) - (j & 3) - 4 * g);
+  if (const float inside = R.inside; inside != 1.0f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) on_diagonal[i] *= inside, below[i] *= inside;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) follow[j] *= inside;
+  }
 
   // out: rows of a chunk are tokens, columns 4 g + i of a tile of sixteen
   const bool wide = R.wide;

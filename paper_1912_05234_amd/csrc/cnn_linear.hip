@@ -24,7 +24,7 @@ __global__ __launch_bounds__(CARRY_THREADS) void carry_kernel(Args args) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (row + i < R.DK) raw[i] = R.first[unit * R.DK * R.DV + (row + i) * R.first_i + column * R.first_j];
-  f4 run = raw * R.first_by;
+  f4 run = raw;
   f4* carry = reinterpret_cast<f4*>(R.carry) + unit * args.segments * size + at;
   const double log2a = log2((double)a);
   const auto power_of = [&](int64_t e) { return e > 0 ? (float)exp2(log2a * (double)e) : 1.0f; };
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(CARRY_THREADS) void carry_kernel(Args args) {
     }
   }
   if (R.last && column < R.DV) {
-    run = n == 0 ? raw : run * (R.last_by * (R.reversed ? a : 1.0f));
+    if (n > 0) run *= R.last_by * (R.reversed ? a : 1.0f);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (row + i < R.DK) R.last[(unit * R.DK + row + i) * R.DV + column] = run[i];
@@ -319,7 +319,7 @@ int cnn_linear_attention_fwd(const cnn_linear_shape* s, const cnn_heads* q, cons
   r.out = o, r.first = initial_state, r.last = final_state, r.carry = static_cast<float*>(workspace);
   r.first_i = s->Dv, r.first_j = 1, r.DK = s->Dk, r.DV = s->Dv;
   set_form(r, p.form[0]);
-  r.scale = scale, r.first_by = r.last_by = 1.0f;
+  r.scale = scale, r.inside = r.last_by = 1.0f;
   r.packed = near_ok(s) && packed_ok(q, s->Dk, s->type) && packed_ok(k, s->Dk, s->type) && packed_ok(v, s->Dv, s->type);
   return run(a, s->type, 1, (hipStream_t)hip_stream);
 }
@@ -347,13 +347,15 @@ int cnn_linear_attention_bwd(const cnn_linear_shape* s, const cnn_heads* q, cons
   for (int i = 0; i < 3; ++i) {
     Role& r = a.role[i];
     r.carry = reinterpret_cast<float*>(ws + (i ? p.state_bytes : 0));
-    r.scale = scale, r.packed = packed, r.first_by = r.last_by = 1.0f;
+    r.scale = scale, r.inside = 1.0f, r.last_by = scale, r.packed = packed;
     r.reversed = i > 0, r.wide = i > 0 && shared;
     r.DK = i < 2 ? s->Dv : s->Dk, r.DV = i < 2 ? s->Dk : s->Dv;
     set_form(r, p.form[i < 2]);
     r.first = i == 0 ? initial_state : d_final_state;
     r.first_i = i < 2 ? 1 : s->Dv, r.first_j = i < 2 ? s->Dv : 1;  // the first two hold the state transposed
-    if (i > 0 && (d_final_state || d_initial_state)) r.first_by = 1.0f / scale, r.last_by = scale;  // (else any scale, zero too)
+    // An error of the state over the scale may be past the range of numbers, and a scale alone next to its end: the first is taken as it
+    // is, and where there is none the scale comes last.
+    if (i > 0 && d_final_state) r.scale = r.last_by = 1.0f, r.inside = scale;
   }
   a.role[0].q = D, a.role[0].k = V, a.role[0].v = K, a.role[0].out = d_q;
   a.role[1].q = V, a.role[1].k = D, a.role[1].v = Q, a.role[1].out = shared ? ws + p.wide_k : d_k;

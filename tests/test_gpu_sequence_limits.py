@@ -1,0 +1,32 @@
+"""The sequence operators at the ends of what they take."""
+import pytest
+import torch
+
+import sequence_reference as ref
+from paper_1912_05234_amd import binding
+from test_gpu_linear_attention import CUT, in_64, magnitudes, make, steps
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.mark.parametrize("type_", list(ref.TYPES))
+@pytest.mark.parametrize("case", [(2, 40, 2, 1, 32, 48, [40, 0], True, False), (1, 21, 1, 1, 20, 7, None, True, True),
+                                  (1, 900, 2, 2, 32, 64, None, True, False)], ids=["one pass", "odd widths", "segments"])
+@pytest.mark.parametrize("scale,by_d_o,by_final", [(2.0 ** -100, 1.0, 2.0 ** 30), (-2.0 ** -100, 1.0, 2.0 ** 90), (2.0 ** 100, 0.0, 2.0 ** -60),
+                                                   (2.0 ** 100, 0.0, 2.0 ** -26)])
+def test_errors_of_states_far_from_the_scale(scale, by_d_o, by_final, case, type_):
+    """The state's error over the scale is past the range of fp32, the state's error itself and what it leads to are not.  Bounds as in
+    test_backward; decays near 1, so that the state's error reaches every token."""
+    q, k, v, decay, d_o, n, initial, d_final = make(case, type_)
+    decay, d_o, d_final = torch.linspace(0.995, 0.9995, len(decay), device=DEV), d_o * by_d_o, d_final * by_final
+    if type_ == "fp16" and by_final > 1.0:  # (whose range ends at 2^16: only the state's own error then)
+        k, v = k * 0.0, v * 0.0
+    arrays = in_64(q, k, v, decay, d_o)
+    i64, f64 = in_64(initial, d_final)
+    want = ref.linear_attention_gradient(*arrays, scale, case[6], i64, f64)
+    size = ref.linear_attention_gradient(*magnitudes(*arrays), abs(scale), case[6], *magnitudes(i64, f64))
+    got = binding.linear_attention_bwd(q, k, v, decay, d_o, scale, lengths=n, initial_state=initial, d_final_state=d_final, want_d_state=True)
+    for name, g, w, m, dtype in zip(("d_q", "d_k", "d_v", "d_state"), got, want, size, [q.dtype] * 3 + [torch.float32]):
+        cut = 0.0 if name == "d_state" else CUT[type_]
+        ref.near(g, w, m * (steps(case) + cut), dtype, "%s far from the scale %s" % (name, type_))
