@@ -338,6 +338,7 @@ uint64_t word64(PyObject* o) {
 CALL(embedding_fwd, 3)  // table, tokens, scale
   const at::Tensor &table = any_tensor(a[0]), &tokens = token_tensor(a[1]);
   if (table.dim() != 2) raise(PyExc_ValueError, "expected a table of 2 dimensions");
+  if (table.size(1) > INT_MAX) raise(PyExc_ValueError, "a dimension is too large");
   const int type = element_type(table);
   const float scale = (float)number(a[2]);
   std::vector<int64_t> sizes = tokens.sizes().vec();

@@ -1,4 +1,4 @@
-"""The sequence operators at the ends of what they take."""
+"""The sequence operators at the ends of what they take: scales and errors of states far from 1, sizes past 32 bits."""
 import pytest
 import torch
 
@@ -30,3 +30,10 @@ def test_errors_of_states_far_from_the_scale(scale, by_d_o, by_final, case, type
     for name, g, w, m, dtype in zip(("d_q", "d_k", "d_v", "d_state"), got, want, size, [q.dtype] * 3 + [torch.float32]):
         cut = 0.0 if name == "d_state" else CUT[type_]
         ref.near(g, w, m * (steps(case) + cut), dtype, "%s far from the scale %s" % (name, type_))
+
+
+def test_a_table_wider_than_32_bits_count_is_refused():
+    """2^32 + 8 columns are not 8."""
+    table = torch.empty(1, (1 << 32) + 8, dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(ValueError):
+        binding.embedding_fwd(table, torch.zeros(1, dtype=torch.int32, device=DEV))
