@@ -450,7 +450,7 @@ Linear linear_of(PyObject* const* a, int dims) {  // q, k, v, decay, scale
   bool fits = k.size(0) == B && v.size(0) == B && k.size(h) == v.size(h) && k.size(d) == q.size(d);
   if (dims == 4) fits = fits && k.size(1) == T && v.size(1) == T;
   if (!fits) raise(PyExc_ValueError, "expected q, k and v of one batch and length, k and v of as many heads, q and k of one width");
-  for (const int64_t n : {B, T, q.size(h), q.size(d), v.size(d)})
+  for (const int64_t n : {B, T, q.size(h), k.size(h), q.size(d), v.size(d)})
     if (n > INT_MAX) raise(PyExc_ValueError, "a dimension is too large");
   const int64_t H = q.size(h), Hk = k.size(h), Dk = q.size(d), Dv = v.size(d);
   const float* decay = a[3] == Py_None ? (raise(PyExc_TypeError, "expected a tensor of decays"), nullptr) : optional(a[3], {H}, "decays");

@@ -37,3 +37,14 @@ def test_a_table_wider_than_32_bits_count_is_refused():
     table = torch.empty(1, (1 << 32) + 8, dtype=torch.bfloat16, device=DEV)
     with pytest.raises(ValueError):
         binding.embedding_fwd(table, torch.zeros(1, dtype=torch.int32, device=DEV))
+
+
+def test_more_key_heads_than_32_bits_count_are_refused():
+    """2^32 + 2 key heads (one, repeated without memory of its own) are not 2."""
+    q, decay = torch.ones(1, 3, 2, 8, device=DEV), torch.ones(2, device=DEV)
+    kv = torch.ones(1, 3, 1, 8, device=DEV).expand(1, 3, (1 << 32) + 2, 8)
+    with pytest.raises(ValueError):
+        binding.linear_attention_fwd(q, kv, kv, decay)
+    state = torch.zeros(1, 2, 8, 8, device=DEV)
+    with pytest.raises(ValueError):
+        binding.linear_attention_step(q[:, 0], kv[:, 0], kv[:, 0], decay, state)
