@@ -292,7 +292,8 @@ int cnn_dropout_bwd(const void* d_y, void* d_x, size_t n, int type, double p, ui
  * B * H <= 2^20.  q, k, v (and d_o) are given with their strides, in elements, none negative, and need only be aligned to their
  * element: slices of one projection's output serve as they are.  (Rows of whole packs of eight elements, all at multiples of 16
  * bytes, are read sixteen bytes at a time, others element by element.)  Results are contiguous: [B,T,heads,width] and
- * [B,H,Dk,Dv].  decay[H]: 0 <= a <= 1, not checked on the device; constants of the operator, without a gradient.
+ * [B,H,Dk,Dv].  decay[H]: 0 <= a <= 1, not checked on the device (a NaN shows in all results of its head);
+ * constants of the operator, without a gradient.
  * lengths[B] (nullable: all T; below 0 counts as 0, above T as T): tokens past a sequence's length are not read, and their rows of
  * the results are zero.  Inputs up to it must be finite and below 2^127.  An initial or final state may be NULL (zero; not wanted);
  * they may be the same memory.  `workspace` holds states of pieces of the sequences where there are too few heads to fill the GPU,

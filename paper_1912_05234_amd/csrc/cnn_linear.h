@@ -334,10 +334,10 @@ struct Columns {
   }
 };
 
-// log2 of a decay, finite also for a = 0 (a^0 = 1 and a^n = 0 then come out right), to fp32 also next to 1.
+// log2 of a decay, finite also for a = 0 (a^0 = 1 and a^n = 0 then come out right), to fp32 also next to 1; NaN for a NaN, which so shows.
 __device__ __forceinline__ float log2_decay(float a) {
   const double l = log2((double)a);
-  return l > -1.0e4 ? (float)l : -1.0e4f;
+  return l < -1.0e4 ? -1.0e4f : (float)l;
 }
 __device__ __forceinline__ float power(float log2a, int e) { return __builtin_amdgcn_exp2f(log2a * (float)e); }
 

@@ -1,4 +1,5 @@
-"""The sequence operators at the ends of what they take: scales and errors of states far from 1, sizes past 32 bits."""
+"""The sequence operators at the ends of what they take: scales and errors of states far from 1, sizes past 32 bits, parameters that are
+no numbers."""
 import pytest
 import torch
 
@@ -48,3 +49,17 @@ def test_more_key_heads_than_32_bits_count_are_refused():
     state = torch.zeros(1, 2, 8, 8, device=DEV)
     with pytest.raises(ValueError):
         binding.linear_attention_step(q[:, 0], kv[:, 0], kv[:, 0], decay, state)
+
+
+@pytest.mark.parametrize("T", [1, 40, 900])
+def test_a_decay_that_is_no_number_shows(T):
+    """In every form, also where the sequence is cut into segments (900): NaN in its head's results, nothing in the others'."""
+    q, k, v, decay, d_o, _, _, _ = make((1, T, 3, 3, 32, 48, None, False, False), "fp32")
+    decay = torch.tensor([0.9, float("nan"), 1.0], device=DEV)
+    o, state = binding.linear_attention_fwd(q, k, v, decay, 0.3, want_state=True)
+    grads = binding.linear_attention_bwd(q, k, v, decay, d_o, 0.3, want_d_state=True)
+    pool = torch.zeros(1, 3, 32, 48, device=DEV)
+    one = binding.linear_attention_step(q[:, 0], k[:, 0], v[:, 0], decay, pool, 0.3)
+    by_head = [o[0].transpose(0, 1), state[0], *(g[0].transpose(0, 1) for g in grads[:3]), grads[3][0], pool[0], one[0]]
+    for x in by_head:
+        assert x[1].isnan().all() and x[0].isfinite().all() and x[2].isfinite().all()
