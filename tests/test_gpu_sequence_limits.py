@@ -63,3 +63,25 @@ def test_a_decay_that_is_no_number_shows(T):
     by_head = [o[0].transpose(0, 1), state[0], *(g[0].transpose(0, 1) for g in grads[:3]), grads[3][0], pool[0], one[0]]
     for x in by_head:
         assert x[1].isnan().all() and x[0].isfinite().all() and x[2].isfinite().all()
+
+
+@pytest.mark.parametrize("type_", list(ref.TYPES))
+@pytest.mark.parametrize("case", [(2, 777, 4, 2, 32, 32, [777, 20], True, True), (1, 1100, 3, 1, 64, 90, [1099], True, False),
+                                  (2, 640, 2, 2, 128, 96, [3, 640], True, True)], ids=lambda c: str(c[:6]))
+def test_decays_of_zero_in_segments(case, type_):
+    """The state is the last token's alone, and the state before the sequence reaches no further than the first: in sequences cut into
+    segments, one of them shorter than a segment.  Bounds as in test_forward and test_backward."""
+    q, k, v, decay, d_o, n, initial, d_final = make(case, type_)
+    decay = torch.tensor([0.0, 1.0, 0.0, 0.5][:case[2]], device=DEV)
+    shape = binding.LinearShape(*case[:6], list(ref.TYPES).index(type_))
+    assert binding.lib().cnn_linear_attention_fwd_workspace_bytes(shape) > 0
+    arrays, (i64, f64) = in_64(q, k, v, decay, d_o), in_64(initial, d_final)
+    want = ref.linear_attention(*arrays[:4], 0.3, case[6], i64)
+    size = ref.linear_attention(*magnitudes(*arrays[:4]), 0.3, case[6], *magnitudes(i64))
+    got = binding.linear_attention_fwd(q, k, v, decay, 0.3, n, initial, True)
+    want += ref.linear_attention_gradient(*arrays, 0.3, case[6], i64, f64)
+    size += ref.linear_attention_gradient(*magnitudes(*arrays), 0.3, case[6], *magnitudes(i64, f64))
+    got += binding.linear_attention_bwd(q, k, v, decay, d_o, 0.3, n, initial, d_final, True)
+    for name, g, w, m in zip(("o", "state", "d_q", "d_k", "d_v", "d_state"), got, want, size):
+        state = name in ("state", "d_state")
+        ref.near(g, w, m * (steps(case) + (0.0 if state else CUT[type_])), torch.float32 if state else q.dtype, "%s %s" % (name, type_))
