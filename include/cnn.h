@@ -256,8 +256,9 @@ int cnn_logistic_bwd(const float* y, const float* d_y, float* d_x, size_t n, voi
 
 /* ---- Operators on sequences, beside the paper: layers of a classifier that reads its input token by token (an image as
  * 784 pixels, a text as words), trained with the fully connected and logistic calls above. ----------------------------------
- * Data are fp32, bfloat16 or half as `type` says, sums and states fp32 in registers, results rounded to nearest once.  No
- * context, no device state.  Unless said otherwise tensors are contiguous and 16-byte aligned, and an output overlaps no input. */
+ * Data are fp32, bfloat16 or half as `type` says, sums and states fp32 in registers, results rounded to nearest once (what linear
+ * attention multiplies is cut before that, see there).  No context, no device state.  Unless said otherwise tensors are contiguous and
+ * 16-byte aligned, and an output overlaps no input. */
 #define CNN_F32 0
 #define CNN_BF16 1
 #define CNN_F16 2
@@ -295,9 +296,15 @@ int cnn_dropout_bwd(const void* d_y, void* d_x, size_t n, int type, double p, ui
  * [B,H,Dk,Dv].  decay[H]: 0 <= a <= 1, not checked on the device (a NaN shows in all results of its head);
  * constants of the operator, without a gradient.
  * lengths[B] (nullable: all T; below 0 counts as 0, above T as T): tokens past a sequence's length are not read, and their rows of
- * the results are zero.  Inputs up to it must be finite and below 2^127.  An initial or final state may be NULL (zero; not wanted);
- * they may be the same memory.  `workspace` holds states of pieces of the sequences where there are too few heads to fill the GPU,
- * and the gradients of shared heads; the size queries return 0 where none is needed, and for refused shapes. */
+ * the results are zero.  Inputs up to it must be finite and below 2^127: one that is not makes results NaN that the formulas leave
+ * finite or infinite, also of up to 31 tokens before it (in d_k and d_v, after it).  An initial or final state may be NULL (zero; not
+ * wanted); they may be the same memory.  `workspace` holds states of pieces of the sequences where there are too few heads to fill the GPU,
+ * and the gradients of shared heads; the size queries return 0 where none is needed, and for refused shapes.
+ * Precision: sums and states are fp32, but over whole sequences they are fed to bfloat16 matrix products as sums of bfloat16 numbers.
+ * Of floats three are kept, which is fp32.  For bfloat16 and half the state where it meets q, the scores q k and, between the pieces of
+ * a sequence that is cut, the decayed v keep two, sixteen bits: before it is rounded to its type a result is off by up to 2^-16
+ * (bfloat16) or 2^-15 (half) of the same sums over magnitudes, with an error some sixteen times that of fp32 operands.  It shows where
+ * large terms cancel.  States that are results keep three, whatever the type; one token at a time everything is fp32. */
 typedef struct {
   int B, T, H, Hk, Dk, Dv, type;
 } cnn_linear_shape;
