@@ -11,8 +11,8 @@
 // (Adding into the table with atomics would be shorter, but its results change from run to run and bfloat16 has none.)
 //
 // Bounds: the lookup is memory (131071 rows of 2 KB: 55 us).  The gradient of 65521 words over 32003 rows of 1000 (bfloat16, 196 MB that
-// have to be moved, 38 us at a copy's rate) takes 75 us: the sums 27 (4.8 TB/s), the sort 30 (of four dependent kernels, with the table
-// cleared on the side), the join 7.  Of 78400 pixels over 256 rows of 64 floats: 29 us, all of it round trips of four dependent kernels.
+// have to be moved, 38 us at a copy's rate) takes 70 to 74 us: the sums 28 (4.7 TB/s), the sort 27 (of four dependent kernels, with the table
+// cleared on the side), the join 7.  Of 78400 pixels over 256 rows of 64 floats: 28 us, all of it round trips of four dependent kernels.
 #include <type_traits>
 
 #include "cnn_common.h"
@@ -76,7 +76,7 @@ struct Entry {  // of the sorted list
 
 constexpr int RADIX = 256;
 constexpr int SORT_THREADS = 256, SORT_WAVES = SORT_THREADS / 64;
-constexpr int SORT_EACH = 4;        // positions that a lane holds at once, so that their loads are under way together (8: 64 us for 60 below)
+constexpr int SORT_EACH = 4;        // positions that a lane holds at once, so that their loads are under way together (8: 74.7 us for the 70.2 of the text above, inputs in turn)
 constexpr int SORT_CHUNK = SORT_THREADS * SORT_EACH;  // positions to a workgroup, at least
 constexpr int SORT_GROUPS = 256;    // workgroups of a pass, at most: each adds up the counts of those before it
 constexpr int SMALL_THREADS = 1024, SMALL_WAVES = SMALL_THREADS / 64, SMALL_EACH = 4;

@@ -23,11 +23,12 @@
 // lost, of results that are rounded to 2^-9 or 2^-12), three for floats; a^{C-1-s} v_s into three, so that the state is exact to fp32
 // sums for every type, or two in the second pass over segments, whose own state is no result.
 //
-// Measured (MI355X; in brackets the bytes that have to be moved at a copy's 5.15 TB/s): 8192 tokens of 2 x 16 heads of 128 (bf16) 120 us
-// (53): 33 for the first pass, 14 for the scan over 16 segments, 71 for the second pass, in which a SIMD's two waves issue vector
-// instructions, most of them cutting and decaying the state, 60 % of the time and matrix instructions 33 %.  100 x 2 heads of 784 tokens,
-// 32 wide (fp32): 33 us forward on uneven lengths (10), 72 us backward (27), bound by the cutting of floats, some 700 vector instructions
-// for 32 tokens.  3 x 12 heads of 2047 tokens, 64 and 96 wide (fp16), backward: 107 us (10), of six dependent launches.
+// Measured (MI355X; in brackets the bytes that have to be moved at a copy's 5.15 TB/s): 8192 tokens of 2 x 16 heads of 128 (bf16) 118 us
+// (53): 32 for the first pass, 14 for the scan over 16 segments, 72 for the second pass, in which a SIMD's two waves issue vector
+// instructions, most of them cutting and decaying the state, 60 % of the time and its matrix unit is busy 35 %.  100 x 2 heads of 784 tokens,
+// 32 wide (fp32): 33 us forward on uneven lengths (10), 72 us backward (27), bound by the cutting of floats, some 840 vector instructions
+// for 32 tokens and a role, with what stands around the loop.  3 x 12 heads of 2047 tokens, 64 and 96 wide (fp16), backward: 105 us (10),
+// of six dependent launches.
 #pragma once
 
 #include <type_traits>
@@ -365,6 +366,8 @@ __device__ __forceinline__ uint32_t state_index(int row, int column, int tiles) 
 }
 
 // Waves to a SIMD, which bound the registers of a kernel.  (Three would spill: the pixel sequences' gradients took 105 us, not 71.)
+// Two make floats of 96 and 128 columns of q and k spill 3 to 21 registers where two or three waves share v, and 185 where rows of 128 are
+// not made of packs: 8 x 8 heads of 1024 tokens, 128 x 64, forward 74 us (20), of 126 x 62 116 us.  Not changed, not compared with one.
 constexpr int waves_wanted(int DKP) { return DKP <= 128 ? 2 : 1; }
 
 // STATE_ONLY: the first pass.  EXACT: the state is a result, not only what the segment's own tokens see.

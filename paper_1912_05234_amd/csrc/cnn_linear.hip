@@ -103,7 +103,7 @@ constexpr int STEP_THREADS = 256, STEP_COLUMNS = 32;
 
 // A workgroup takes 32 columns of one state: the whole of DK, so that nothing has to be joined outside it.  Every thread
 // updates VN columns of one row in so many, and keeps their products with q; these are added over the rows at the end.
-// Memory bounds it: 256 rows of 16 states of 128 x 128 (537 MB read and written) take 100 to 109 us, 5.4 to 4.9 TB/s.
+// Memory bounds it: 256 rows of 16 states of 128 x 128 (537 MB read and written) take 96 us, after other work 102, 5.6 to 5.3 TB/s.
 template <class T, int VN, bool PAST_CACHES>
 __global__ __launch_bounds__(STEP_THREADS) void step_kernel(StepArgs a) {
   constexpr int LANES = STEP_COLUMNS / VN, ROWS = STEP_THREADS / LANES, AHEAD = 4;
@@ -225,7 +225,8 @@ double cost_of(const cnn_linear_shape& s, const Plan& p, int roles, int64_t leng
 Plan plan_of(const cnn_linear_shape& s, int roles) {
   Plan p{};
   const int64_t units = (int64_t)s.B * s.H;
-  // No segments whose state, written and read twice, is more to move than its tokens.
+  // No segments whose state, written and read twice, is more to move than its tokens, both counted without the columns that pad them.
+  // (So widths far from the padded ones may have more: Dk = 158, Dv = 6 holds states of 256 x 128, seventeen times the tokens' bytes.)
   const int64_t least = 16 * (int64_t)s.Dk * s.Dv / (2 * (s.Dk + s.Dv) * (int64_t)type_bytes(s.type));
   const int64_t most = s.T / (least > 2 * C ? least : 2 * C);
   double best = 0.0;
@@ -389,8 +390,9 @@ int cnn_linear_attention_step(const cnn_linear_shape* s, const cnn_heads* q, con
   const int share = s->H / s->Hk, blocks = (s->Dv + STEP_COLUMNS - 1) / STEP_COLUMNS;
   const StepArgs a{operand_of(q, 1), operand_of(k, share), operand_of(v, share), decay, state, slots, o, pool, s->H, s->Dk, s->Dv, blocks, scale};
   const unsigned grid = (unsigned)((int64_t)s->B * s->H * blocks);
-  // States that do not fit the last cache of 256 MB go past it.  268 MB of them 98 and 125 us (again and again, and after other work),
-  // past the caches 100 and 109; 402 MB 153 and 167, 143 and 151; but 134 MB 42 and 71, 51 and 59.
+  // States that do not fit the last cache (256 MiB) go past it.  Again and again, and after other work that filled it: 252 MB of them 78 and
+  // 114 us, past the caches 91 and 97; 268 MB 96 and 118, 96 and 102; 302 MB 113 and 130, 108 and 113; 403 MB 160 and 167, 143 and 149;
+  // and 134 MB 44 and 67, 50 and 56.  (What a server's other layers leave of smaller states is not known here.)
   const bool past_caches = (int64_t)s->B * s->H * s->Dk * s->Dv * 4 >= (int64_t)256 << 20;
   return with_type(s->type, [&](auto t) {
     using T = decltype(t);
