@@ -41,3 +41,9 @@ def test_gradients_under_the_masks_of_a_step(p, step):
     # and the bound tells masks apart: those of the next step do not pass
     other = plain(net, tokens, target, p, step + 1)[1]
     assert all((g.double().cpu() - w).abs().max() > 2.0 ** -12 * w.abs().max() for g, w in zip(grads[:4], other))
+
+
+def test_training_reaches_what_the_documentation_says():
+    """180 steps of 100 images: 99.8 % of a thousand held-out images as measured, 98 % at the least."""
+    records = pixels.run(inputs.make_digits(6000, 1), inputs.make_digits(1000, 2), 3, report=lambda line: None)
+    assert records[-1]["test_accuracy"] >= 0.98
