@@ -301,8 +301,8 @@ int cnn_dropout_bwd(const void* d_y, void* d_x, size_t n, int type, double p, ui
  * wanted); they may be the same memory.  `workspace` holds states of pieces of the sequences where there are too few heads to fill the GPU,
  * and the gradients of shared heads; the size queries return 0 where none is needed, and for refused shapes.
  * Precision: sums and states are fp32, but over whole sequences they are fed to bfloat16 matrix products as sums of bfloat16 numbers.
- * Of floats three are kept, which is fp32.  For bfloat16 and half the state where it meets q, the scores q k and, between the pieces of
- * a sequence that is cut, the decayed v keep two, sixteen bits: before it is rounded to its type a result is off by up to 2^-16
+ * Of floats three are kept, which is fp32.  For bfloat16 and half the state where it meets q, the scores q k and, in sequences cut
+ * into pieces, the decayed v keep two, sixteen bits: before it is rounded to its type a result is off by up to 2^-16
  * (bfloat16) or 2^-15 (half) of the same sums over magnitudes, with an error some sixteen times that of fp32 operands.  It shows where
  * large terms cancel.  States that are results keep three, whatever the type; one token at a time everything is fp32. */
 typedef struct {
