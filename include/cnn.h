@@ -333,6 +333,60 @@ int cnn_linear_attention_step(const cnn_linear_shape* shape, const cnn_heads* q,
                               const float* decay, float scale, float* state, int64_t pool, const int32_t* slots, void* o,
                               void* hip_stream);
 
+/* Norms around a block, for rows of groups * width elements: n = v / sqrt(mean(v^2) + eps) for each group of `width` consecutive ones, times
+ * weight[groups * width] (fp32).  Two element types: `type` of what goes into and comes out of the block, `stream_type` (the same, or
+ * CNN_F32) of the residual stream.  Inputs are given with the distance of their rows, in elements, not negative, and need only be aligned to
+ * their element; results are contiguous.  1 <= rows < 2^31, 1 <= width <= 16384, groups * width <= 2^20, 0 < eps.  Elements whose square's
+ * sum over a group is not below 2^128 make the group's results meaningless; a NaN or an infinity stays in its group (and, backward, in
+ * d_weight).  Weight gradients are fp32 sums in an order that the shape fixes. */
+typedef struct {
+  int64_t rows;
+  int groups, width, type, stream_type;
+  float scale, eps;
+} cnn_norm_shape;
+typedef struct {
+  const void* data; /* element j of row n at n * row + j */
+  int64_t row;
+} cnn_rows;
+/* Before a block: r = residual + scale * x, y = n w with n of r (before r is rounded to stream_type).  Without a residual (NULL) r is x: scale
+ * must be 1, the types equal and r NULL.  With one r may be NULL (not wanted). */
+int cnn_add_norm_fwd(const cnn_norm_shape* shape, const cnn_rows* x, const cnn_rows* residual, const float* weight, void* y, void* r,
+                     void* hip_stream);
+/* For the error d_y of y and (nullable) d_r of r, and the r of the forward call (x where it had no residual): d_residual = d_r + the
+ * error through the norm, d_x = scale * d_residual (nullable: not wanted, as where it would be the same), d_weight = sum over rows of d_y n. */
+size_t cnn_norm_bwd_workspace_bytes(const cnn_norm_shape* shape);
+int cnn_add_norm_bwd(const cnn_norm_shape* shape, const cnn_rows* d_y, const cnn_rows* r, const cnn_rows* d_r, const float* weight, void* d_x,
+                     void* d_residual, float* d_weight, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Behind a block: y = residual + scale * n w silu(gate) with n of x and silu(z) = z / (1 + exp(-z)); gate (of `type`) and residual (of stream_type) may be
+ * NULL (a factor of 1; 0).  y is of stream_type. */
+int cnn_norm_gate_fwd(const cnn_norm_shape* shape, const cnn_rows* x, const cnn_rows* gate, const cnn_rows* residual, const float* weight, void* y,
+                      void* hip_stream);
+/* d_x, d_gate (NULL where the gate is) and d_weight for the error d_y (of stream_type) of y.  (The residual's gradient is d_y itself.) */
+int cnn_norm_gate_bwd(const cnn_norm_shape* shape, const cnn_rows* d_y, const cnn_rows* x, const cnn_rows* gate, const float* weight, void* d_x,
+                      void* d_gate, float* d_weight, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Log probabilities of rows of logits l[vocab]: ln p_v = scale * l_v - ln sum exp(scale * l), scale > 0 (an inverse temperature).
+ *   log_probs[rows,given]   ln p of the tokens[rows,given] (int32, or int64 with wide_tokens != 0); 0 for a token outside 0 .. vocab-1 (padding)
+ *   entropy[rows]           - sum p ln p (nullable)
+ *   top_tokens, top_log_probs[rows,top]   the `top` largest logits in descending order, equal ones (0 and -0 among them) in the order of their tokens
+ *   stats[rows,3]           what the backward call needs: max l, ln sum exp(scale * (l - max)), the entropy (nullable)
+ * Results are fp32.  A logit of -inf is an impossible token: p = 0.  A row of nothing else has log_probs and top_log_probs of -inf and an entropy of 0,
+ * and its gradient is zero.  A NaN or +inf makes its row's results NaN, except that top_tokens are tokens of the row and padding's log_probs are 0.
+ * 1 <= rows < 2^31, 1 <= vocab <= 2^24, 1 <= given <= 256, 0 <= top <= min(64, vocab).  Logits as a cnn_rows of `type`. */
+typedef struct {
+  int64_t rows, vocab;
+  int given, top, type, wide_tokens;
+  float scale;
+} cnn_log_probs_shape;
+size_t cnn_log_probs_fwd_workspace_bytes(const cnn_log_probs_shape* shape);
+int cnn_log_probs_fwd(const cnn_log_probs_shape* shape, const cnn_rows* logits, const void* tokens, float* log_probs, float* entropy, float* stats,
+                      float* top_log_probs, int32_t* top_tokens, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* d_logits[rows,vocab] (contiguous, of `type`) for the errors d_log_probs[rows,given] and (nullable) d_entropy[rows]: scale * (sum of the errors of the
+ * positions whose token v is - p_v * sum of all errors - d_entropy p_v (ln p_v + entropy)).  Padding's errors are not read.  A token that a row is given
+ * several times gets the sum of its errors, in their order.  (`top` is not used.) */
+int cnn_log_probs_bwd(const cnn_log_probs_shape* shape, const cnn_rows* logits, const void* tokens, const float* stats, const float* d_log_probs,
+                      const float* d_entropy, void* d_logits, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

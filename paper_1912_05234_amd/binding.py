@@ -88,6 +88,34 @@ SIGNATURES.update({
     "cnn_linear_attention_step": (_i, [_shape] + [_heads] * 3 + [_vp, _f, _vp, _i64, _vp, _vp, _vp]),
 })
 
+
+class NormShape(ctypes.Structure):
+    """cnn_norm_shape"""
+    _fields_ = [("rows", _i64)] + [(name, _i) for name in ("groups", "width", "type", "stream_type")] + [("scale", _f), ("eps", _f)]
+
+
+class LogProbsShape(ctypes.Structure):
+    """cnn_log_probs_shape"""
+    _fields_ = [("rows", _i64), ("vocab", _i64)] + [(name, _i) for name in ("given", "top", "type", "wide_tokens")] + [("scale", _f)]
+
+
+class Rows(ctypes.Structure):
+    """cnn_rows"""
+    _fields_ = [("data", _vp), ("row", _i64)]
+
+
+_norm, _logp, _rows = ctypes.POINTER(NormShape), ctypes.POINTER(LogProbsShape), ctypes.POINTER(Rows)
+SIGNATURES.update({
+    "cnn_add_norm_fwd": (_i, [_norm] + [_rows] * 2 + [_vp] * 4),
+    "cnn_norm_bwd_workspace_bytes": (_sz, [_norm]),
+    "cnn_add_norm_bwd": (_i, [_norm] + [_rows] * 3 + [_vp] * 5 + [_sz, _vp]),
+    "cnn_norm_gate_fwd": (_i, [_norm] + [_rows] * 3 + [_vp] * 3),
+    "cnn_norm_gate_bwd": (_i, [_norm] + [_rows] * 3 + [_vp] * 5 + [_sz, _vp]),
+    "cnn_log_probs_fwd_workspace_bytes": (_sz, [_logp]),
+    "cnn_log_probs_fwd": (_i, [_logp, _rows] + [_vp] * 7 + [_sz, _vp]),
+    "cnn_log_probs_bwd": (_i, [_logp, _rows] + [_vp] * 6),
+})
+
 _lib = None
 _calls = None
 
@@ -337,3 +365,42 @@ def linear_attention_step(q, k, v, decay, state, scale=1.0, slots=None):
     """o[B, H, Dv] of one token of every sequence, q[B, H, Dk], k[B, Hk, Dk], v[B, Hk, Dv]; state[pool, H, Dk, Dv] fp32 is updated in
     place, row b using state slots[b] (int32; None: state b).  A slot outside the pool: a row without a sequence, its o is zero."""
     return (_calls or _native()).linear_attention_step(q, k, v, decay, scale, state, slots)
+
+
+# ---- around a block: norms -------------------------------------------------------------
+def add_norm_fwd(x, weight, residual=None, scale=1.0, eps=1e-6, groups=1):
+    """(y, r): r = residual + scale * x, and y = r / sqrt(mean(r^2) + eps) * weight, the mean over each of `groups` equal pieces of the last
+    dimension.  weight is fp32, residual of x's type or fp32, r of the residual's.  Without a residual r is x itself (and scale 1)."""
+    return (_calls or _native()).add_norm_fwd(x, weight, residual, scale, eps, groups)
+
+
+def add_norm_bwd(d_y, r, weight, d_r=None, scale=1.0, eps=1e-6, groups=1):
+    """(d_x, d_residual, d_weight) of the call above, from the r that it returned.  Where scale is 1 and the types are the same, d_x and
+    d_residual are one tensor."""
+    (d_x, d_residual), d_weight = (_calls or _native()).add_norm_bwd(d_y, r, weight, d_r, scale, eps, groups)
+    return d_x, d_residual, d_weight
+
+
+def norm_gate_fwd(x, weight, gate=None, residual=None, scale=1.0, eps=1e-6, groups=1):
+    """residual + scale * x / sqrt(mean(x^2) + eps) * weight * silu(gate), of the residual's type if there is one (x's or fp32)."""
+    return (_calls or _native()).norm_gate_fwd(x, weight, gate, residual, scale, eps, groups)
+
+
+def norm_gate_bwd(d_y, x, weight, gate=None, scale=1.0, eps=1e-6, groups=1):
+    """(d_x, d_gate or None, d_weight); the residual's gradient is d_y itself, whose type is the forward result's."""
+    (d_x, d_gate), d_weight = (_calls or _native()).norm_gate_bwd(d_y, x, weight, gate, scale, eps, groups)
+    return d_x, d_gate, d_weight
+
+
+# ---- log probabilities -----------------------------------------------------------------
+def log_probs_fwd(logits, tokens, scale=1.0, top=0):
+    """(log_probs, entropy, stats, top_log_probs or None, top_tokens or None) of logits[..., V] times scale: the log probabilities of the given
+    tokens (int32 or int64, one for each row, or [..., M] for M of them; 0 where a token is not in 0..V-1), each row's entropy, what the backward call needs, and
+    the `top` most probable tokens (int32)."""
+    (log_probs, entropy), (stats, (top_log_probs, top_tokens)) = (_calls or _native()).log_probs_fwd(logits, tokens, scale, top)
+    return log_probs, entropy, stats, top_log_probs, top_tokens
+
+
+def log_probs_bwd(logits, tokens, stats, d_log_probs, d_entropy=None, scale=1.0):
+    """The logits' gradient for the errors of log_probs and entropy (fp32)."""
+    return (_calls or _native()).log_probs_bwd(logits, tokens, stats, d_log_probs, d_entropy, scale)

@@ -1,0 +1,482 @@
+// Log probabilities of given tokens, entropy and the most probable tokens of rows of logits, and the logits' gradient.
+//
+//   z = scale l,  m = max z,  ln p_v = z_v - m - ln sum exp(z - m),  H = - sum p ln p
+//   d_l_v = scale ( sum_j g_j [v = token_j] - p_v sum_j g_j - d_H p_v (ln p_v + H) )
+//
+// Memory bounds both: a pass reads the logits once.  A workgroup holds its part of a row in registers, at most 32 elements to a lane,
+// so the maximum, the two sums (of e = exp(z - m) and of e (z - m), from which the entropy comes without cancellation: both of its
+// terms have one sign) and the choice of the largest elements all work on them.  Rows longer than 32768 are cut into parts, more
+// of them where rows are few, which a second kernel joins.
+//
+// The k largest: the k-th largest of the maxima of 64 (128) groups of lanes is a lower bound that few elements reach (24 are expected
+// for k = 20 of 64 groups); those go into a list in LDS, and each finds its place by counting the larger ones.  Keys are unique,
+// the value's bits in order above the complement of the index, so equal values keep the order of their tokens.  Where the list
+// overflows (rows of equal logits) the workgroup takes the largest key k times instead.
+#include "cnn_common.h"
+#include "cnn_types.h"
+
+namespace cnn {
+namespace logp {
+namespace {
+
+constexpr int MOST_GIVEN = 256, MOST_TOP = 64;
+constexpr int64_t MOST_VOCAB = 1 << 24;
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+
+struct Sums {  // of e and of e (z - m) in powers of two, relative to the maximum m of the logits
+  float m, s, t;
+};
+
+struct Args {
+  const void* logits;
+  int64_t row, rows, vocab, part_length;
+  const void* tokens;
+  float *log_probs, *entropy, *stats, *top_log_probs;
+  int32_t* top_tokens;
+  Sums* sums;      // [rows][parts]
+  uint64_t* keys;  // [rows][parts][top]
+  int parts, given, top, wide;
+  float scale;
+};
+
+__device__ __forceinline__ float minus_infinity() { return -__builtin_inff(); }
+
+// e d for e = 2^d, which is 0 for d = -inf.  (A NaN of d is in e.)
+__device__ __forceinline__ float weighted(float e, float d) { return e * fmaxf(d, -1e30f); }
+
+// Adds another piece's sums: the maximum of the two, sums rescaled.  Pieces without a possible token have m = -inf, s = t = 0.
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {  // c = scale log2(e)
+  const float m = fmaxf(a.m, b.m), ref = m == minus_infinity() ? 0.0f : m;
+  const float da = (a.m - ref) * c, db = (b.m - ref) * c;
+  const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
+  return {m, a.s * ea + b.s * eb, ea * (a.t + weighted(a.s, da)) + eb * (b.t + weighted(b.s, db))};
+}
+
+__device__ __forceinline__ uint64_t key_of(float x, int64_t index) {
+  const uint32_t bits = __float_as_uint(x + 0.0f);  // (-0 is 0)
+  uint32_t order = bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
+  if (x != x) order = 0xfffffffeu;  // above infinity, and no key is all ones
+  return (uint64_t)order << 32 | (uint32_t)~(uint32_t)index;
+}
+__device__ __forceinline__ int64_t index_of(uint64_t key) { return (int64_t)(uint32_t)~(uint32_t)key; }
+
+__device__ __forceinline__ int64_t token_of(const void* tokens, int wide, int64_t i) {
+  return wide ? static_cast<const int64_t*>(tokens)[i] : (int64_t) static_cast<const int32_t*>(tokens)[i];
+}
+
+// The row's results from its sums; lanes of one workgroup share the given tokens.
+template <class T>
+__device__ __forceinline__ float finish_row(const Args& a, const T* logits, int64_t n, const Sums& r) {
+  const bool none = r.m == minus_infinity() && r.s == 0.0f;  // (a NaN would be in s)
+  const float log_sum = none ? 0.0f : logf(r.s), base = none ? 0.0f : r.m;
+  if (threadIdx.x == 0) {
+    // (a row with an infinite or NaN logit has s = NaN)
+    const float h = none ? 0.0f : log_sum - r.t * LN2 / r.s;
+    if (a.entropy) a.entropy[n] = h;
+    if (a.stats) a.stats[n * 3] = r.m, a.stats[n * 3 + 1] = log_sum, a.stats[n * 3 + 2] = h;
+  }
+  for (int j = threadIdx.x; j < a.given; j += blockDim.x) {
+    const int64_t token = token_of(a.tokens, a.wide, n * a.given + j);
+    float lp = 0.0f;
+    if (token >= 0 && token < a.vocab) lp = ((float)logits[token] - base) * a.scale - log_sum;
+    a.log_probs[n * a.given + j] = lp;
+  }
+  return log_sum;
+}
+
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint64_t o = __shfl_xor(v, d);
+    v = o > v ? o : v;
+  }
+  return v;
+}
+
+template <int THREADS>
+struct TopShared {
+  static constexpr int LIST = THREADS > 64 ? 1024 : 256;
+  uint64_t list[LIST];
+  uint64_t waves[2][THREADS / 64];
+  int count;
+};
+
+// Calls put(rank, key) for the `top` largest of the keys that each(fn) hands out (a thread its own), key 0 where there are fewer; `likely`
+// says which keys may be among them.  The whole workgroup calls it; keys are unique and not 0.
+template <int THREADS, class EACH, class LIKELY, class PUT>
+__device__ void top_keys(TopShared<THREADS>& sh, int top, EACH each, LIKELY likely, PUT put) {
+  if (threadIdx.x == 0) sh.count = 0;
+  __syncthreads();
+  each([&](uint64_t key) {
+    if (!likely(key)) return;
+    const int at = atomicAdd(&sh.count, 1);  // (their order in the list does not matter)
+    if (at < TopShared<THREADS>::LIST) sh.list[at] = key;
+  });
+  __syncthreads();
+  const int count = sh.count;
+  if (count <= TopShared<THREADS>::LIST) {
+    for (int i = threadIdx.x; i < count; i += THREADS) {
+      const uint64_t key = sh.list[i];
+      int rank = 0;
+      for (int j = 0; j < count; ++j) rank += sh.list[j] > key;
+      if (rank < top) put(rank, key);
+    }
+    for (int i = count + (int)threadIdx.x; i < top; i += THREADS) put(i, (uint64_t)0);
+    return;
+  }
+  uint64_t last = ~(uint64_t)0;
+  for (int r = 0; r < top; ++r) {
+    uint64_t best = 0;
+    each([&](uint64_t key) {
+      if (key < last && key > best) best = key;
+    });
+    best = wave_max(best);
+    if (threadIdx.x % 64 == 0) sh.waves[r & 1][threadIdx.x / 64] = best;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) best = sh.waves[r & 1][w] > best ? sh.waves[r & 1][w] : best;
+    if (threadIdx.x == 0) put(r, best);
+    last = best;
+  }
+}
+
+// A lower bound of the k-th largest (k <= 64 * PER) of 64 * PER values, PER to a lane, the same in every lane of a wave: the sixteen high bits of its
+// key, found bit by bit.  NaN, to which nothing compares as smaller, where that is -inf.
+template <int PER>
+__device__ __forceinline__ float kth_largest(const float (&v)[PER], int k) {
+  uint32_t key[PER], found = 0;
+#pragma unroll
+  for (int p = 0; p < PER; ++p) key[p] = (uint32_t)(key_of(v[p], 0) >> 32);
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t now = found | 1u << bit;
+    int reach = 0;
+#pragma unroll
+    for (int p = 0; p < PER; ++p) reach += __popcll(__ballot(key[p] >= now));
+    if (reach >= k) found = now;
+  }
+  return __uint_as_float(found & 0x80000000u ? found ^ 0x80000000u : ~found);
+}
+
+template <class T, int THREADS, int EACH>
+__global__ __launch_bounds__(THREADS) void logp_part_kernel(Args a) {
+  constexpr int V = sizeof(T) == 2 ? 8 : 4, PACKS = EACH / V, WAVES = THREADS / 64;
+  __shared__ Sums sums[WAVES];
+  __shared__ float groups[128];
+  __shared__ TopShared<THREADS> sh;
+  const int64_t n = workgroup() / a.parts, begin = workgroup() % a.parts * a.part_length;
+  if (n >= a.rows) return;
+  const int64_t left = a.vocab - begin, length = left < a.part_length ? left : a.part_length;  // (every part has an element)
+  const T* logits = static_cast<const T*>(a.logits) + n * a.row;
+  const T* part = logits + begin;
+  float x[PACKS][V];
+#pragma unroll
+  for (int p = 0; p < PACKS; ++p) {
+    const int at = (p * THREADS + (int)threadIdx.x) * V;
+    const int count = (int)length - at;
+    get_loose(x[p], part + at, count);
+    if (count < V)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j >= count) x[p][j] = minus_infinity();
+  }
+  float mine = minus_infinity();
+#pragma unroll
+  for (int p = 0; p < PACKS; ++p)
+#pragma unroll
+    for (int j = 0; j < V; ++j) mine = fmaxf(mine, x[p][j]);
+  Sums r{mine, 0.0f, 0.0f};
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) r.m = fmaxf(r.m, __shfl_xor(r.m, d));
+  const float c = a.scale * LOG2E, ref = r.m == minus_infinity() ? 0.0f : r.m;
+#pragma unroll
+  for (int p = 0; p < PACKS; ++p)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float d = (x[p][j] - ref) * c, e = __builtin_amdgcn_exp2f(d);
+      r.s += e, r.t += weighted(e, d);
+    }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) r.s += __shfl_xor(r.s, d), r.t += __shfl_xor(r.t, d);
+  if constexpr (WAVES > 1) {
+    if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = r;
+    __syncthreads();
+    r = sums[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) r = join(r, sums[w], c);
+  }
+  float log_sum = 0.0f;
+  if (a.parts == 1) log_sum = finish_row(a, logits, n, r);
+  else if (threadIdx.x == 0) a.sums[workgroup()] = r;
+  if (!a.top) return;
+  float least;  // no fewer than `top` elements reach it
+  if constexpr (WAVES == 1) {
+    const float one[1] = {mine};
+    least = kth_largest(one, a.top);
+  } else {
+    constexpr int LANES = THREADS / 128;  // of a group
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) mine = fmaxf(mine, __shfl_xor(mine, d));
+    if (threadIdx.x % LANES == 0) groups[threadIdx.x / LANES] = mine;
+    __syncthreads();
+    const float two[2] = {groups[threadIdx.x % 64], groups[threadIdx.x % 64 + 64]};
+    least = kth_largest(two, a.top);
+  }
+  const auto each = [&](auto fn) {
+#pragma unroll
+    for (int p = 0; p < PACKS; ++p)
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int at = (p * THREADS + (int)threadIdx.x) * V + j;
+        if (!(x[p][j] < least) && at < length) fn(key_of(x[p][j], begin + at));
+      }
+  };
+  const float base = r.m == minus_infinity() ? 0.0f : r.m;
+  top_keys<THREADS>(sh, a.top, each, [](uint64_t) { return true; }, [&](int rank, uint64_t key) {
+    if (a.parts > 1) {
+      a.keys[workgroup() * a.top + rank] = key;
+    } else {
+      const int64_t v = index_of(key);
+      a.top_tokens[n * a.top + rank] = (int32_t)v;
+      a.top_log_probs[n * a.top + rank] = ((float)logits[v] - base) * a.scale - log_sum;
+    }
+  });
+}
+
+// The parts of a row joined.
+constexpr int JOIN_THREADS = 256;
+template <class T>
+__global__ __launch_bounds__(JOIN_THREADS) void logp_join_kernel(Args a) {
+  __shared__ Sums sums[JOIN_THREADS / 64];
+  __shared__ TopShared<JOIN_THREADS> sh;
+  const int64_t n = workgroup();
+  if (n >= a.rows) return;
+  const T* logits = static_cast<const T*>(a.logits) + n * a.row;
+  const float c = a.scale * LOG2E;
+  Sums r{minus_infinity(), 0.0f, 0.0f};
+  uint64_t least = 0;  // a part's last key: `top` others are no smaller
+  const uint64_t* keys = a.keys + n * a.parts * a.top;
+  for (int p = threadIdx.x; p < a.parts; p += JOIN_THREADS) {
+    r = join(r, a.sums[n * a.parts + p], c);
+    if (a.top) {
+      const uint64_t last = keys[(int64_t)p * a.top + a.top - 1];
+      least = last > least ? last : least;
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) r = join(r, Sums{__shfl_xor(r.m, d), __shfl_xor(r.s, d), __shfl_xor(r.t, d)}, c);
+  least = wave_max(least);
+  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = r, sh.waves[0][threadIdx.x / 64] = least;
+  __syncthreads();
+  r = sums[0];
+#pragma unroll
+  for (int w = 1; w < JOIN_THREADS / 64; ++w) r = join(r, sums[w], c);
+#pragma unroll
+  for (int w = 0; w < JOIN_THREADS / 64; ++w) least = sh.waves[0][w] > least ? sh.waves[0][w] : least;
+  const float log_sum = finish_row(a, logits, n, r), base = r.m == minus_infinity() ? 0.0f : r.m;
+  if (!a.top) return;
+  const auto each = [&](auto fn) {
+    for (int i = threadIdx.x; i < a.parts * a.top; i += JOIN_THREADS) {
+      const uint64_t key = keys[i];
+      if (key && key >= least) fn(key);
+    }
+  };
+  __syncthreads();  // (top_keys writes sh.waves again)
+  top_keys<JOIN_THREADS>(sh, a.top, each, [](uint64_t) { return true; }, [&](int rank, uint64_t key) {
+    const int64_t v = index_of(key);
+    a.top_tokens[n * a.top + rank] = (int32_t)v;
+    a.top_log_probs[n * a.top + rank] = ((float)logits[v] - base) * a.scale - log_sum;
+  });
+}
+
+// ---- backward ----------------------------------------------------------------------------------------------------------
+struct BackArgs {
+  const void* logits;
+  int64_t row, rows, vocab;
+  const void* tokens;
+  const float *stats, *d_log_probs, *d_entropy;
+  void* d_logits;
+  int tiles, given, wide;
+  float scale;
+};
+
+// One tile of a row: THREADS lanes with PACKS packs each, all on their way at once.
+template <class T, int THREADS, int PACKS>
+__global__ __launch_bounds__(THREADS) void logp_backward_kernel(BackArgs a) {
+  constexpr int V = sizeof(T) == 2 ? 8 : 4;
+  __shared__ int64_t tokens[MOST_GIVEN];
+  __shared__ float errors[MOST_GIVEN];
+  const int64_t n = workgroup() / a.tiles, begin = workgroup() % a.tiles * (THREADS * PACKS * V);
+  if (n >= a.rows) return;
+  const T* logits = static_cast<const T*>(a.logits) + n * a.row;
+  T* d_logits = static_cast<T*>(a.d_logits) + n * a.vocab;
+  const int64_t left = a.vocab - begin;
+  float x[PACKS][V];
+#pragma unroll
+  for (int p = 0; p < PACKS; ++p) {
+    const int at = (p * THREADS + (int)threadIdx.x) * V;
+    get_loose(x[p], logits + begin + at, (int)left - at);
+  }
+  const float m = a.stats[n * 3], log_sum = a.stats[n * 3 + 1], h = a.stats[n * 3 + 2];
+  const float d_h = a.d_entropy ? a.d_entropy[n] : 0.0f;
+  const bool none = m == minus_infinity() && log_sum == 0.0f;
+  const float base = none ? 0.0f : m;
+  float total = 0.0f;  // of the given tokens' errors; the same in every wave
+  int64_t token = -1;  // of the only one
+  float error = 0.0f;
+  if (a.given == 1) {
+    token = token_of(a.tokens, a.wide, n);
+    if (token >= 0 && token < a.vocab && !none) total = error = a.d_log_probs[n];
+    else token = -1;
+  } else {
+    for (int j = threadIdx.x % 64; j < a.given; j += 64) {
+      const int64_t t = token_of(a.tokens, a.wide, n * a.given + j);
+      const bool known = t >= 0 && t < a.vocab && !none;
+      const float g = known ? a.d_log_probs[n * a.given + j] : 0.0f;
+      total += g;
+      if (threadIdx.x < 64) tokens[j] = known ? t : -1, errors[j] = g;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
+  }
+  const float by = a.scale, c = by * LOG2E, log2_sum = log_sum * LOG2E;
+  const auto gradient = [&](float l, float g) {
+    const float z = (l - base) * c - log2_sum, p = __builtin_amdgcn_exp2f(z);
+    float d = g - p * total;
+    if (a.d_entropy) d -= d_h * weighted(p, z * LN2 + h);
+    return none ? 0.0f : by * d;
+  };
+#pragma unroll
+  for (int p = 0; p < PACKS; ++p) {
+    const int at = (p * THREADS + (int)threadIdx.x) * V;
+    const int64_t first = begin + at;
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[p][j] = gradient(x[p][j], first + j == token ? error : 0.0f);
+    put_loose(d_logits + first, x[p], (int)left - at);
+  }
+  if (a.given == 1) return;
+  __syncthreads();  // the rows' stores are done before a given token's element is written again
+  for (int j = threadIdx.x; j < a.given; j += THREADS) {
+    const int64_t t = tokens[j];
+    if (t < begin || t >= begin + THREADS * PACKS * V) continue;
+    bool before = false;
+    float g = 0.0f;
+    for (int i = 0; i < a.given; ++i) {
+      if (tokens[i] != t) continue;
+      before |= i < j;
+      g += errors[i];
+    }
+    if (!before) d_logits[t] = (T)gradient((float)logits[t], g);
+  }
+}
+
+// ---- plans ---------------------------------------------------------------------------------------------------------------
+bool shape_ok(const cnn_log_probs_shape* s) {
+  return s && s->rows >= 1 && s->rows < (int64_t)1 << 31 && s->vocab >= 1 && s->vocab <= MOST_VOCAB && s->given >= 1 && s->given <= MOST_GIVEN && s->top >= 0 &&
+         s->top <= MOST_TOP && s->top <= s->vocab && type_known(s->type) && s->scale > 0.0f && s->scale <= 1e30f;
+}
+
+bool rows_ok(const cnn_rows* r, int type) {
+  return r && r->data && reinterpret_cast<uintptr_t>(r->data) % type_bytes(type) == 0 && r->row >= 0;
+}
+
+struct Plan {
+  int threads, each, parts;
+  int64_t part_length;
+  size_t keys, bytes;
+};
+
+// One part where a workgroup holds the row.  Else the second kernel is needed anyway, and parts are as short as a thousand workgroups ask.
+Plan plan_of(const cnn_log_probs_shape& s) {
+  Plan p{};
+  constexpr struct { int threads, each; } FORMS[] = {{64, 8}, {64, 16}, {64, 32}, {256, 16}, {256, 32}, {1024, 32}};
+  int64_t want = s.vocab;
+  if (want > 32768) {
+    want = s.rows * s.vocab / 1024;
+    want = want < 4096 ? 4096 : want > 32768 ? 32768 : want;
+  }
+  for (const auto& f : FORMS) {
+    p.threads = f.threads, p.each = f.each;
+    if (want <= (int64_t)f.threads * f.each) break;
+  }
+  const int64_t most = (int64_t)p.threads * p.each;
+  p.parts = (int)((s.vocab + most - 1) / most);
+  p.part_length = ((s.vocab + p.parts - 1) / p.parts + 7) / 8 * 8;
+  p.parts = (int)((s.vocab + p.part_length - 1) / p.part_length);
+  if (p.parts > 1) {
+    p.keys = ((size_t)s.rows * p.parts * sizeof(Sums) + 255) & ~(size_t)255;
+    p.bytes = p.keys + (size_t)s.rows * p.parts * s.top * 8;
+  }
+  return p;
+}
+
+template <class T>
+void launch_part(const Args& a, const Plan& p, hipStream_t st) {
+  const dim3 grid = grid_of(a.rows * a.parts);
+  if (p.threads == 64 && p.each == 8) logp_part_kernel<T, 64, 8><<<grid, 64, 0, st>>>(a);
+  else if (p.threads == 64 && p.each == 16) logp_part_kernel<T, 64, 16><<<grid, 64, 0, st>>>(a);
+  else if (p.threads == 64) logp_part_kernel<T, 64, 32><<<grid, 64, 0, st>>>(a);
+  else if (p.threads == 256 && p.each == 16) logp_part_kernel<T, 256, 16><<<grid, 256, 0, st>>>(a);
+  else if (p.threads == 256) logp_part_kernel<T, 256, 32><<<grid, 256, 0, st>>>(a);
+  else logp_part_kernel<T, 1024, 32><<<grid, 1024, 0, st>>>(a);
+}
+
+template <class T, int THREADS, int PACKS>
+void launch_backward(BackArgs a, hipStream_t st) {
+  constexpr int64_t TILE = THREADS * PACKS * (sizeof(T) == 2 ? 8 : 4);
+  a.tiles = (int)((a.vocab + TILE - 1) / TILE);
+  logp_backward_kernel<T, THREADS, PACKS><<<grid_of(a.rows * a.tiles), THREADS, 0, st>>>(a);
+}
+
+}  // namespace
+}  // namespace logp
+}  // namespace cnn
+
+extern "C" {
+
+size_t cnn_log_probs_fwd_workspace_bytes(const cnn_log_probs_shape* s) { return cnn::logp::shape_ok(s) ? cnn::logp::plan_of(*s).bytes : 0; }
+
+int cnn_log_probs_fwd(const cnn_log_probs_shape* s, const cnn_rows* logits, const void* tokens, float* log_probs, float* entropy, float* stats,
+                      float* top_log_probs, int32_t* top_tokens, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  using namespace cnn;
+  using namespace cnn::logp;
+  if (!shape_ok(s) || !rows_ok(logits, s->type) || !tokens || !log_probs || (s->top && (!top_log_probs || !top_tokens))) return CNN_EINVAL;
+  for (const void* p : {(const void*)tokens, (const void*)log_probs, (const void*)entropy, (const void*)stats, (const void*)top_log_probs,
+                        (const void*)top_tokens, (const void*)workspace})
+    if (!aligned16(p)) return CNN_EINVAL;
+  const Plan p = plan_of(*s);
+  if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return CNN_EWORKSPACE;
+  char* ws = static_cast<char*>(workspace);
+  const Args a{logits->data, logits->row, s->rows, s->vocab, p.part_length, tokens, log_probs, entropy, stats, top_log_probs, top_tokens,
+               reinterpret_cast<Sums*>(ws), reinterpret_cast<uint64_t*>(ws + p.keys), p.parts, s->given, s->top, s->wide_tokens != 0, s->scale};
+  hipStream_t st = (hipStream_t)hip_stream;
+  return with_type(s->type, [&](auto t) {
+    using T = decltype(t);
+    launch_part<T>(a, p, st);
+    if (launch_status() != CNN_OK) return CNN_EHIP;
+    if (p.parts == 1) return CNN_OK;
+    logp_join_kernel<T><<<grid_of(a.rows), JOIN_THREADS, 0, st>>>(a);
+    return launch_status();
+  });
+}
+
+int cnn_log_probs_bwd(const cnn_log_probs_shape* s, const cnn_rows* logits, const void* tokens, const float* stats, const float* d_log_probs,
+                      const float* d_entropy, void* d_logits, void* hip_stream) {
+  using namespace cnn;
+  using namespace cnn::logp;
+  if (!shape_ok(s) || !rows_ok(logits, s->type) || !tokens || !stats || !d_log_probs || !d_logits) return CNN_EINVAL;
+  for (const void* p : {(const void*)tokens, (const void*)stats, (const void*)d_log_probs, (const void*)d_entropy, (const void*)d_logits})
+    if (!aligned16(p)) return CNN_EINVAL;
+  const BackArgs a{logits->data, logits->row, s->rows, s->vocab, tokens, stats, d_log_probs, d_entropy, d_logits, 1, s->given, s->wide_tokens != 0, s->scale};
+  hipStream_t st = (hipStream_t)hip_stream;
+  return with_type(s->type, [&](auto t) {
+    using T = decltype(t);
+    constexpr int PACK = sizeof(T) == 2 ? 8 : 4;
+    if (s->vocab <= 64 * PACK) launch_backward<T, 64, 1>(a, st);
+    else if (s->vocab <= 256 * PACK) launch_backward<T, 256, 1>(a, st);
+    else launch_backward<T, 256, 32 / PACK>(a, st);
+    return launch_status();
+  });
+}
+
+}  // extern "C"

@@ -38,6 +38,38 @@ __device__ __forceinline__ P got_past_caches(const P* at) {
   return __builtin_bit_cast(P, words);
 }
 
+// N elements at any multiple of their own size: global memory takes loads and stores of up to sixteen bytes there.
+template <class T, int N>
+struct Loose {
+  T v[N];
+};
+
+// The first `count` of N elements as floats, zeros behind them; and their stores.  A whole pack is one access.
+template <int N, class T>
+__device__ __forceinline__ void get_loose(float (&to)[N], const T* at, int count) {
+  if (count >= N) {
+    const Loose<T, N> p = *reinterpret_cast<const Loose<T, N>*>(at);
+#pragma unroll
+    for (int j = 0; j < N; ++j) to[j] = (float)p.v[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) to[j] = j < count ? (float)at[j] : 0.0f;
+  }
+}
+template <int N, class T>
+__device__ __forceinline__ void put_loose(T* at, const float (&from)[N], int count) {
+  if (count >= N) {
+    Loose<T, N> p;
+#pragma unroll
+    for (int j = 0; j < N; ++j) p.v[j] = (T)from[j];
+    *reinterpret_cast<Loose<T, N>*>(at) = p;
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < count) at[j] = (T)from[j];
+  }
+}
+
 // Calls fn with a value of the element type that `type` names.
 template <class FN>
 auto with_type(int type, FN fn) {

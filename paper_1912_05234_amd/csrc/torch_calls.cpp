@@ -11,6 +11,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 
 #include <climits>
@@ -520,6 +521,195 @@ CALL(linear_attention_step, 7)  // q, k, v, decay, scale, state, slots or None
   return wrap(std::move(o));
 END
 
+// ---- around a block, and the loss ------------------------------------------------------------------------------
+// These calls run on the device of their first tensor, whatever the current one is, and want all tensors there.
+const at::Tensor& on(const at::Tensor& t, at::Device device) {
+  if (t.device() != device) raise(PyExc_ValueError, "expected all tensors on one GPU");
+  return t;
+}
+
+// Rows of the last dimension, which has no gaps, at one distance.
+const at::Tensor& rows_tensor(PyObject* o, cnn_rows* rows) {
+  const at::Tensor& t = any_tensor(o, true);
+  if (t.dim() < 1) raise(PyExc_ValueError, "expected a tensor of at least 1 dimension");
+  const int last = (int)t.dim() - 1;
+  if (t.size(last) > 1 && t.stride(last) != 1) raise(PyExc_ValueError, "expected a last dimension without gaps");
+  int64_t row = t.size(last), next = -1;  // what the dimension in front would have for a stride
+  for (int i = last - 1; i >= 0; --i) {
+    if (t.size(i) == 1) continue;
+    if (next < 0) row = t.stride(i);
+    else if (t.stride(i) != next) raise(PyExc_ValueError, "expected rows at one distance");
+    next = t.stride(i) * t.size(i);
+  }
+  *rows = {t.data_ptr(), row};
+  return t;
+}
+
+const cnn_rows* rows_or_null(PyObject* o, cnn_rows* rows, const at::Tensor& x, at::ScalarType type, const char* what) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = on(rows_tensor(o, rows), x.device());
+  if (t.scalar_type() != type || t.sizes() != x.sizes()) {
+    PyErr_Format(PyExc_ValueError, "expected %s of the same shape and a fitting type", what);
+    throw Raised();
+  }
+  return rows;
+}
+
+at::ScalarType type_or(PyObject* o, at::ScalarType type) {
+  return THPVariable_Check(o) ? THPVariable_Unpack(o).scalar_type() : type;
+}
+
+// x or r [..., groups * width], its weight, scale, eps, groups.
+cnn_norm_shape norm_shape(const at::Tensor& x, at::ScalarType type, at::ScalarType stream_type, PyObject* scale, PyObject* eps, PyObject* groups) {
+  const auto code = [](at::ScalarType t) {
+    return t == at::kFloat ? CNN_F32 : t == at::kBFloat16 ? CNN_BF16 : t == at::kHalf ? CNN_F16 : -1;
+  };
+  const int64_t D = x.size(-1), G = integer(groups);
+  if (G < 1 || G > INT_MAX || D < 1 || D > INT_MAX || D % G) raise(PyExc_ValueError, "expected groups that divide the last dimension");
+  if (code(type) < 0 || code(stream_type) < 0 || (stream_type != type && stream_type != at::kFloat))
+    raise(PyExc_ValueError, "expected torch.float32, torch.bfloat16 or torch.float16 tensors, of one type or with a residual stream of torch.float32");
+  return {x.numel() / D, (int)G, (int)(D / G), code(type), code(stream_type), (float)number(scale), (float)number(eps)};
+}
+
+const float* weight_of(PyObject* o, const at::Tensor& x) {
+  const at::Tensor& w = on(tensor(o), x.device());
+  if (w.dim() != 1 || w.size(0) != x.size(-1)) raise(PyExc_ValueError, "expected one weight for each element of a row");
+  return data(w);
+}
+
+PyObject* object(const at::Tensor& t) { return t.defined() ? THPVariable_Wrap(t) : (Py_INCREF(Py_None), Py_None); }
+
+CALL(add_norm_fwd, 6)  // x, weight, residual or None, scale, eps, groups
+  cnn_rows rx, rr;
+  const at::Tensor& x = rows_tensor(a[0], &rx);
+  const at::ScalarType stream_type = type_or(a[2], x.scalar_type());
+  const cnn_norm_shape shape = norm_shape(x, x.scalar_type(), stream_type, a[3], a[4], a[5]);
+  const float* weight = weight_of(a[1], x);
+  const cnn_rows* residual = rows_or_null(a[2], &rr, x, stream_type, "a residual");
+  const c10::DeviceGuard guard(x.device());
+  at::Tensor y = empty(x.sizes(), x.device(), x.scalar_type()), r;
+  if (residual) r = empty(x.sizes(), x.device(), stream_type);
+  call("cnn_add_norm_fwd", [&] { return cnn_add_norm_fwd(&shape, &rx, residual, weight, y.data_ptr(), residual ? r.data_ptr() : nullptr, stream()); });
+  return pair(wrap(std::move(y)), residual ? wrap(std::move(r)) : (Py_INCREF(a[0]), a[0]));
+END
+
+at::Tensor bytes_on(size_t bytes, at::Device device) { return bytes ? empty({(int64_t)bytes}, device, at::kByte) : at::Tensor(); }
+
+CALL(add_norm_bwd, 7)  // d_y, r, weight, d_r or None, scale, eps, groups
+  cnn_rows ry, rr, rd;
+  const at::Tensor& r = rows_tensor(a[1], &rr);
+  const at::ScalarType type = type_or(a[0], r.scalar_type()), stream_type = r.scalar_type();
+  const cnn_norm_shape shape = norm_shape(r, type, stream_type, a[4], a[5], a[6]);
+  if (!rows_or_null(a[0], &ry, r, type, "an output error")) raise(PyExc_TypeError, "expected a tensor");
+  const float* weight = weight_of(a[2], r);
+  const cnn_rows* d_r = rows_or_null(a[3], &rd, r, stream_type, "a residual stream's error");
+  const c10::DeviceGuard guard(r.device());
+  const bool two = type != stream_type || shape.scale != 1.0f;
+  at::Tensor d_residual = empty(r.sizes(), r.device(), stream_type), d_x, d_weight = empty({r.size(-1)}, r.device());
+  if (two) d_x = empty(r.sizes(), r.device(), type);
+  const size_t bytes = cnn_norm_bwd_workspace_bytes(&shape);
+  const at::Tensor ws = bytes_on(bytes, r.device());
+  call("cnn_add_norm_bwd", [&] {
+    return cnn_add_norm_bwd(&shape, &ry, &rr, d_r, weight, two ? d_x.data_ptr() : nullptr, d_residual.data_ptr(), data(d_weight),
+                            bytes ? ws.data_ptr() : nullptr, bytes, stream());
+  });
+  PyObject* residual = object(d_residual);
+  return pair(pair(two ? object(d_x) : (Py_XINCREF(residual), residual), residual), object(d_weight));
+END
+
+CALL(norm_gate_fwd, 7)  // x, weight, gate or None, residual or None, scale, eps, groups
+  cnn_rows rx, rg, rr;
+  const at::Tensor& x = rows_tensor(a[0], &rx);
+  const at::ScalarType stream_type = type_or(a[3], x.scalar_type());
+  const cnn_norm_shape shape = norm_shape(x, x.scalar_type(), stream_type, a[4], a[5], a[6]);
+  const float* weight = weight_of(a[1], x);
+  const cnn_rows *gate = rows_or_null(a[2], &rg, x, x.scalar_type(), "a gate"), *residual = rows_or_null(a[3], &rr, x, stream_type, "a residual");
+  const c10::DeviceGuard guard(x.device());
+  at::Tensor y = empty(x.sizes(), x.device(), stream_type);
+  call("cnn_norm_gate_fwd", [&] { return cnn_norm_gate_fwd(&shape, &rx, gate, residual, weight, y.data_ptr(), stream()); });
+  return wrap(std::move(y));
+END
+
+CALL(norm_gate_bwd, 7)  // d_y, x, weight, gate or None, scale, eps, groups
+  cnn_rows ry, rx, rg;
+  const at::Tensor& x = rows_tensor(a[1], &rx);
+  const at::ScalarType type = x.scalar_type(), stream_type = type_or(a[0], type);
+  const cnn_norm_shape shape = norm_shape(x, type, stream_type, a[4], a[5], a[6]);
+  if (!rows_or_null(a[0], &ry, x, stream_type, "an output error")) raise(PyExc_TypeError, "expected a tensor");
+  const float* weight = weight_of(a[2], x);
+  const cnn_rows* gate = rows_or_null(a[3], &rg, x, type, "a gate");
+  const c10::DeviceGuard guard(x.device());
+  at::Tensor d_x = empty(x.sizes(), x.device(), type), d_gate, d_weight = empty({x.size(-1)}, x.device());
+  if (gate) d_gate = empty(x.sizes(), x.device(), type);
+  const size_t bytes = cnn_norm_bwd_workspace_bytes(&shape);
+  const at::Tensor ws = bytes_on(bytes, x.device());
+  call("cnn_norm_gate_bwd", [&] {
+    return cnn_norm_gate_bwd(&shape, &ry, &rx, gate, weight, d_x.data_ptr(), gate ? d_gate.data_ptr() : nullptr, data(d_weight),
+                             bytes ? ws.data_ptr() : nullptr, bytes, stream());
+  });
+  return pair(pair(object(d_x), object(d_gate)), object(d_weight));
+END
+
+// logits [..., V] and tokens [...] or [..., M]
+struct LogProbs {
+  cnn_log_probs_shape shape;
+  cnn_rows logits;
+  const at::Tensor &x, &tokens;
+};
+
+LogProbs log_probs_of(PyObject* logits, PyObject* tokens, PyObject* scale, PyObject* top) {
+  cnn_rows rows;
+  const at::Tensor& x = rows_tensor(logits, &rows);
+  const at::Tensor& t = on(token_tensor(tokens), x.device());
+  const int type = element_type(x);
+  const int64_t lead = x.dim() - 1, V = x.size(-1), M = t.dim() == lead ? 1 : t.size(-1), k = top ? integer(top) : 0;
+  if ((t.dim() != lead && t.dim() != lead + 1) || t.sizes().slice(0, lead) != x.sizes().slice(0, lead))
+    raise(PyExc_ValueError, "expected one token, or as many as the last dimension of tokens says, for each row of logits");
+  if (V < 1) raise(PyExc_ValueError, "expected logits");
+  if (M > INT_MAX) raise(PyExc_ValueError, "a dimension is too large");
+  if (k < 0 || k > V || k > INT_MAX) raise(PyExc_ValueError, "expected no more top tokens than a row has");
+  return {{x.numel() / V, V, (int)M, (int)k, type, t.scalar_type() == at::kLong, (float)number(scale)}, rows, x, t};
+}
+
+CALL(log_probs_fwd, 4)  // logits, tokens, scale, top
+  const LogProbs l = log_probs_of(a[0], a[1], a[2], a[3]);
+  const at::Device device = l.x.device();
+  const c10::DeviceGuard guard(device);
+  const std::vector<int64_t> lead(l.x.sizes().begin(), l.x.sizes().end() - 1);
+  const auto with = [&](int64_t n) {
+    std::vector<int64_t> sizes = lead;
+    sizes.push_back(n);
+    return sizes;
+  };
+  const int top = l.shape.top;
+  at::Tensor log_probs = empty(l.tokens.sizes(), device), entropy = empty(lead, device), stats = empty(with(3), device), top_log_probs, top_tokens;
+  if (top) top_log_probs = empty(with(top), device), top_tokens = empty(with(top), device, at::kInt);
+  const size_t bytes = cnn_log_probs_fwd_workspace_bytes(&l.shape);
+  const at::Tensor ws = bytes_on(bytes, device);
+  call("cnn_log_probs_fwd", [&] {
+    return cnn_log_probs_fwd(&l.shape, &l.logits, l.tokens.data_ptr(), data(log_probs), data(entropy), data(stats), top ? data(top_log_probs) : nullptr,
+                             top ? data<int32_t>(top_tokens) : nullptr, bytes ? ws.data_ptr() : nullptr, bytes, stream());
+  });
+  return pair(pair(object(log_probs), object(entropy)), pair(object(stats), pair(object(top_log_probs), object(top_tokens))));
+END
+
+CALL(log_probs_bwd, 6)  // logits, tokens, stats, d_log_probs, d_entropy or None, scale
+  const LogProbs l = log_probs_of(a[0], a[1], a[5], nullptr);
+  const at::Device device = l.x.device();
+  const at::Tensor &stats = on(tensor(a[2]), device), &d = on(tensor(a[3]), device);
+  const at::IntArrayRef lead = l.x.sizes().slice(0, l.x.dim() - 1);
+  if (stats.dim() != l.x.dim() || stats.sizes().slice(0, lead.size()) != lead || stats.size(-1) != 3) raise(PyExc_ValueError, "expected the stats of the forward call");
+  if (d.sizes() != l.tokens.sizes()) raise(PyExc_ValueError, "expected an error for each given token");
+  const float* d_entropy = optional(a[4], lead, "an entropy's error");
+  if (d_entropy) on(THPVariable_Unpack(a[4]), device);
+  const c10::DeviceGuard guard(device);
+  at::Tensor d_logits = empty(l.x.sizes(), device, l.x.scalar_type());
+  call("cnn_log_probs_bwd", [&] {
+    return cnn_log_probs_bwd(&l.shape, &l.logits, l.tokens.data_ptr(), data(stats), data(d), d_entropy, d_logits.data_ptr(), stream());
+  });
+  return wrap(std::move(d_logits));
+END
+
 PyObject* raise_through(PyObject*, PyObject* fn) {  // binding._check
   Py_INCREF(fn);
   Py_XSETREF(check, fn);
@@ -531,7 +721,7 @@ PyMethodDef methods[] = {FAST(forward), FAST(gradient), FAST(train_batch), FAST(
                          FAST(conv_bwd_weight), FAST(avgpool_fwd), FAST(avgpool_bwd), FAST(fc_fwd), FAST(fc_bwd_input),
                          FAST(fc_bwd_weight), FAST(logistic_fwd), FAST(logistic_bwd), FAST(embedding_fwd), FAST(embedding_bwd), FAST(dropout_fwd),
                          FAST(dropout_bwd), FAST(linear_attention_fwd), FAST(linear_attention_bwd), FAST(linear_attention_step),
-                        
+                         FAST(add_norm_fwd), FAST(add_norm_bwd), FAST(norm_gate_fwd), FAST(norm_gate_bwd), FAST(log_probs_fwd), FAST(log_probs_bwd),
                          {"raise_through", raise_through, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

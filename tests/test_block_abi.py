@@ -1,0 +1,89 @@
+"""Host-side checks of the entry points around a block: what is refused before anything touches the device, and the workspaces."""
+import ctypes
+
+from paper_1912_05234_amd import binding
+
+EINVAL, EWS = -1, -2
+nul, fake, odd = ctypes.c_void_p(None), ctypes.c_void_p(0x1000), ctypes.c_void_p(0x1004)  # never dereferenced
+
+
+def rows(data=0x1002, row=77):
+    return binding.Rows(data, row)
+
+
+def norm(rows=100, groups=3, width=32, type_=1, stream=1, scale=0.5, eps=1e-6):
+    return binding.NormShape(rows, groups, width, type_, stream, scale, eps)
+
+
+BAD_NORMS = [{"rows": 0}, {"rows": 1 << 31}, {"groups": 0}, {"width": 0}, {"width": 16385}, {"groups": 1 << 16, "width": 17}, {"type_": 3}, {"type_": -1},
+             {"type_": 1, "stream": 2}, {"type_": 0, "stream": 1}, {"stream": 5}, {"eps": 0.0}, {"eps": -1.0}, {"eps": float("nan")},
+             {"eps": float("inf")}, {"scale": float("nan")}, {"scale": float("inf")}]
+BAD_ROWS = [rows(data=0), rows(data=0x1001), rows(row=-1)]
+
+
+def test_norm_refusals():
+    L = binding.lib()
+    add = lambda s=norm(), x=rows(), res=rows(), w=fake, y=fake, r=fake: L.cnn_add_norm_fwd(s, x, res, w, y, r, nul)  # noqa: E731
+    addb = lambda s=norm(), d=rows(), r=rows(), dr=rows(), w=fake, dx=fake, res=fake, dw=fake, ws=fake, n=1 << 40: L.cnn_add_norm_bwd(  # noqa: E731
+        s, d, r, dr, w, dx, res, dw, ws, n, nul)
+    gate = lambda s=norm(), x=rows(), g=rows(), res=rows(), w=fake, y=fake: L.cnn_norm_gate_fwd(s, x, g, res, w, y, nul)  # noqa: E731
+    gateb = lambda s=norm(), d=rows(), x=rows(), g=rows(), w=fake, dx=fake, dg=fake, dw=fake, ws=fake, n=1 << 40: L.cnn_norm_gate_bwd(  # noqa: E731
+        s, d, x, g, w, dx, dg, dw, ws, n, nul)
+    assert add(s=None) == addb(s=None) == gate(s=None) == gateb(s=None) == EINVAL
+    assert add(x=None) == addb(d=None) == addb(r=None) == gate(x=None) == gateb(d=None) == gateb(x=None) == EINVAL
+    for bad in BAD_NORMS:
+        s = norm(**bad)
+        assert add(s=s) == addb(s=s) == gate(s=s) == gateb(s=s) == EINVAL and L.cnn_norm_bwd_workspace_bytes(s) == 0, bad
+    for r in BAD_ROWS:
+        assert add(x=r) == add(res=r) == addb(d=r) == addb(r=r) == addb(dr=r) == gate(x=r) == gate(g=r) == gate(res=r) == gateb(d=r) == gateb(x=r) == gateb(g=r) == EINVAL
+    for p in (nul, odd):
+        assert add(w=p) == add(y=p) == addb(w=p) == addb(res=p) == addb(dw=p) == gate(w=p) == gate(y=p) == gateb(w=p) == gateb(dx=p) == gateb(dw=p) == gateb(dg=p) == EINVAL
+    assert add(r=odd) == addb(dx=odd) == addb(ws=odd) == EINVAL
+    # without a residual there is nothing to scale, to return or of another type
+    assert add(res=None) == add(res=None, r=nul) == add(s=norm(scale=1.0), res=None) == add(s=norm(scale=1.0, stream=0), res=None, r=nul) == EINVAL
+    assert gateb(g=None) == EINVAL  # a gate's gradient without a gate
+    need = L.cnn_norm_bwd_workspace_bytes(norm())
+    assert need and addb(n=need - 1) == gateb(n=need - 1) == addb(ws=nul) == gateb(ws=nul) == EWS
+
+
+def test_norm_workspaces():
+    """A row of partial sums for every workgroup along the rows; none where there is one."""
+    q = binding.lib().cnn_norm_bwd_workspace_bytes
+    assert q(norm(rows=1)) == 0 and q(norm(rows=2, groups=1)) == 0 and q(None) == 0
+    assert q(norm(rows=1 << 20, groups=1, width=64)) == 1024 * 64 * 4
+    assert q(norm(rows=1 << 20, groups=1, width=4096)) == 1024 * 4096 * 4
+    assert q(norm(rows=1 << 20, groups=64, width=16384)) == 4 * 64 * 16384 * 4
+
+
+def logp(rows=100, vocab=1000, given=2, top=5, type_=1, wide=1, scale=1.0):
+    return binding.LogProbsShape(rows, vocab, given, top, type_, wide, scale)
+
+
+BAD_LOGP = [{"rows": 0}, {"rows": 1 << 31}, {"vocab": 0}, {"vocab": (1 << 24) + 1}, {"given": 0}, {"given": 257}, {"top": -1}, {"top": 65}, {"vocab": 4}, {"type_": 3},
+            {"scale": 0.0}, {"scale": -1.0}, {"scale": float("nan")}, {"scale": float("inf")}]
+
+
+def test_log_probs_refusals():
+    L = binding.lib()
+    fwd = lambda s=logp(), x=rows(), t=fake, lp=fake, h=fake, st=fake, tl=fake, tt=fake, ws=fake, n=1 << 40: L.cnn_log_probs_fwd(  # noqa: E731
+        s, x, t, lp, h, st, tl, tt, ws, n, nul)
+    bwd = lambda s=logp(), x=rows(), t=fake, st=fake, d=fake, dh=fake, o=fake: L.cnn_log_probs_bwd(s, x, t, st, d, dh, o, nul)  # noqa: E731
+    assert fwd(s=None) == fwd(x=None) == bwd(s=None) == bwd(x=None) == EINVAL
+    for bad in BAD_LOGP:
+        assert fwd(s=logp(**bad)) == bwd(s=logp(**bad)) == EINVAL and L.cnn_log_probs_fwd_workspace_bytes(logp(**bad)) == 0, bad
+    for r in BAD_ROWS:
+        assert fwd(x=r) == bwd(x=r) == EINVAL
+    for p in (nul, odd):
+        assert fwd(t=p) == fwd(lp=p) == fwd(tl=p) == fwd(tt=p) == bwd(t=p) == bwd(st=p) == bwd(d=p) == bwd(o=p) == EINVAL
+    assert fwd(h=odd) == fwd(st=odd) == fwd(ws=odd) == bwd(dh=odd) == EINVAL
+    long = logp(vocab=100000)
+    need = L.cnn_log_probs_fwd_workspace_bytes(long)
+    assert need and fwd(s=long, n=need - 1) == fwd(s=long, ws=nul) == EWS
+
+
+def test_log_probs_workspaces():
+    """None for rows that a workgroup holds; sums and keys of the parts of longer ones."""
+    q = binding.lib().cnn_log_probs_fwd_workspace_bytes
+    assert q(logp(vocab=32768)) == 0 and q(None) == 0
+    assert q(logp(rows=1, vocab=32769, top=0)) >= 2 * 12
+    assert q(logp(rows=1, vocab=1 << 24, top=64)) >= 512 * (12 + 64 * 8)
