@@ -387,6 +387,32 @@ int cnn_log_probs_fwd(const cnn_log_probs_shape* shape, const cnn_rows* logits, 
 int cnn_log_probs_bwd(const cnn_log_probs_shape* shape, const cnn_rows* logits, const void* tokens, const float* stats, const float* d_log_probs,
                       const float* d_entropy, void* d_logits, void* hip_stream);
 
+/* Causal convolution of K taps along each channel: p_t = bias + sum_k weight[d,k] x_{t-K+1+k}, y = p, or silu(p) = p / (1 + exp(-p)) with silu != 0.
+ * weight[D,K] and bias[D] (nullable) are fp32.  x (and d_y) of `type` with their strides, in elements, none negative, aligned to their element; y and d_x
+ * are contiguous, [B,T,D].  A state [B,K-1,D] of `type` holds a sequence's last K - 1 inputs, the newest last: what stands before its first token
+ * (initial_state, nullable: zeros), and what it leaves (final_state, nullable: not wanted), of a short sequence the initial state's rest too.  They may not be the
+ * same memory.  lengths[B] (nullable: all T; below 0 counts as 0, above T as T): tokens past a sequence's length are not read, and their rows of the results are
+ * zero.  2 <= K <= 8, 1 <= D <= 2^20, B * T < 2^31.  A NaN or an infinity reaches its channel's results of the K tokens that see it (and d_weight, d_bias). */
+typedef struct {
+  int B, T, D, K, type, silu;
+} cnn_causal_conv_shape;
+typedef struct {
+  const void* data; /* element (b, t, d) at b * batch + t * token + d */
+  int64_t batch, token;
+} cnn_tokens;
+int cnn_causal_conv_fwd(const cnn_causal_conv_shape* shape, const cnn_tokens* x, const float* weight, const float* bias, const int32_t* lengths,
+                        const void* initial_state, void* y, void* final_state, void* hip_stream);
+/* For the error d_y of y and (nullable) d_final_state of the final state: d_x, d_weight, d_bias and d_initial_state (both nullable: not
+ * wanted).  Sums of the weights' gradients are fp32 in an order that the shape fixes. */
+size_t cnn_causal_conv_bwd_workspace_bytes(const cnn_causal_conv_shape* shape);
+int cnn_causal_conv_bwd(const cnn_causal_conv_shape* shape, const cnn_tokens* x, const cnn_tokens* d_y, const float* weight, const float* bias,
+                        const int32_t* lengths, const void* initial_state, const void* d_final_state, void* d_x, float* d_weight, float* d_bias,
+                        void* d_initial_state, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* One token of every sequence (T = 1, token strides unused): state[pool,K-1,D] is moved on in place, y[B,D].  Slots as for
+ * cnn_linear_attention_step. */
+int cnn_causal_conv_step(const cnn_causal_conv_shape* shape, const cnn_tokens* x, const float* weight, const float* bias, void* state, int64_t pool,
+                         const int32_t* slots, void* y, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

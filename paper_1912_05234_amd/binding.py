@@ -104,6 +104,17 @@ class Rows(ctypes.Structure):
     _fields_ = [("data", _vp), ("row", _i64)]
 
 
+class CausalConvShape(ctypes.Structure):
+    """cnn_causal_conv_shape"""
+    _fields_ = [(name, _i) for name in ("B", "T", "D", "K", "type", "silu")]
+
+
+class Tokens(ctypes.Structure):
+    """cnn_tokens"""
+    _fields_ = [("data", _vp), ("batch", _i64), ("token", _i64)]
+
+
+_conv, _tokens = ctypes.POINTER(CausalConvShape), ctypes.POINTER(Tokens)
 _norm, _logp, _rows = ctypes.POINTER(NormShape), ctypes.POINTER(LogProbsShape), ctypes.POINTER(Rows)
 SIGNATURES.update({
     "cnn_add_norm_fwd": (_i, [_norm] + [_rows] * 2 + [_vp] * 4),
@@ -114,6 +125,10 @@ SIGNATURES.update({
     "cnn_log_probs_fwd_workspace_bytes": (_sz, [_logp]),
     "cnn_log_probs_fwd": (_i, [_logp, _rows] + [_vp] * 7 + [_sz, _vp]),
     "cnn_log_probs_bwd": (_i, [_logp, _rows] + [_vp] * 6),
+    "cnn_causal_conv_fwd": (_i, [_conv, _tokens] + [_vp] * 7),
+    "cnn_causal_conv_bwd_workspace_bytes": (_sz, [_conv]),
+    "cnn_causal_conv_bwd": (_i, [_conv, _tokens, _tokens] + [_vp] * 10 + [_sz, _vp]),
+    "cnn_causal_conv_step": (_i, [_conv, _tokens] + [_vp] * 3 + [_i64] + [_vp] * 3),
 })
 
 _lib = None
@@ -390,6 +405,26 @@ def norm_gate_bwd(d_y, x, weight, gate=None, scale=1.0, eps=1e-6, groups=1):
     """(d_x, d_gate or None, d_weight); the residual's gradient is d_y itself, whose type is the forward result's."""
     (d_x, d_gate), d_weight = (_calls or _native()).norm_gate_bwd(d_y, x, weight, gate, scale, eps, groups)
     return d_x, d_gate, d_weight
+
+
+# ---- short causal convolution ----------------------------------------------------------
+def causal_conv_fwd(x, weight, bias=None, silu=False, lengths=None, initial_state=None, want_state=False):
+    """(y[B, T, D], final state [B, K - 1, D] or None) of p_t = bias + sum_k weight[:, k] x_{t-K+1+k}, y = silu(p) or p, for x[B, T, D] of any
+    strides but the last, weight[D, K] and bias[D] fp32, K from 2 to 8, lengths[B] int32 (None: all T).  A state is the last K - 1 inputs, the newest last."""
+    return (_calls or _native()).causal_conv_fwd(x, weight, bias, bool(silu), lengths, initial_state, bool(want_state))
+
+
+def causal_conv_bwd(x, weight, d_y, bias=None, silu=False, lengths=None, initial_state=None, d_final_state=None, want_d_state=False):
+    """(d_x, d_weight, d_bias or None, error of the initial state or None) of the call above with the same arguments."""
+    (d_x, d_weight), (d_bias, d_state) = (_calls or _native()).causal_conv_bwd(x, weight, bias, bool(silu), d_y, lengths, initial_state, d_final_state,
+                                                                              bool(want_d_state))
+    return d_x, d_weight, d_bias, d_state
+
+
+def causal_conv_step(x, weight, state, bias=None, silu=False, slots=None):
+    """y[B, D] of one token x[B, D] of every sequence; state[pool, K - 1, D] is moved on in place, row b using state slots[b] (int32; None:
+    state b).  A slot outside the pool: a row without a sequence, its y is zero.  No two rows may have the same slot."""
+    return (_calls or _native()).causal_conv_step(x, weight, bias, bool(silu), state, slots)
 
 
 # ---- log probabilities -----------------------------------------------------------------

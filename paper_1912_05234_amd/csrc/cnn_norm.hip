@@ -1,29 +1,18 @@
 // Entry points of the norms around a block, and the sum of their weight's gradient over workgroups.
 #include "cnn_norm.h"
 
+#include "cnn_fold.h"
+
 namespace cnn {
 namespace norm {
 namespace {
 
 constexpr int MOST_WIDTH = 16384, MOST_COLUMNS = 1 << 20;
 
-// d_weight[c] = sum of partial[.][c], 32 rows side by side and then over those.
-constexpr int FOLD_COLUMNS = 32, FOLD_ROWS = 32;
-__global__ __launch_bounds__(FOLD_COLUMNS* FOLD_ROWS) void norm_fold_kernel(const float* partial, float* d_weight, int64_t rows, int columns) {
-  __shared__ float sums[FOLD_ROWS][FOLD_COLUMNS];
-  const int column = threadIdx.x % FOLD_COLUMNS, row = threadIdx.x / FOLD_COLUMNS, c = blockIdx.x * FOLD_COLUMNS + column;
-  float s = 0.0f;
-  if (c < columns)
-#pragma unroll 8
-    for (int64_t r = row; r < rows; r += FOLD_ROWS) s += partial[r * columns + c];
-  sums[row][column] = s;
-  __syncthreads();
-  if (row == 0 && c < columns) {
-#pragma unroll
-    for (int r = 1; r < FOLD_ROWS; ++r) s += sums[r][column];
-    d_weight[c] = s;
-  }
-}
+struct PutWeight {
+  float* d_weight;
+  __device__ void operator()(int64_t c, float sum) const { d_weight[c] = sum; }
+};
 
 bool shape_ok(const cnn_norm_shape* s) {
   return s && s->rows >= 1 && s->rows < (int64_t)1 << 31 && s->groups >= 1 && s->width >= 1 && s->width <= MOST_WIDTH &&
@@ -76,9 +65,7 @@ int run(const Args& a, const cnn_norm_shape& s, const Plan& p, Mode mode, bool b
   (s.type == CNN_F32 ? launch_f32 : s.type == CNN_BF16 ? launch_bf16 : launch_f16)(a, s.stream_type, mode, backward, p.cut, grid, st);
   if (launch_status() != CNN_OK) return CNN_EHIP;
   if (!p.bytes) return CNN_OK;
-  const int columns = s.groups * s.width;
-  norm_fold_kernel<<<(columns + FOLD_COLUMNS - 1) / FOLD_COLUMNS, FOLD_COLUMNS * FOLD_ROWS, 0, st>>>(a.partial, d_weight, p.row_blocks, columns);
-  return launch_status();
+  return fold(a.partial, p.row_blocks, (int64_t)s.groups * s.width, PutWeight{d_weight}, st);
 }
 
 bool all_aligned(std::initializer_list<const void*> all) {

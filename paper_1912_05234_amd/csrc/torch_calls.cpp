@@ -710,6 +710,113 @@ CALL(log_probs_bwd, 6)  // logits, tokens, stats, d_log_probs, d_entropy or None
   return wrap(std::move(d_logits));
 END
 
+// A [batch, token, width] (the step's: [batch, width]) tensor with whatever strides, its last dimension without gaps.
+const at::Tensor& tokens_tensor(PyObject* o, int dims, cnn_tokens* tokens) {
+  const at::Tensor& t = any_tensor(o, true);
+  if (t.dim() != dims) {
+    PyErr_Format(PyExc_ValueError, "expected %d dimensions, got %d", dims, (int)t.dim());
+    throw Raised();
+  }
+  for (int i = 0; i < dims; ++i)
+    if (t.size(i) > INT_MAX) raise(PyExc_ValueError, "a dimension is too large");
+  if (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1) raise(PyExc_ValueError, "expected a last dimension without gaps");
+  *tokens = {t.data_ptr(), t.stride(0), dims == 3 ? t.stride(1) : 0};
+  return t;
+}
+
+const cnn_tokens& same_tokens(PyObject* o, cnn_tokens* tokens, const at::Tensor& x) {
+  const at::Tensor& t = on(tokens_tensor(o, (int)x.dim(), tokens), x.device());
+  if (t.scalar_type() != x.scalar_type() || t.sizes() != x.sizes()) raise(PyExc_ValueError, "expected tensors of one shape and type");
+  return *tokens;
+}
+
+// A contiguous tensor of a type and shape, on a device.
+void* optional_on(PyObject* o, at::IntArrayRef sizes, at::ScalarType type, at::Device device, const char* what) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = on(any_tensor(o), device);
+  if (t.scalar_type() != type || t.sizes() != sizes) {
+    PyErr_Format(PyExc_ValueError, "expected %s of another shape or type", what);
+    throw Raised();
+  }
+  return t.data_ptr();
+}
+
+struct Conv {
+  cnn_causal_conv_shape shape;
+  cnn_tokens tokens;
+  const at::Tensor& x;
+  const float *weight, *bias;
+  int64_t B, T, D, K;
+};
+
+Conv conv_of(PyObject* const* a, int dims) {  // x, weight, bias or None, silu
+  cnn_tokens tokens;
+  const at::Tensor &x = tokens_tensor(a[0], dims, &tokens), &w = on(tensor(a[1]), x.device());
+  const int type = element_type(x);
+  const int64_t B = x.size(0), T = dims == 3 ? x.size(1) : 1, D = x.size(dims - 1);
+  if (w.dim() != 2 || w.size(0) != D || w.size(1) > INT_MAX) raise(PyExc_ValueError, "expected a weight of a few taps for each channel");
+  const int64_t K = w.size(1);
+  const float* bias = static_cast<const float*>(optional_on(a[2], {D}, at::kFloat, x.device(), "a bias"));
+  return {{(int)B, (int)T, (int)D, (int)K, type, integer(a[3]) != 0}, tokens, x, data(w), bias, B, T, D, K};
+}
+
+const int32_t* lengths_on(PyObject* o, int64_t count, at::Device device, const char* what) {
+  return static_cast<const int32_t*>(optional_on(o, {count}, at::kInt, device, what));
+}
+
+CALL(causal_conv_fwd, 7)  // x, weight, bias or None, silu, lengths or None, initial state or None, want_state
+  const Conv c = conv_of(a, 3);
+  const at::Device device = c.x.device();
+  const at::ScalarType type = c.x.scalar_type();
+  const int32_t* lengths = lengths_on(a[4], c.B, device, "one length per sequence (torch.int32)");
+  const void* initial = optional_on(a[5], {c.B, c.K - 1, c.D}, type, device, "a state");
+  const c10::DeviceGuard guard(device);
+  at::Tensor y = empty({c.B, c.T, c.D}, device, type), state;
+  if (integer(a[6]) && c.K > 1) state = empty({c.B, c.K - 1, c.D}, device, type);
+  call("cnn_causal_conv_fwd", [&] {
+    return cnn_causal_conv_fwd(&c.shape, &c.tokens, c.weight, c.bias, lengths, initial, y.data_ptr(), state.defined() ? state.data_ptr() : nullptr, stream());
+  });
+  return pair(wrap(std::move(y)), or_none(std::move(state)));
+END
+
+CALL(causal_conv_bwd, 9)  // x, weight, bias or None, silu, d_y, lengths, initial state, error of the final state, want_d_state
+  const Conv c = conv_of(a, 3);
+  const at::Device device = c.x.device();
+  const at::ScalarType type = c.x.scalar_type();
+  cnn_tokens d_tokens;
+  const cnn_tokens& d_y = same_tokens(a[4], &d_tokens, c.x);
+  const int32_t* lengths = lengths_on(a[5], c.B, device, "one length per sequence (torch.int32)");
+  const void* initial = optional_on(a[6], {c.B, c.K - 1, c.D}, type, device, "a state");
+  const void* d_final = optional_on(a[7], {c.B, c.K - 1, c.D}, type, device, "a state's error");
+  const c10::DeviceGuard guard(device);
+  const size_t bytes = cnn_causal_conv_bwd_workspace_bytes(&c.shape);
+  at::Tensor d_x = empty({c.B, c.T, c.D}, device, type), d_weight = empty({c.D, c.K}, device), d_bias, d_state;
+  if (c.bias) d_bias = empty({c.D}, device);
+  if (integer(a[8]) && c.K > 1) d_state = empty({c.B, c.K - 1, c.D}, device, type);
+  const at::Tensor ws = bytes_on(bytes, device);
+  call("cnn_causal_conv_bwd", [&] {
+    return cnn_causal_conv_bwd(&c.shape, &c.tokens, &d_y, c.weight, c.bias, lengths, initial, d_final, d_x.data_ptr(), data(d_weight),
+                               c.bias ? data(d_bias) : nullptr, d_state.defined() ? d_state.data_ptr() : nullptr, bytes ? ws.data_ptr() : nullptr, bytes,
+                               stream());
+  });
+  return pair(pair(object(d_x), object(d_weight)), pair(object(d_bias), object(d_state)));
+END
+
+CALL(causal_conv_step, 6)  // x, weight, bias or None, silu, state, slots or None
+  const Conv c = conv_of(a, 2);
+  const at::Device device = c.x.device();
+  const at::Tensor& state = on(any_tensor(a[4]), device);
+  if (state.dim() != 3 || state.size(1) != c.K - 1 || state.size(2) != c.D || state.scalar_type() != c.x.scalar_type())
+    raise(PyExc_ValueError, "expected a pool of states of another shape or type");
+  const int32_t* slots = lengths_on(a[5], c.B, device, "one slot per sequence (torch.int32)");
+  const c10::DeviceGuard guard(device);
+  at::Tensor y = empty({c.B, c.D}, device, c.x.scalar_type());
+  call("cnn_causal_conv_step", [&] {
+    return cnn_causal_conv_step(&c.shape, &c.tokens, c.weight, c.bias, state.data_ptr(), state.size(0), slots, y.data_ptr(), stream());
+  });
+  return wrap(std::move(y));
+END
+
 PyObject* raise_through(PyObject*, PyObject* fn) {  // binding._check
   Py_INCREF(fn);
   Py_XSETREF(check, fn);
@@ -722,6 +829,7 @@ PyMethodDef methods[] = {FAST(forward), FAST(gradient), FAST(train_batch), FAST(
                          FAST(fc_bwd_weight), FAST(logistic_fwd), FAST(logistic_bwd), FAST(embedding_fwd), FAST(embedding_bwd), FAST(dropout_fwd),
                          FAST(dropout_bwd), FAST(linear_attention_fwd), FAST(linear_attention_bwd), FAST(linear_attention_step),
                          FAST(add_norm_fwd), FAST(add_norm_bwd), FAST(norm_gate_fwd), FAST(norm_gate_bwd), FAST(log_probs_fwd), FAST(log_probs_bwd),
+                         FAST(causal_conv_fwd), FAST(causal_conv_bwd), FAST(causal_conv_step),
                          {"raise_through", raise_through, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

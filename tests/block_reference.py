@@ -62,6 +62,44 @@ def norm_gate_gradient(d_y, x, weight, gate, scale, eps, groups):
     return (d, d_gate, terms.sum(0)), (size, None if gate is None else d_gate.abs() + (scale * d_y * n * weight).abs(), terms.abs().sum(0))
 
 
+# ---- short convolution (x [B, T, D], weight [D, K], states [B, K - 1, D], lengths a list) --------------------------------
+def _inputs(x, initial, b, n, K):
+    head = torch.zeros(K - 1, x.shape[2], dtype=x.dtype) if initial is None else initial[b]
+    return torch.cat([head, x[b, :n]])
+
+
+def conv(x, weight, bias, active, lengths, initial):
+    """(y, final state, p, sums of magnitudes of p)"""
+    (B, T, D), K = x.shape, weight.shape[1]
+    y, p, size, state = torch.zeros_like(x), torch.zeros_like(x), torch.zeros_like(x), torch.zeros(B, K - 1, D, dtype=x.dtype)
+    for b, n in enumerate(lengths):
+        seen = _inputs(x, initial, b, n, K)
+        for t in range(n):
+            terms = torch.cat([seen[t:t + K] * weight.t(), bias[None]])
+            p[b, t], size[b, t] = terms.sum(0), terms.abs().sum(0)
+        state[b] = seen[n:]
+        y[b, :n] = silu(p[b, :n]) if active else p[b, :n]
+    return y, state, p, size
+
+
+def conv_gradient(x, weight, bias, active, lengths, initial, d_y, d_final, off=None):
+    """(d_x, d_weight, d_bias, d_initial) for errors of p in magnitudes where `off` gives them (in place of d_y times silu'), else the gradient."""
+    (B, T, D), K = x.shape, weight.shape[1]
+    p = conv(x, weight, bias, active, lengths, initial)[2]
+    e = (d_y * d_silu(p) if active else d_y) if off is None else off
+    d_x, d_w, d_b, d_first = torch.zeros_like(x), torch.zeros_like(weight), torch.zeros_like(bias), torch.zeros(B, K - 1, D, dtype=x.dtype)
+    for b, n in enumerate(lengths):
+        seen, d_seen = _inputs(x, initial, b, n, K), torch.zeros(K - 1 + n, D, dtype=x.dtype)
+        for k in range(K):
+            d_seen[k:k + n] += e[b, :n] * weight[:, k]
+            d_w[:, k] += (e[b, :n] * seen[k:k + n]).sum(0)
+        if d_final is not None:
+            d_seen[n:] += d_final[b]
+        d_b += e[b, :n].sum(0)
+        d_first[b], d_x[b, :n] = d_seen[:K - 1], d_seen[K - 1:]
+    return d_x, d_w, d_b, d_first
+
+
 # ---- log probabilities (rows [N, V], tokens [N, M]) ----------------------------------------------------------------
 def log_probs(logits, tokens, scale, top):
     """(log probabilities of the tokens, entropy, log probabilities of the top ones, their tokens, all log probabilities)"""

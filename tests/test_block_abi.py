@@ -55,6 +55,39 @@ def test_norm_workspaces():
     assert q(norm(rows=1 << 20, groups=64, width=16384)) == 4 * 64 * 16384 * 4
 
 
+def conv(B=3, T=50, D=20, K=4, type_=1, silu=1):
+    return binding.CausalConvShape(B, T, D, K, type_, silu)
+
+
+def tokens(data=0x1002, batch=1000, token=20):
+    return binding.Tokens(data, batch, token)
+
+
+BAD_CONVS = [{"B": 0}, {"T": 0}, {"D": 0}, {"D": (1 << 20) + 1}, {"K": 1}, {"K": 9}, {"type_": 3}, {"type_": -1}, {"B": 1 << 16, "T": 1 << 15}]
+BAD_TOKENS = [tokens(data=0), tokens(data=0x1001), tokens(batch=-1), tokens(token=-1)]
+
+
+def test_conv_refusals():
+    L = binding.lib()
+    fwd = lambda s=conv(), x=tokens(), w=fake, b=fake, n=fake, i=fake, y=fake, f=fake: L.cnn_causal_conv_fwd(s, x, w, b, n, i, y, f, nul)  # noqa: E731
+    bwd = lambda s=conv(), x=tokens(), d=tokens(), w=fake, b=fake, n=fake, i=fake, f=fake, dx=fake, dw=fake, db=fake, di=fake, ws=fake, size=1 << 40: (  # noqa: E731
+        L.cnn_causal_conv_bwd(s, x, d, w, b, n, i, f, dx, dw, db, di, ws, size, nul))
+    step = lambda s=conv(T=1), x=tokens(), w=fake, b=fake, st=fake, pool=3, slots=nul, y=fake: L.cnn_causal_conv_step(s, x, w, b, st, pool, slots, y, nul)  # noqa: E731
+    assert fwd(s=None) == fwd(x=None) == bwd(s=None) == bwd(x=None) == bwd(d=None) == step(s=None) == step(x=None) == EINVAL
+    for bad in BAD_CONVS:
+        assert fwd(s=conv(**bad)) == bwd(s=conv(**bad)) == EINVAL and L.cnn_causal_conv_bwd_workspace_bytes(conv(**bad)) == 0, bad
+        if "T" not in bad:
+            assert step(s=conv(**{"T": 1, **bad})) == EINVAL, bad
+    for x in BAD_TOKENS:
+        assert fwd(x=x) == bwd(x=x) == bwd(d=x) == step(x=x) == EINVAL
+    for p in (nul, odd):
+        assert fwd(w=p) == fwd(y=p) == bwd(w=p) == bwd(dx=p) == bwd(dw=p) == bwd(ws=p) == step(w=p) == step(st=p) == step(y=p) == EINVAL
+    assert fwd(b=odd) == fwd(n=odd) == fwd(i=odd) == fwd(f=odd) == bwd(b=odd) == bwd(n=odd) == bwd(i=odd) == bwd(f=odd) == bwd(db=odd) == bwd(di=odd) == EINVAL
+    assert step(b=odd) == step(slots=odd) == step(pool=0) == step(pool=2) == step(s=conv(T=2)) == step(pool=(1 << 30) + 1) == EINVAL
+    need = L.cnn_causal_conv_bwd_workspace_bytes(conv())
+    assert need % (20 * 5 * 4) == 0 and 0 < need and bwd(size=need - 1) == EWS and L.cnn_causal_conv_bwd_workspace_bytes(None) == 0
+
+
 def logp(rows=100, vocab=1000, given=2, top=5, type_=1, wide=1, scale=1.0):
     return binding.LogProbsShape(rows, vocab, given, top, type_, wide, scale)
 

@@ -37,6 +37,18 @@ def test_norms(groups):
     close(d_w, differences(lambda v: [ref.norm_gate(x, v, gate, res, 0.7, 1e-3, groups)], w, [d_y]))
 
 
+@pytest.mark.parametrize("active", [True, False])
+def test_conv(active):
+    x, w, b, first = normal(2, 5, 3), normal(3, 4, seed=1), normal(3, seed=2), normal(2, 3, 3, seed=3)
+    d_y, d_last, n = normal(2, 5, 3, seed=4), normal(2, 3, 3, seed=5), [5, 1]
+    grads = ref.conv_gradient(x, w, b, active, n, first, d_y, d_last)
+    for got, (at, make) in zip(grads, [(x, lambda v: (v, w, b, first)), (w, lambda v: (x, v, b, first)), (b, lambda v: (x, w, v, first)), (first, lambda v: (x, w, b, v))]):
+        def fn(v):
+            x_, w_, b_, first_ = make(v)
+            return ref.conv(x_, w_, b_, active, n, first_)[:2]
+        close(got, differences(fn, at, (d_y, d_last)))
+
+
 def test_log_probs():
     logits, tokens = normal(3, 7), torch.tensor([[0, 0, 6], [3, -1, 9], [2, 2, 2]])
     logits[1, 4] = -float("inf")
