@@ -413,6 +413,35 @@ int cnn_causal_conv_bwd(const cnn_causal_conv_shape* shape, const cnn_tokens* x,
 int cnn_causal_conv_step(const cnn_causal_conv_shape* shape, const cnn_tokens* x, const float* weight, const float* bias, void* state, int64_t pool,
                          const int32_t* slots, void* y, void* hip_stream);
 
+/* Selective state space scan: N states to each channel d of a sequence, whose decays the data choose,
+ *   D_t = softplus(dt_t + dt_bias), or dt_t + dt_bias with softplus == 0,   h_t[n] = exp(D_t a[d,n]) h_{t-1}[n] + D_t x_t b_t[n],
+ *   y_t = sum_n c_t[n] h_t[n] + skip[d] x_t,   t = 0 .. length - 1,   softplus(z) = ln(1 + exp(z)).
+ * a[D,N], skip[D], dt_bias[D] (the last two nullable: zeros) are fp32; a below 0 and D_t above make decays of at most 1, which is not checked.  x and dt (and
+ * d_y) as cnn_tokens of `type`; b and c [B,T,G,N] as cnn_heads, D a multiple of G, D / G consecutive channels to a group.  Results y, d_x, d_dt [B,T,D] and
+ * d_b, d_c [B,T,G,N] are contiguous; states [B,D,N] are fp32, an initial or final one may be NULL (zero; not wanted), and they may be the same memory.  lengths
+ * as for cnn_causal_conv_fwd.  1 <= N <= 128, B * D <= 2^24, B * T < 2^31, D <= 2^20.  Inputs up to a sequence's length must be finite: one that is not
+ * makes results NaN that the formulas leave finite, also of tokens before it, of its own channel and, backward, its group's d_b and d_c.  Everything is
+ * computed in fp32 and rounded once; a decay below 2^-126 counts as 0.  `workspace` holds states of pieces of the sequences, and backward partial sums; its size query returns 0 where none is
+ * needed and for refused shapes. */
+typedef struct {
+  int B, T, D, N, G, type, softplus;
+} cnn_selective_scan_shape;
+size_t cnn_selective_scan_fwd_workspace_bytes(const cnn_selective_scan_shape* shape);
+int cnn_selective_scan_fwd(const cnn_selective_scan_shape* shape, const cnn_tokens* x, const cnn_tokens* dt, const float* a, const cnn_heads* b,
+                           const cnn_heads* c, const float* skip, const float* dt_bias, const int32_t* lengths, const float* initial_state, void* y,
+                           float* final_state, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Gradients for the error d_y of y and (nullable) d_final_state of the final state; d_skip, d_dt_bias and d_initial_state may be NULL (not wanted), and
+ * d_initial_state must not be the memory of an input.  Sums over tokens and channels are fp32 in an order that the shape fixes. */
+size_t cnn_selective_scan_bwd_workspace_bytes(const cnn_selective_scan_shape* shape);
+int cnn_selective_scan_bwd(const cnn_selective_scan_shape* shape, const cnn_tokens* x, const cnn_tokens* dt, const float* a, const cnn_heads* b,
+                           const cnn_heads* c, const cnn_tokens* d_y, const float* skip, const float* dt_bias, const int32_t* lengths,
+                           const float* initial_state, const float* d_final_state, void* d_x, void* d_dt, float* d_a, void* d_b, void* d_c, float* d_skip,
+                           float* d_dt_bias, float* d_initial_state, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* One token of every sequence (T = 1, token strides unused): state[pool,D,N] is updated in place, y[B,D].  Slots as for cnn_linear_attention_step. */
+int cnn_selective_scan_step(const cnn_selective_scan_shape* shape, const cnn_tokens* x, const cnn_tokens* dt, const float* a, const cnn_heads* b,
+                            const cnn_heads* c, const float* skip, const float* dt_bias, float* state, int64_t pool, const int32_t* slots, void* y,
+                            void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

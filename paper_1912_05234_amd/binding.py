@@ -109,12 +109,18 @@ class CausalConvShape(ctypes.Structure):
     _fields_ = [(name, _i) for name in ("B", "T", "D", "K", "type", "silu")]
 
 
+class SelectiveScanShape(ctypes.Structure):
+    """cnn_selective_scan_shape"""
+    _fields_ = [(name, _i) for name in ("B", "T", "D", "N", "G", "type", "softplus")]
+
+
 class Tokens(ctypes.Structure):
     """cnn_tokens"""
     _fields_ = [("data", _vp), ("batch", _i64), ("token", _i64)]
 
 
 _conv, _tokens = ctypes.POINTER(CausalConvShape), ctypes.POINTER(Tokens)
+_select = ctypes.POINTER(SelectiveScanShape)
 _norm, _logp, _rows = ctypes.POINTER(NormShape), ctypes.POINTER(LogProbsShape), ctypes.POINTER(Rows)
 SIGNATURES.update({
     "cnn_add_norm_fwd": (_i, [_norm] + [_rows] * 2 + [_vp] * 4),
@@ -128,6 +134,11 @@ SIGNATURES.update({
     "cnn_causal_conv_fwd": (_i, [_conv, _tokens] + [_vp] * 7),
     "cnn_causal_conv_bwd_workspace_bytes": (_sz, [_conv]),
     "cnn_causal_conv_bwd": (_i, [_conv, _tokens, _tokens] + [_vp] * 10 + [_sz, _vp]),
+    "cnn_selective_scan_fwd_workspace_bytes": (_sz, [_select]),
+    "cnn_selective_scan_fwd": (_i, [_select, _tokens, _tokens, _vp, _heads, _heads] + [_vp] * 7 + [_sz, _vp]),
+    "cnn_selective_scan_bwd_workspace_bytes": (_sz, [_select]),
+    "cnn_selective_scan_bwd": (_i, [_select, _tokens, _tokens, _vp, _heads, _heads, _tokens] + [_vp] * 14 + [_sz, _vp]),
+    "cnn_selective_scan_step": (_i, [_select, _tokens, _tokens, _vp, _heads, _heads] + [_vp] * 3 + [_i64] + [_vp] * 3),
     "cnn_causal_conv_step": (_i, [_conv, _tokens] + [_vp] * 3 + [_i64] + [_vp] * 3),
 })
 
@@ -425,6 +436,27 @@ def causal_conv_step(x, weight, state, bias=None, silu=False, slots=None):
     """y[B, D] of one token x[B, D] of every sequence; state[pool, K - 1, D] is moved on in place, row b using state slots[b] (int32; None:
     state b).  A slot outside the pool: a row without a sequence, its y is zero.  No two rows may have the same slot."""
     return (_calls or _native()).causal_conv_step(x, weight, bias, bool(silu), state, slots)
+
+
+# ---- selective scan --------------------------------------------------------------------
+def selective_scan_fwd(x, dt, a, b, c, skip=None, dt_bias=None, softplus=True, lengths=None, initial_state=None, want_state=False):
+    """(y[B, T, D], final state [B, D, N] fp32 or None) of h_t = exp(D_t a) h_{t-1} + D_t x_t b_t, y_t = sum_n c_t h_t + skip x_t with D_t = softplus(dt_t +
+    dt_bias), or dt_t + dt_bias, for x, dt[B, T, D] and b, c[B, T, G, N] of any strides but the last (D / G channels to a group), a[D, N], skip[D] and
+    dt_bias[D] fp32, lengths[B] int32 (None: all T)."""
+    return (_calls or _native()).selective_scan_fwd(x, dt, a, b, c, skip, dt_bias, bool(softplus), lengths, initial_state, bool(want_state))
+
+
+def selective_scan_bwd(x, dt, a, b, c, d_y, skip=None, dt_bias=None, softplus=True, lengths=None, initial_state=None, d_final_state=None,
+                       want_d_state=False):
+    """(d_x, d_dt, d_a, d_b, d_c, d_skip or None, d_dt_bias or None, error of the initial state or None) of the call above with the same arguments."""
+    return (_calls or _native()).selective_scan_bwd(x, dt, a, b, c, skip, dt_bias, bool(softplus), d_y, lengths, initial_state, d_final_state,
+                                                    bool(want_d_state))
+
+
+def selective_scan_step(x, dt, a, b, c, state, skip=None, dt_bias=None, softplus=True, slots=None):
+    """y[B, D] of one token of every sequence, x, dt[B, D], b, c[B, G, N]; state[pool, D, N] fp32 is updated in place, row b using state slots[b]
+    (int32; None: state b).  A slot outside the pool: a row without a sequence, its y is zero.  No two rows may have the same slot."""
+    return (_calls or _native()).selective_scan_step(x, dt, a, b, c, skip, dt_bias, bool(softplus), state, slots)
 
 
 # ---- log probabilities -----------------------------------------------------------------

@@ -1,9 +1,6 @@
+// The norms' kernels for one element type (a file to each, so that they compile side by side).
 #include "cnn_norm.h"
 
-namespace cnn {
-namespace norm {
-void launch_bf16(const Args& a, int stream_type, Mode mode, bool backward, Cut cut, unsigned grid, hipStream_t st) {
+void cnn::norm::launch_bf16(const Args& a, int stream_type, Mode mode, bool backward, Cut cut, unsigned grid, hipStream_t st) {
   launch_type<__bf16>(a, stream_type, mode, backward, cut, grid, st);
 }
-}  // namespace norm
-}  // namespace cnn

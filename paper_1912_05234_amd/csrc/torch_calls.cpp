@@ -817,6 +817,92 @@ CALL(causal_conv_step, 6)  // x, weight, bias or None, silu, state, slots or Non
   return wrap(std::move(y));
 END
 
+struct Scan {
+  cnn_selective_scan_shape shape;
+  cnn_tokens x, dt;
+  cnn_heads b, c;
+  const float *a, *skip, *dt_bias;
+  const at::Tensor& first;  // x
+  at::Device device;
+  at::ScalarType type;
+  int64_t B, T, D, N, G;
+};
+
+Scan scan_of(PyObject* const* a, int dims) {  // x, dt, a, b, c, skip or None, dt_bias or None, softplus
+  cnn_tokens x, dt;
+  const at::Tensor& t = tokens_tensor(a[0], dims, &x);
+  const at::Device device = t.device();
+  const at::ScalarType type = t.scalar_type();
+  const int code = element_type(t);
+  same_tokens(a[1], &dt, t);
+  const at::Tensor &b = on(heads_tensor(a[3], dims + 1, type), device), &c = on(heads_tensor(a[4], dims + 1, type), device), &w = on(tensor(a[2]), device);
+  const int64_t B = t.size(0), T = dims == 3 ? t.size(1) : 1, D = t.size(dims - 1), G = b.size(dims - 1), N = b.size(dims);
+  if (b.sizes() != c.sizes() || b.size(0) != B || (dims == 3 && b.size(1) != T)) raise(PyExc_ValueError, "expected b and c of one shape, of x's batch and length");
+  for (const int64_t n : {G, N})
+    if (n > INT_MAX) raise(PyExc_ValueError, "a dimension is too large");
+  if (w.sizes() != at::IntArrayRef({D, N})) raise(PyExc_ValueError, "expected a of as many rows as channels and as many columns as b and c");
+  const float* skip = static_cast<const float*>(optional_on(a[5], {D}, at::kFloat, device, "a skip"));
+  const float* bias = static_cast<const float*>(optional_on(a[6], {D}, at::kFloat, device, "a bias"));
+  return {{(int)B, (int)T, (int)D, (int)N, (int)G, code, integer(a[7]) != 0}, x, dt, heads_of(b), heads_of(c), data(w), skip, bias, t, device, type, B, T, D, N, G};
+}
+
+CALL(selective_scan_fwd, 11)  // as scan_of, lengths or None, initial state or None, want_state
+  const Scan s = scan_of(a, 3);
+  const int32_t* lengths = lengths_on(a[8], s.B, s.device, "one length per sequence (torch.int32)");
+  const float* initial = static_cast<const float*>(optional_on(a[9], {s.B, s.D, s.N}, at::kFloat, s.device, "a state"));
+  const c10::DeviceGuard guard(s.device);
+  const size_t bytes = cnn_selective_scan_fwd_workspace_bytes(&s.shape);
+  at::Tensor y = empty({s.B, s.T, s.D}, s.device, s.type), state;
+  if (integer(a[10])) state = empty({s.B, s.D, s.N}, s.device);
+  const at::Tensor ws = bytes_on(bytes, s.device);
+  call("cnn_selective_scan_fwd", [&] {
+    return cnn_selective_scan_fwd(&s.shape, &s.x, &s.dt, s.a, &s.b, &s.c, s.skip, s.dt_bias, lengths, initial, y.data_ptr(),
+                                  state.defined() ? data(state) : nullptr, bytes ? ws.data_ptr() : nullptr, bytes, stream());
+  });
+  return pair(wrap(std::move(y)), or_none(std::move(state)));
+END
+
+CALL(selective_scan_bwd, 13)  // as scan_of, d_y, lengths, initial state, error of the final state, want_d_state
+  const Scan s = scan_of(a, 3);
+  cnn_tokens d_y;
+  same_tokens(a[8], &d_y, s.first);
+  const int32_t* lengths = lengths_on(a[9], s.B, s.device, "one length per sequence (torch.int32)");
+  const float* initial = static_cast<const float*>(optional_on(a[10], {s.B, s.D, s.N}, at::kFloat, s.device, "a state"));
+  const float* d_final = static_cast<const float*>(optional_on(a[11], {s.B, s.D, s.N}, at::kFloat, s.device, "a state's error"));
+  const c10::DeviceGuard guard(s.device);
+  const size_t bytes = cnn_selective_scan_bwd_workspace_bytes(&s.shape);
+  at::Tensor d_x = empty({s.B, s.T, s.D}, s.device, s.type), d_dt = empty({s.B, s.T, s.D}, s.device, s.type), d_a = empty({s.D, s.N}, s.device);
+  at::Tensor d_b = empty({s.B, s.T, s.G, s.N}, s.device, s.type), d_c = empty({s.B, s.T, s.G, s.N}, s.device, s.type), d_skip, d_bias, d_state;
+  if (s.skip) d_skip = empty({s.D}, s.device);
+  if (s.dt_bias) d_bias = empty({s.D}, s.device);
+  if (integer(a[12])) d_state = empty({s.B, s.D, s.N}, s.device);
+  const at::Tensor ws = bytes_on(bytes, s.device);
+  const auto or_null = [](const at::Tensor& t) { return t.defined() ? data(t) : nullptr; };
+  call("cnn_selective_scan_bwd", [&] {
+    return cnn_selective_scan_bwd(&s.shape, &s.x, &s.dt, s.a, &s.b, &s.c, &d_y, s.skip, s.dt_bias, lengths, initial, d_final, d_x.data_ptr(), d_dt.data_ptr(),
+                                  data(d_a), d_b.data_ptr(), d_c.data_ptr(), or_null(d_skip), or_null(d_bias), or_null(d_state),
+                                  bytes ? ws.data_ptr() : nullptr, bytes, stream());
+  });
+  PyObject* all = PyTuple_New(8);
+  if (!all) throw Raised();
+  int i = 0;
+  for (const at::Tensor* t : {&d_x, &d_dt, &d_a, &d_b, &d_c, &d_skip, &d_bias, &d_state}) PyTuple_SET_ITEM(all, i++, object(*t));
+  return all;
+END
+
+CALL(selective_scan_step, 10)  // as scan_of, state, slots or None
+  const Scan s = scan_of(a, 2);
+  const at::Tensor& state = on(tensor(a[8], 3), s.device);
+  if (state.size(1) != s.D || state.size(2) != s.N) raise(PyExc_ValueError, "expected a pool of states of another shape");
+  const int32_t* slots = lengths_on(a[9], s.B, s.device, "one slot per sequence (torch.int32)");
+  const c10::DeviceGuard guard(s.device);
+  at::Tensor y = empty({s.B, s.D}, s.device, s.type);
+  call("cnn_selective_scan_step", [&] {
+    return cnn_selective_scan_step(&s.shape, &s.x, &s.dt, s.a, &s.b, &s.c, s.skip, s.dt_bias, data(state), state.size(0), slots, y.data_ptr(), stream());
+  });
+  return wrap(std::move(y));
+END
+
 PyObject* raise_through(PyObject*, PyObject* fn) {  // binding._check
   Py_INCREF(fn);
   Py_XSETREF(check, fn);
@@ -830,6 +916,7 @@ PyMethodDef methods[] = {FAST(forward), FAST(gradient), FAST(train_batch), FAST(
                          FAST(dropout_bwd), FAST(linear_attention_fwd), FAST(linear_attention_bwd), FAST(linear_attention_step),
                          FAST(add_norm_fwd), FAST(add_norm_bwd), FAST(norm_gate_fwd), FAST(norm_gate_bwd), FAST(log_probs_fwd), FAST(log_probs_bwd),
                          FAST(causal_conv_fwd), FAST(causal_conv_bwd), FAST(causal_conv_step),
+                         FAST(selective_scan_fwd), FAST(selective_scan_bwd), FAST(selective_scan_step),
                          {"raise_through", raise_through, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -3,6 +3,7 @@ with its gradient written out, and the sums of magnitudes that bound a computati
 import torch
 
 U = 2.0 ** -24  # one rounding of fp32
+LEAST = 2.0 ** -126  # its smallest normal number
 
 
 def silu(z):
@@ -98,6 +99,76 @@ def conv_gradient(x, weight, bias, active, lengths, initial, d_y, d_final, off=N
         d_b += e[b, :n].sum(0)
         d_first[b], d_x[b, :n] = d_seen[:K - 1], d_seen[K - 1:]
     return d_x, d_w, d_b, d_first
+
+
+# ---- selective scan (x, dt [B, T, D], a [D, N], b, c [B, T, G, N], states [B, D, N], lengths a list) ---------------------------
+def softplus(z):
+    return torch.logaddexp(z, torch.zeros_like(z))
+
+
+def scan(x, dt, a, b, c, skip, dt_bias, soft, lengths, initial, d_y=None, d_final=None):
+    """((y, final state), their errors in 32 bits), and with d_y the gradients (d_x, d_dt, d_a, d_b, d_c, d_skip, d_dt_bias, d_initial) and theirs.
+
+    Errors are carried along, in roundings U of what is added.  z is rounded once and the exponent of softplus twice, so D is off by (3 |z| + 8) U of
+    itself (by U |z| without softplus), a decay by |D a| (3 |z| + 10) + 2 roundings, D x b by 3 |z| + 11; where sequences are cut, a segment's decay
+    from the sum of its D is off by no more, and a decay below 2^-126, the smallest normal number, may be 0.  So a state's error, and an adjoint's, is the last one's decayed and (|D a| + 1) (3 |z| + 12) + 4 roundings of its magnitude.  Sums over n take up to N
+    + 4 roundings, over channels 6 of a wave and D / 4 of waves, over tokens and sequences 64 of a segment, 32 + 64 of the rest."""
+    (B, T, D), (G, N) = x.shape, b.shape[2:]
+    zeros = lambda *s: torch.zeros(s, dtype=x.dtype)  # noqa: E731
+    b, c = b.repeat_interleave(D // G, 2), c.repeat_interleave(D // G, 2)
+    inside = torch.arange(T)[None, :] < torch.tensor(lengths)[:, None]
+    z = dt + dt_bias
+    delta = torch.where(inside[..., None], softplus(z) if soft else z, 0.0)
+    rough = (3 * z.abs() + 12)[..., None] * U  # of D, of products with it
+    x = torch.where(inside[..., None], x, 0.0)
+    b, c = torch.where(inside[..., None, None], b, 0.0), torch.where(inside[..., None, None], c, 0.0)
+    h, size, off = (zeros(B, D, N) if initial is None else initial), zeros(B, D, N) if initial is None else initial.abs(), zeros(B, D, N)
+    hs, sizes, offs, decays, steps = [h], [size], [off], [], []
+    for t in range(T):
+        decay, u = torch.exp(delta[:, t, :, None] * a), (delta[:, t] * x[:, t])[..., None] * b[:, t]
+        step = ((delta[:, t, :, None] * a).abs() + 1) * rough[:, t] + 4 * U
+        h, size = decay * h + u, decay * size + u.abs()
+        off = decay * off + size * step + LEAST * sizes[-1]
+        hs.append(h), sizes.append(size), offs.append(off), decays.append(decay), steps.append(step)
+    stack = lambda v: torch.stack(v, 1)  # noqa: E731
+    H, M, E, A, S = stack(hs), stack(sizes), stack(offs), stack(decays), stack(steps)
+    y = (H[:, 1:] * c).sum(3) + skip * x
+    y_off = (c.abs() * (E[:, 1:] + (N + 4) * U * M[:, 1:])).sum(3) + 2 * U * (skip * x).abs()
+    forward = (torch.where(inside[..., None], y, 0.0), H[:, -1]), (torch.where(inside[..., None], y_off, 0.0), E[:, -1])
+    if d_y is None:
+        return forward
+    d_y = torch.where(inside[..., None], d_y, 0.0)
+    q, q_size, q_off = (zeros(B, D, N) if d_final is None else d_final), zeros(B, D, N) if d_final is None else d_final.abs(), zeros(B, D, N)
+    gs, g_sizes, g_offs = [], [], []
+    for t in reversed(range(T)):
+        g, g_size = q + c[:, t] * d_y[:, t, :, None], q_size + (c[:, t] * d_y[:, t, :, None]).abs()
+        g_off = q_off + 2 * U * g_size
+        q, q_size, q_off = A[:, t] * g, A[:, t] * g_size, A[:, t] * (g_off + g_size * S[:, t]) + LEAST * g_size
+        gs.append(g), g_sizes.append(g_size), g_offs.append(g_off)
+    back = lambda v: torch.stack(v[::-1], 1)  # noqa: E731
+    g, gm, ge = back(gs), back(g_sizes), back(g_offs)
+    sums = (N + 8) * U
+    gb, gb_size = (g * b).sum(3), (gm * b.abs()).sum(3)
+    gb_off = (ge * b.abs()).sum(3) + sums * gb_size
+    along, along_size = A * g * H[:, :-1], A * gm * M[:, :-1]
+    along_off = A * (ge * M[:, :-1] + gm * E[:, :-1]) + along_size * S + LEAST * gm * M[:, :-1]
+    r, d_size = rough[..., 0], delta.abs()
+    d_x, d_x_off = delta * gb + skip * d_y, d_size * (gb_off + r * gb_size) + 2 * U * (skip * d_y).abs()
+    dd = x * gb + (along * a).sum(3)
+    dd_size = x.abs() * gb_size + (along_size * a.abs()).sum(3)
+    dd_off = x.abs() * gb_off + (a.abs() * (along_off + sums * along_size)).sum(3) + 3 * U * dd_size
+    slope = 1 / (1 + torch.exp(-z)) if soft else torch.ones_like(z)
+    d_dt, d_dt_size, d_dt_off = dd * slope, dd_size * slope, slope * (dd_off + r * dd_size)
+    share = lambda v: v.unflatten(2, (G, D // G)).sum(3)  # noqa: E731
+    u, u_size = (delta * x)[..., None], (delta * x)[..., None].abs()
+    channels, tokens = (6 + D / 4) * U, (64 + 32 + 64) * U
+    total = lambda v: v.sum((0, 1))  # noqa: E731
+    masked = lambda v: torch.where(inside[..., None], v, 0.0)  # noqa: E731
+    grads = (masked(d_x), masked(d_dt), total(along * delta[..., None]), share(g * u), share(H[:, 1:] * d_y[..., None]), total(d_y * x), total(masked(d_dt)), q)
+    off = (masked(d_x_off), masked(d_dt_off), total(d_size[..., None] * (along_off + along_size * (rough + tokens))),
+           share(u_size * (ge + gm * (rough + channels))), share(d_y[..., None].abs() * (E[:, 1:] + channels * M[:, 1:])), tokens * total((d_y * x).abs()),
+           total(masked(d_dt_off + tokens * d_dt_size)), q_off)
+    return forward, (grads, off)
 
 
 # ---- log probabilities (rows [N, V], tokens [N, M]) ----------------------------------------------------------------

@@ -88,6 +88,59 @@ def test_conv_refusals():
     assert need % (20 * 5 * 4) == 0 and 0 < need and bwd(size=need - 1) == EWS and L.cnn_causal_conv_bwd_workspace_bytes(None) == 0
 
 
+def scan(B=3, T=50, D=20, N=16, G=2, type_=1, soft=1):
+    return binding.SelectiveScanShape(B, T, D, N, G, type_, soft)
+
+
+def heads(data=0x1002, batch=1600, token=32, head=16):
+    return binding.Heads(data, batch, token, head)
+
+
+BAD_SCANS = [{"B": 0}, {"T": 0}, {"D": 0}, {"N": 0}, {"N": 129}, {"G": 0}, {"G": 3}, {"type_": 3}, {"type_": -1}, {"B": 1 << 20, "T": 1, "D": 32}, {"B": 1 << 16, "T": 1 << 15}]
+BAD_HEADS = [heads(data=0), heads(data=0x1001), heads(batch=-1), heads(token=-1), heads(head=-1)]
+
+
+def test_scan_refusals():
+    L = binding.lib()
+    fwd = lambda s=scan(), x=tokens(), dt=tokens(), a=fake, b=heads(), c=heads(), k=fake, z=fake, n=fake, i=fake, y=fake, f=fake, ws=fake, size=1 << 40: (  # noqa: E731
+        L.cnn_selective_scan_fwd(s, x, dt, a, b, c, k, z, n, i, y, f, ws, size, nul))
+    bwd = lambda s=scan(), x=tokens(), dt=tokens(), a=fake, b=heads(), c=heads(), d=tokens(), k=fake, z=fake, n=fake, i=fake, f=fake, o=(fake,) * 8, ws=fake, size=1 << 40: (  # noqa: E731
+        L.cnn_selective_scan_bwd(s, x, dt, a, b, c, d, k, z, n, i, f, *o, ws, size, nul))
+    step = lambda s=scan(T=1), x=tokens(), dt=tokens(), a=fake, b=heads(), c=heads(), k=fake, z=fake, st=fake, pool=3, slots=nul, y=fake: (  # noqa: E731
+        L.cnn_selective_scan_step(s, x, dt, a, b, c, k, z, st, pool, slots, y, nul))
+    assert fwd(s=None) == bwd(s=None) == step(s=None) == EINVAL
+    for bad in BAD_SCANS:
+        s = scan(**bad)
+        assert fwd(s=s) == bwd(s=s) == EINVAL and L.cnn_selective_scan_fwd_workspace_bytes(s) == L.cnn_selective_scan_bwd_workspace_bytes(s) == 0, bad
+        if bad.get("T", 1) == 1:
+            assert step(s=scan(**{"T": 1, **bad})) == EINVAL, bad
+    for x in [None] + BAD_TOKENS:
+        assert fwd(x=x) == fwd(dt=x) == bwd(x=x) == bwd(dt=x) == bwd(d=x) == step(x=x) == step(dt=x) == EINVAL
+    for h in [None] + BAD_HEADS:
+        assert fwd(b=h) == fwd(c=h) == bwd(b=h) == bwd(c=h) == step(b=h) == step(c=h) == EINVAL
+    for p in (nul, odd):
+        assert fwd(a=p) == fwd(y=p) == bwd(a=p) == bwd(ws=p) == step(a=p) == step(st=p) == step(y=p) == EINVAL
+        for i in range(5):
+            assert bwd(o=(fake,) * i + (p,) + (fake,) * (7 - i)) == EINVAL, i
+    for name in ("k", "z", "n", "i"):
+        assert fwd(**{name: odd}) == bwd(**{name: odd}) == EINVAL
+    assert fwd(f=odd) == fwd(ws=odd) == bwd(f=odd) == bwd(o=(fake,) * 5 + (odd, fake, fake)) == bwd(o=(fake,) * 7 + (odd,)) == step(k=odd) == step(z=odd) == EINVAL
+    assert step(slots=odd) == step(pool=0) == step(pool=2) == step(s=scan(T=2)) == step(pool=(1 << 30) + 1) == EINVAL
+    need = L.cnn_selective_scan_bwd_workspace_bytes(scan())
+    assert need and bwd(size=need - 1) == EWS
+    long = scan(B=1, T=8192)
+    need = L.cnn_selective_scan_fwd_workspace_bytes(long)
+    assert need and fwd(s=long, size=need - 1) == fwd(s=long, ws=nul) == EWS
+
+
+def test_scan_workspaces():
+    """Forward none where the channels fill the chip, or a sequence is short; backward always, for the partial sums."""
+    L = binding.lib()
+    fwd, bwd = L.cnn_selective_scan_fwd_workspace_bytes, L.cnn_selective_scan_bwd_workspace_bytes
+    assert fwd(scan(T=64)) == 0 and fwd(scan(B=128, T=10000, D=2048)) == 0 and fwd(None) == bwd(None) == 0
+    assert bwd(scan(T=1)) > 0 and bwd(scan(T=8192)) > 128 * 3 * 20 * 16 * 4 * 2
+
+
 def logp(rows=100, vocab=1000, given=2, top=5, type_=1, wide=1, scale=1.0):
     return binding.LogProbsShape(rows, vocab, given, top, type_, wide, scale)
 

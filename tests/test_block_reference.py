@@ -49,6 +49,26 @@ def test_conv(active):
         close(got, differences(fn, at, (d_y, d_last)))
 
 
+@pytest.mark.parametrize("soft", [True, False])
+def test_scan(soft):
+    x, dt, a, b, c = normal(2, 4, 6), normal(2, 4, 6, seed=1).abs(), -normal(6, 3, seed=2).abs(), normal(2, 4, 2, 3, seed=3), normal(2, 4, 2, 3, seed=4)
+    skip, bias, first = normal(6, seed=5), normal(6, seed=6), normal(2, 6, 3, seed=7)
+    d_y, d_last, n = normal(2, 4, 6, seed=8), normal(2, 6, 3, seed=9), [4, 1]
+    args = [x, dt, a, b, c, skip, bias, first]
+    run = lambda *v, **k: ref.scan(*v[:7], soft, n, v[7], **k)  # noqa: E731
+    grads = run(*args, d_y=d_y, d_final=d_last)[1][0]
+    for i, got in enumerate(grads):
+        def fn(v):
+            return run(*args[:i], v, *args[i + 1:])[0]
+        close(got, differences(fn, args[i], (d_y, d_last)))
+    y, state = run(*args)[0]  # the definition, one number at a time
+    h = first[1, 4].clone()
+    d = dt[1, 0, 4] + bias[4]
+    d = torch.log1p(torch.exp(d)) if soft else d
+    h = torch.exp(d * a[4]) * h + d * x[1, 0, 4] * b[1, 0, 1]
+    assert torch.allclose(state[1, 4], h) and torch.allclose(y[1, 0, 4], (c[1, 0, 1] * h).sum() + skip[4] * x[1, 0, 4]) and (y[1, 1:] == 0.0).all()
+
+
 def test_log_probs():
     logits, tokens = normal(3, 7), torch.tensor([[0, 0, 6], [3, -1, 9], [2, 2, 2]])
     logits[1, 4] = -float("inf")
