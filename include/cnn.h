@@ -417,7 +417,8 @@ int cnn_causal_conv_step(const cnn_causal_conv_shape* shape, const cnn_tokens* x
  *   D_t = softplus(dt_t + dt_bias), or dt_t + dt_bias with softplus == 0,   h_t[n] = exp(D_t a[d,n]) h_{t-1}[n] + D_t x_t b_t[n],
  *   y_t = sum_n c_t[n] h_t[n] + skip[d] x_t,   t = 0 .. length - 1,   softplus(z) = ln(1 + exp(z)).
  * a[D,N], skip[D], dt_bias[D] (the last two nullable: zeros) are fp32; a below 0 and D_t above make decays of at most 1, which is not checked.  x and dt (and
- * d_y) as cnn_tokens of `type`; b and c [B,T,G,N] as cnn_heads, D a multiple of G, D / G consecutive channels to a group.  Results y, d_x, d_dt [B,T,D] and
+ * d_y) as cnn_tokens of `type`; b and c [B,T,G,N] as cnn_heads, tokens at most 2^26 elements apart; D a multiple of G, D / G
+ * consecutive channels to a group.  Results y, d_x, d_dt [B,T,D] and
  * d_b, d_c [B,T,G,N] are contiguous; states [B,D,N] are fp32, an initial or final one may be NULL (zero; not wanted), and they may be the same memory.  lengths
  * as for cnn_causal_conv_fwd.  1 <= N <= 128, B * D <= 2^24, B * T < 2^31, D <= 2^20.  Inputs up to a sequence's length must be finite: one that is not
  * makes results NaN that the formulas leave finite, also of tokens before it, of its own channel and, backward, its group's d_b and d_c.  Everything is

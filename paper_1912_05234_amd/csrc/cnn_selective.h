@@ -48,13 +48,13 @@ struct Args {
   float* last;                  // the final state, or the error of the first; nullable
   float *ends, *errors, *sums;  // of the segments: [segments][B][D][N], the same, [segments][B][D]
   float *partial, *shared;      // backward: [segments][B][D][N + 2], [channel blocks][B][T][G][2][NP]
-  int64_t T, length;            // of a segment
+  int T, length;                // of a segment
   int B, D, N, G, per, blocks, segments, softplus;  // per: channels of a group; blocks: waves that these take
 };
 
-__device__ __forceinline__ int64_t length_of(const Args& a, int64_t b) {
+__device__ __forceinline__ int length_of(const Args& a, int b) {
   if (!a.lengths) return a.T;
-  const int64_t n = a.lengths[b];
+  const int n = a.lengths[b];
   return n < 0 ? 0 : n > a.T ? a.T : n;
 }
 
@@ -94,7 +94,7 @@ __device__ __forceinline__ float softplus_of(float z) {
 
 // A wave's place: its channel and states, the tokens of its segment.
 struct Place {
-  int64_t b, t0, t1, end;  // tokens t0 .. t1 - 1, of which those from `end` on are past the sequence
+  int b, t0, t1, end;  // tokens t0 .. t1 - 1, of which those from `end` on are past the sequence
   int segment, group, channel, state, s, block;
   bool mine;  // a channel of the group (else the lane has the last one's parameters, inputs and errors of zero, and stores nothing)
 };
@@ -106,14 +106,14 @@ __device__ __forceinline__ Place place_of(const Args& a) {
   int64_t w = workgroup();
   p.block = (int)(w % a.blocks), w /= a.blocks;
   p.group = (int)(w % a.G), w /= a.G;
-  p.b = w % a.B, p.segment = (int)(w / a.B);
+  p.b = (int)(w % a.B), p.segment = (int)(w / a.B);
   const int lane = threadIdx.x, in = p.block * CHANNELS + lane / S;
   p.mine = in < a.per;
   p.channel = p.group * a.per + (p.mine ? in : a.per - 1);
   p.s = lane % S, p.state = p.s * NL;
   p.t0 = p.segment * a.length;
-  p.t1 = p.t0 + a.length < a.T ? p.t0 + a.length : a.T;
-  const int64_t n = length_of(a, p.b);
+  p.t1 = a.T - p.t0 < a.length ? a.T : p.t0 + a.length;
+  const int n = length_of(a, p.b);
   p.end = n < p.t0 ? p.t0 : n < p.t1 ? n : p.t1;
   return p;
 }
@@ -132,45 +132,89 @@ __device__ __forceinline__ void put_states(float* to, const float (&h)[NL], cons
     for (int i = 0; i < NL; i += 4) put_loose<4>(at + i, *reinterpret_cast<const float(*)[4]>(h + i), a.N - p.state - i);
 }
 
-// What U tokens have once a channel, each lane its tokens k S + s; zeros past the sequence.
+// What U tokens have once a channel, each lane its tokens k S + s.
+template <int S>
+struct Own {
+  static constexpr int EACH = U > S ? U / S : 1;
+};
 template <class T, int S>
 struct Once {
-  static constexpr int EACH = U > S ? U / S : 1;
-  float v[EACH];
-  __device__ __forceinline__ void get(const Tokens& from, const Place& p, int64_t t) {
-    const T* at = static_cast<const T*>(from.data) + p.b * from.batch + p.channel;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const int64_t k = t + i * S + p.s;
-      v[i] = p.mine && (S <= U || p.s < U) && k >= p.t0 && k < p.end ? (float)at[k * from.token] : 0.0f;
-    }
-  }
+  static constexpr int EACH = Own<S>::EACH;
+  T v[EACH];
   template <int K>
-  __device__ __forceinline__ float of() const {  // token K's
+  __device__ __forceinline__ T of() const {  // token K's
     return from_lane<S, K % S>(v[K / S]);
   }
 };
 
-// Rows of B and C of U tokens on their way through LDS, as floats; zeros past the sequence and past N.
+// The loads of a tensor's U tokens of one chunk.  They are not looked at here, so that all of a chunk's are on their way together: no
+// lane has a branch of its own, and where a chunk ends past its segment the last token is taken again.  Chunks outside
+// the segment are not read.  A chunk's address is the same in all lanes, their offsets from it are below 2^31 bytes.
+template <class T, int S>
+struct Source {
+  const T* base;
+  int64_t token;
+  uint32_t lane;
+  int own;
+  __device__ __forceinline__ Source(const Tokens& from, const Place& p)
+      : base(static_cast<const T*>(from.data) + p.b * from.batch), token(from.token), own(p.s % U) {
+    lane = (uint32_t)p.channel + (uint32_t)own * (uint32_t)token;
+  }
+  __device__ __forceinline__ void get(Once<T, S>& to, const Place& p, int t) const {
+    if (t < p.t0 || t >= p.end) return;
+    const T* row = base + t * token;
+    if (t + U <= p.end) {
+#pragma unroll
+      for (int i = 0; i < Own<S>::EACH; ++i) to.v[i] = row[lane + (uint32_t)(i * S) * (uint32_t)token];
+    } else {
+#pragma unroll
+      for (int i = 0; i < Own<S>::EACH; ++i) {
+        const int k = i * S + own, last = p.end - 1 - t;
+        to.v[i] = row[(uint32_t)p.channel + (uint32_t)(k < last ? k : last) * (uint32_t)token];
+      }
+    }
+  }
+};
+
+// Stores of U tokens of one chunk, contiguous rows of D: of the tokens below `stop`.
+template <class T, int S>
+__device__ __forceinline__ void put_tokens(T* to, const Once<float, S>& from, const Place& p, const Args& a, int t, int stop) {
+  if (!p.mine || (S > U && p.s >= U)) return;
+  T* row = to + ((int64_t)p.b * a.T + t) * a.D;
+  const uint32_t lane = (uint32_t)p.channel + (uint32_t)p.s * (uint32_t)a.D;
+  if (t + U <= stop) {
+#pragma unroll
+    for (int i = 0; i < Own<S>::EACH; ++i) row[lane + (uint32_t)(i * S) * (uint32_t)a.D] = (T)from.v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < Own<S>::EACH; ++i)
+      if (t + i * S + p.s < stop) row[lane + (uint32_t)(i * S) * (uint32_t)a.D] = (T)from.v[i];
+  }
+}
+
+// Rows of B and C of U tokens on their way through LDS, as floats; zeros past N.
 template <class T, int NP>
 struct Row {
   static constexpr int EACH = U * NP >= 64 ? U * NP / 64 : 1;
+  const T* base;
+  int64_t token;
   T v[EACH];
-  __device__ __forceinline__ void get(const Tokens& from, const Place& p, const Args& a, int64_t t) {
-    const T* at = static_cast<const T*>(from.data) + p.b * from.batch + p.group * from.group;
+  __device__ __forceinline__ Row(const Tokens& from, const Place& p)
+      : base(static_cast<const T*>(from.data) + p.b * from.batch + p.group * from.group), token(from.token) {}
+  __device__ __forceinline__ void get(const Place& p, const Args& a, int t) {
+    if (t < p.t0 || t >= p.end) return;
+    const T* row = base + t * token;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int e = i * 64 + (int)threadIdx.x, k = e / NP, n = e % NP;
-      const int64_t token = t + k;
-      v[i] = (T)0.0f;
-      if (k < U && n < a.N && token >= p.t0 && token < p.end) v[i] = at[token * from.token + n];
+      const int e = i * 64 + (int)threadIdx.x, k = e / NP % U, n = e % NP, last = p.end - 1 - t;
+      v[i] = row[(uint32_t)(k < last ? k : last) * (uint32_t)token + (uint32_t)(n < a.N ? n : a.N - 1)];
     }
   }
-  __device__ __forceinline__ void put(float* to) const {
+  __device__ __forceinline__ void put(float* to, const Args& a) const {
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       const int e = i * 64 + (int)threadIdx.x;
-      if (e < U * NP) to[e] = (float)v[i];
+      if (e < U * NP) to[e] = e % NP < a.N ? (float)v[i] : 0.0f;
     }
   }
 };
@@ -201,23 +245,31 @@ __device__ __forceinline__ void get_decays(float (&a2)[NL], const Args& a, const
   for (int i = 0; i < NL; ++i) a2[i] *= -NEG_LOG2E;
 }
 
-// D_t and D_t x_t of a lane's own tokens.
+// D_t and D_t x_t of a lane's own tokens, and x_t; zeros past the sequence (there the state stays) and for channels that are none.
 template <class T, int S>
-__device__ __forceinline__ void get_steps(const Args& a, const Place& p, int64_t t, float bias, const Once<T, S>& x, const Once<T, S>& dt, Once<T, S>& delta,
-                                          Once<T, S>& u) {
+__device__ __forceinline__ void get_steps(const Args& a, const Place& p, int t, float bias, const Once<T, S>& x, const Once<T, S>& dt, Once<float, S>& z,
+                                          Once<float, S>& delta, Once<float, S>& u, Once<float, S>& input) {
 #pragma unroll
-  for (int i = 0; i < Once<T, S>::EACH; ++i) {
-    const float z = dt.v[i] + bias;
-    delta.v[i] = t + i * S + p.s < p.end ? (a.softplus ? softplus_of(z) : z) : 0.0f;  // past the sequence the state stays
-    u.v[i] = delta.v[i] * x.v[i];
+  for (int i = 0; i < Own<S>::EACH; ++i) {
+    const bool there = p.mine && t + i * S + p.s < p.end;
+    z.v[i] = (float)dt.v[i] + bias;
+    delta.v[i] = there ? (a.softplus ? softplus_of(z.v[i]) : z.v[i]) : 0.0f;
+    input.v[i] = there ? (float)x.v[i] : 0.0f;
+    u.v[i] = delta.v[i] * input.v[i];
   }
+}
+
+template <class T, int S>
+__device__ __forceinline__ void get_errors(const Place& p, int t, const Once<T, S>& d_y, Once<float, S>& error) {
+#pragma unroll
+  for (int i = 0; i < Own<S>::EACH; ++i) error.v[i] = p.mine && t + i * S + p.s < p.end ? (float)d_y.v[i] : 0.0f;
 }
 
 // ---- forward -------------------------------------------------------------------------------------------------------------
 // ENDS: a segment's own end state (from zero) and its sum of D; with ERRORS its first state's error too.  Else y, and the final state where there is
 // one segment.
 template <class T, int NL, int S, bool ENDS, bool ERRORS>
-__global__ __launch_bounds__(64) void selective_tokens_kernel(Args a) {
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(S == 1 ? 2 : S == 16 ? 3 : 4))) void selective_tokens_kernel(Args a) {
   constexpr int NP = NL * S;
   __shared__ __align__(16) float rows[2][2][U * NP];
   const Place p = place_of<NL, S>(a);
@@ -234,33 +286,43 @@ __global__ __launch_bounds__(64) void selective_tokens_kernel(Args a) {
     for (int i = 0; i < NL; ++i) q[i] = 0.0f, run[i] = 1.0f;
   float sum = 0.0f;
   constexpr bool NEEDS_C = !ENDS || ERRORS;
-  Once<T, S> x, dt, d_y, next_x, next_dt, next_d;
-  Row<T, NP> b, c;
-  next_x.get(a.x, p, p.t0), next_dt.get(a.dt, p, p.t0);
-  if constexpr (ERRORS) next_d.get(a.d_y, p, p.t0);
-  b.get(a.b, p, a, p.t0);
-  if constexpr (NEEDS_C) c.get(a.c, p, a, p.t0);
-  const int64_t stop = ENDS ? p.end : p.t1;
-  T* y = static_cast<T*>(a.y) + p.b * a.T * a.D + p.channel;
+  const Source<T, S> from_x(a.x, p), from_dt(a.dt, p), from_d(ERRORS ? a.d_y : a.x, p);
+  Once<T, S> next_x, next_dt, next_d;
+  Row<T, NP> b(a.b, p), c(a.c, p);
+  from_x.get(next_x, p, p.t0), from_dt.get(next_dt, p, p.t0);
+  if constexpr (ERRORS) from_d.get(next_d, p, p.t0);
+  b.get(p, a, p.t0);
+  if constexpr (NEEDS_C) c.get(p, a, p.t0);
+  const int stop = ENDS ? p.end : p.t1;
   int turn = 0;
-  for (int64_t t = p.t0; t < stop; t += U, turn ^= 1) {
-    x = next_x, dt = next_dt;
-    if constexpr (ERRORS) d_y = next_d;
-    b.put(rows[turn][0]);
-    if constexpr (NEEDS_C) c.put(rows[turn][1]);
+  for (int t = p.t0; t < stop; t += U, turn ^= 1) {
+    Once<float, S> z, delta, u, x, d_y, out;
+    get_steps(a, p, t, bias, next_x, next_dt, z, delta, u, x);
+    if constexpr (ERRORS) get_errors(p, t, next_d, d_y);
+    b.put(rows[turn][0], a);
+    if constexpr (NEEDS_C) c.put(rows[turn][1], a);
     __syncthreads();
-    next_x.get(a.x, p, t + U), next_dt.get(a.dt, p, t + U);
-    if constexpr (ERRORS) next_d.get(a.d_y, p, t + U);
-    b.get(a.b, p, a, t + U);
-    if constexpr (NEEDS_C) c.get(a.c, p, a, t + U);
-    Once<T, S> delta, u, out;
-    get_steps(a, p, t, bias, x, dt, delta, u);
+    from_x.get(next_x, p, t + U), from_dt.get(next_dt, p, t + U);
+    if constexpr (ERRORS) from_d.get(next_d, p, t + U);
+    b.get(p, a, t + U);
+    if constexpr (NEEDS_C) c.get(p, a, t + U);
+    float next_B[NL], next_C[NL];  // a token ahead: all of them at once would take too many registers
+    get_row(next_B, rows[turn][0] + p.state);
+    if constexpr (NEEDS_C) get_row(next_C, rows[turn][1] + p.state);
     each<U>([&](auto k) {
       constexpr int K = decltype(k)::value;
       const float d = delta.template of<K>(), input = u.template of<K>();
       float B[NL], C[NL], y_t = 0.0f, error = 0.0f;
-      get_row(B, rows[turn][0] + K * NP + p.state);
-      if constexpr (NEEDS_C) get_row(C, rows[turn][1] + K * NP + p.state);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        B[i] = next_B[i];
+        if constexpr (NEEDS_C) C[i] = next_C[i];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (K + 1 < U) {
+        get_row(next_B, rows[turn][0] + (K + 1) * NP + p.state);
+        if constexpr (NEEDS_C) get_row(next_C, rows[turn][1] + (K + 1) * NP + p.state);
+      }
       if constexpr (ERRORS) error = d_y.template of<K>();
       if constexpr (ENDS) sum += d;
 #pragma unroll
@@ -278,12 +340,11 @@ __global__ __launch_bounds__(64) void selective_tokens_kernel(Args a) {
         if (p.s == K % S) out.v[K / S] = y_t;
       }
     });
-    if constexpr (!ENDS)
+    if constexpr (!ENDS) {
 #pragma unroll
-      for (int i = 0; i < Once<T, S>::EACH; ++i) {
-        const int64_t k = t + i * S + p.s;
-        if (p.mine && (S <= U || p.s < U) && k < p.t1) y[k * a.D] = (T)(k < p.end ? out.v[i] + skip * x.v[i] : 0.0f);
-      }
+      for (int i = 0; i < Own<S>::EACH; ++i) out.v[i] = t + i * S + p.s < p.end ? out.v[i] + skip * x.v[i] : 0.0f;
+      put_tokens(static_cast<T*>(a.y), out, p, a, t, p.t1);
+    }
   }
   if constexpr (ENDS) {
     const int64_t at = (int64_t)p.segment * a.B + p.b;
@@ -363,8 +424,8 @@ struct ChannelSums {
 };
 
 template <class T, int NL, int S>
-__global__ __launch_bounds__(64) void selective_gradient_kernel(Args a) {
-  constexpr int NP = NL * S, EACH = Once<T, S>::EACH;
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void selective_gradient_kernel(Args a) {
+  constexpr int NP = NL * S, EACH = Own<S>::EACH;
   using Sums = ChannelSums<S, 2 * NL>;
   __shared__ __align__(16) float rows[2][2][U * NP];
   __shared__ __align__(16) f4 kept[LONGEST / U][NL / 4][64];
@@ -379,46 +440,52 @@ __global__ __launch_bounds__(64) void selective_gradient_kernel(Args a) {
   for (int i = 0; i < NL; ++i) h[i] = q[i] = d_a[i] = 0.0f;
   if (from) get_states(h, from, p, a);
   if (error_from) get_states(q, error_from, p, a);
-  const int chunks = (int)((p.end - p.t0 + U - 1) / U);
-  Once<T, S> x, dt, d_y, next_x, next_dt, next_d, delta, u;
-  Row<T, NP> b, c;
+  const int chunks = (p.end - p.t0 + U - 1) / U;
+  const Source<T, S> from_x(a.x, p), from_dt(a.dt, p), from_d(a.d_y, p);
+  Once<T, S> next_x, next_dt, next_d;
+  Once<float, S> z, delta, u, x, d_y;
+  Row<T, NP> b(a.b, p), c(a.c, p);
   int turn = 0;
   // forwards: the state in front of every chunk
-  next_x.get(a.x, p, p.t0), next_dt.get(a.dt, p, p.t0), b.get(a.b, p, a, p.t0);
+  from_x.get(next_x, p, p.t0), from_dt.get(next_dt, p, p.t0), b.get(p, a, p.t0);
   for (int j = 0; j < chunks; ++j, turn ^= 1) {
-    const int64_t t = p.t0 + j * U;
+    const int t = p.t0 + j * U;
 #pragma unroll
     for (int i = 0; i < NL; i += 4) kept[j][i / 4][threadIdx.x] = f4{h[i], h[i + 1], h[i + 2], h[i + 3]};
     if (j == chunks - 1) break;
-    x = next_x, dt = next_dt;
-    b.put(rows[turn][0]);
+    get_steps(a, p, t, bias, next_x, next_dt, z, delta, u, x);
+    b.put(rows[turn][0], a);
     __syncthreads();
-    next_x.get(a.x, p, t + U), next_dt.get(a.dt, p, t + U), b.get(a.b, p, a, t + U);
-    get_steps(a, p, t, bias, x, dt, delta, u);
+    from_x.get(next_x, p, t + U), from_dt.get(next_dt, p, t + U), b.get(p, a, t + U);
+    float next_B[NL];
+    get_row(next_B, rows[turn][0] + p.state);
     each<U>([&](auto k) {
       constexpr int K = decltype(k)::value;
       const float d = delta.template of<K>(), input = u.template of<K>();
       float B[NL];
-      get_row(B, rows[turn][0] + K * NP + p.state);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) B[i] = next_B[i];
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (K + 1 < U) get_row(next_B, rows[turn][0] + (K + 1) * NP + p.state);
 #pragma unroll
       for (int i = 0; i < NL; ++i) h[i] = __builtin_amdgcn_exp2f(d * a2[i]) * h[i] + input * B[i];
     });
   }
   __syncthreads();
   // backwards; next_x, next_dt and b hold the last chunk
-  const int64_t last = p.t0 + (int64_t)(chunks - 1) * U;
-  next_d.get(a.d_y, p, last), c.get(a.c, p, a, last);
-  T *d_x = static_cast<T*>(a.d_x) + p.b * a.T * a.D + p.channel, *d_dt = static_cast<T*>(a.d_dt) + p.b * a.T * a.D + p.channel;
+  const int last = p.t0 + (chunks - 1) * U;
+  from_d.get(next_d, p, last), c.get(p, a, last);
   const int value = Sums::first(), row = value < NL ? 0 : 1, state = p.state + value - row * NL;
-  float* shared = a.shared + ((((int64_t)p.block * a.B + p.b) * a.T) * a.G + p.group) * 2 * NP + row * NP + state;
+  float* shared = a.shared + (((int64_t)p.block * a.B + p.b) * a.T * a.G + p.group) * 2 * NP;
+  const uint32_t shared_lane = row * NP + state, shared_token = (uint32_t)a.G * 2 * NP;
   for (int j = chunks - 1; j >= 0; --j, turn ^= 1) {
-    const int64_t t = p.t0 + j * U;
-    x = next_x, dt = next_dt, d_y = next_d;
-    b.put(rows[turn][0]), c.put(rows[turn][1]);
+    const int t = p.t0 + j * U;
+    get_steps(a, p, t, bias, next_x, next_dt, z, delta, u, x);
+    get_errors(p, t, next_d, d_y);
+    b.put(rows[turn][0], a), c.put(rows[turn][1], a);
     __syncthreads();
-    next_x.get(a.x, p, t - U), next_dt.get(a.dt, p, t - U), next_d.get(a.d_y, p, t - U);
-    b.get(a.b, p, a, t - U), c.get(a.c, p, a, t - U);
-    get_steps(a, p, t, bias, x, dt, delta, u);
+    from_x.get(next_x, p, t - U), from_dt.get(next_dt, p, t - U), from_d.get(next_d, p, t - U);
+    b.get(p, a, t - U), c.get(p, a, t - U);
     float before[U + 1][NL], decay[U][NL];  // before[k]: the state in front of token k
 #pragma unroll
     for (int i = 0; i < NL; i += 4) {
@@ -426,24 +493,36 @@ __global__ __launch_bounds__(64) void selective_gradient_kernel(Args a) {
 #pragma unroll
       for (int l = 0; l < 4; ++l) before[0][i + l] = v[l];
     }
+    float next_B[NL], next_C[NL];
+    get_row(next_B, rows[turn][0] + p.state);
     each<U>([&](auto k) {
       constexpr int K = decltype(k)::value;
       const float d = delta.template of<K>(), input = u.template of<K>();
       float B[NL];
-      get_row(B, rows[turn][0] + K * NP + p.state);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) B[i] = next_B[i];
+      __builtin_amdgcn_sched_barrier(0);
+      get_row(next_B, rows[turn][0] + (K + 1 < U ? K + 1 : K) * NP + p.state);
+      if constexpr (K + 1 == U) get_row(next_C, rows[turn][1] + K * NP + p.state);
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         decay[K][i] = __builtin_amdgcn_exp2f(d * a2[i]);
         before[K + 1][i] = decay[K][i] * before[K][i] + input * B[i];
       }
     });
-    Once<T, S> sum_b, sum_a;  // of g B; of A q' h
+    Once<float, S> sum_b, sum_a;  // of g B; of A q' h
+    float over_channels[U][Sums::LEFT];
     each<U>([&](auto k) {
       constexpr int K = U - 1 - decltype(k)::value;
       const float d = delta.template of<K>(), input = u.template of<K>(), error = d_y.template of<K>();
       float B[NL], C[NL], v[16], by_b = 0.0f, by_a = 0.0f;
-      get_row(B, rows[turn][0] + K * NP + p.state);
-      get_row(C, rows[turn][1] + K * NP + p.state);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) B[i] = next_B[i], C[i] = next_C[i];
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (K > 0) {
+        get_row(next_B, rows[turn][0] + (K - 1) * NP + p.state);
+        get_row(next_C, rows[turn][1] + (K - 1) * NP + p.state);
+      }
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const float g = q[i] + C[i] * error;
@@ -458,25 +537,34 @@ __global__ __launch_bounds__(64) void selective_gradient_kernel(Args a) {
       by_b = shared_sum<S>(by_b), by_a = shared_sum<S>(by_a);
       if (p.s == K % S) sum_b.v[K / S] = by_b, sum_a.v[K / S] = by_a;
       Sums::sum(v);
-      if (Sums::writes() && t + K < p.end)
 #pragma unroll
-        for (int i = 0; i < Sums::LEFT; ++i) shared[(t + K) * a.G * 2 * NP + i] = v[i];
+      for (int i = 0; i < Sums::LEFT; ++i) over_channels[K][i] = v[i];
     });
+    if (Sums::writes()) {
+      float* to = shared + t * (int64_t)shared_token;
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+        if (t + k < p.end)
+#pragma unroll
+          for (int i = 0; i < Sums::LEFT; ++i) to[shared_lane + k * shared_token + i] = over_channels[k][i];
+    }
+    Once<float, S> to_x, to_dt;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int64_t k = t + i * S + p.s;
-      if ((S > U && p.s >= U) || k >= p.end) continue;
-      const float z = dt.v[i] + bias;
       const float d_delta = x.v[i] * sum_b.v[i] + sum_a.v[i] * 0.69314718055994530942f;
-      const float d_z = a.softplus ? d_delta * logistic(z) : d_delta;
-      d_skip += d_y.v[i] * x.v[i], d_bias += d_z;
-      if (!p.mine) continue;
-      d_x[k * a.D] = (T)(delta.v[i] * sum_b.v[i] + skip * d_y.v[i]);
-      d_dt[k * a.D] = (T)d_z;
+      const float slope = a.softplus ? logistic(z.v[i]) : 1.0f;
+      to_x.v[i] = delta.v[i] * sum_b.v[i] + skip * d_y.v[i], to_dt.v[i] = d_delta * slope;
+      const bool there = (S <= U || p.s < U) && t + i * S + p.s < p.end;
+      d_skip += there ? d_y.v[i] * x.v[i] : 0.0f, d_bias += there ? to_dt.v[i] : 0.0f;
     }
+    put_tokens(static_cast<T*>(a.d_x), to_x, p, a, t, p.end);
+    put_tokens(static_cast<T*>(a.d_dt), to_dt, p, a, t, p.end);
   }
   if (p.mine && p.s == 0) {
-    for (int64_t k = p.end; k < p.t1; ++k) d_x[k * a.D] = (T)0.0f, d_dt[k * a.D] = (T)0.0f;
+    for (int k = p.end; k < p.t1; ++k) {
+      const int64_t to = ((int64_t)p.b * a.T + k) * a.D + p.channel;
+      static_cast<T*>(a.d_x)[to] = (T)0.0f, static_cast<T*>(a.d_dt)[to] = (T)0.0f;
+    }
   }
   if (a.last && p.segment == 0) put_states(a.last + p.b * states, q, p, a);
   d_skip = shared_sum<S>(d_skip), d_bias = shared_sum<S>(d_bias);
@@ -502,13 +590,18 @@ void launch_f16(const Args& a, Pass pass, Form f, dim3 grid, hipStream_t st);
 
 template <class T, int NL, int S>
 void launch_form(const Args& a, Pass pass, dim3 grid, hipStream_t st) {
-  // Forward any division of the states; backward eight to a lane (four where there are no more).
-  if constexpr (NL == 8 || (NL == 4 && S == 1)) {
+  // Backward a lane has four states, whose U tokens, with their decays, are 64 registers (eight, with 128, spill: the pixel model's step, 100 x 784
+  // tokens of 128 x 16 states, takes 410 us that way and 259 this way); eight only where a channel has more than 16 lanes hold.  Forward eight,
+  // which share a token's work on its channel among more states (a prompt of 2 x 4096 tokens of 2048 x 16 states: 147 us, and 150 with four),
+  // or four where there are no more or more waves are wanted.
+  if constexpr (NL == 4 || S == 16) {
     if (pass == ENDS_AND_ERRORS) return selective_tokens_kernel<T, NL, S, true, true><<<grid, 64, 0, st>>>(a);
     if (pass == GRADIENT) return selective_gradient_kernel<T, NL, S><<<grid, 64, 0, st>>>(a);
   }
-  if (pass == ENDS) selective_tokens_kernel<T, NL, S, true, false><<<grid, 64, 0, st>>>(a);
-  else selective_tokens_kernel<T, NL, S, false, false><<<grid, 64, 0, st>>>(a);
+  if constexpr (NL == 8 || S < 8) {
+    if (pass == ENDS) selective_tokens_kernel<T, NL, S, true, false><<<grid, 64, 0, st>>>(a);
+    if (pass == TOKENS) selective_tokens_kernel<T, NL, S, false, false><<<grid, 64, 0, st>>>(a);
+  }
 }
 
 template <class T>
@@ -522,9 +615,8 @@ void launch_type(const Args& a, Pass pass, Form f, dim3 grid, hipStream_t st) {
   const integral_constant<int, 4> four;
   const integral_constant<int, 8> eight;
   const integral_constant<int, 16> sixteen;
-  at(four, one), at(four, two), at(four, four);
-  at(eight, one), at(eight, two), at(eight, four), at(eight, eight), at(eight, sixteen);
-  at(sixteen, one), at(sixteen, two), at(sixteen, four), at(sixteen, eight);
+  at(four, one), at(four, two), at(four, four), at(four, eight), at(four, sixteen);
+  at(eight, two), at(eight, four), at(eight, eight), at(eight, sixteen);
 }
 
 }  // namespace selective

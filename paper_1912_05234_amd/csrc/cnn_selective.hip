@@ -8,6 +8,7 @@ namespace selective {
 namespace {
 
 constexpr int MOST_STATES = 128, MOST_CHANNELS = 1 << 20;
+constexpr int64_t MOST_STRIDE = 1 << 26;  // from token to token: a chunk's lie within 2^31 bytes
 constexpr float LOG2E = 1.44269504088896340736f;
 
 // ---- states between segments ---------------------------------------------------------------------------------------------
@@ -144,10 +145,10 @@ bool shape_ok(const cnn_selective_scan_shape* s) {
 }
 
 bool tokens_ok(const cnn_tokens* t, int type) {
-  return t && t->data && reinterpret_cast<uintptr_t>(t->data) % type_bytes(type) == 0 && t->batch >= 0 && t->token >= 0;
+  return t && t->data && reinterpret_cast<uintptr_t>(t->data) % type_bytes(type) == 0 && t->batch >= 0 && t->token >= 0 && t->token <= MOST_STRIDE;
 }
 bool heads_ok(const cnn_heads* h, int type) {
-  return h && h->data && reinterpret_cast<uintptr_t>(h->data) % type_bytes(type) == 0 && h->batch >= 0 && h->token >= 0 && h->head >= 0;
+  return h && h->data && reinterpret_cast<uintptr_t>(h->data) % type_bytes(type) == 0 && h->batch >= 0 && h->token >= 0 && h->token <= MOST_STRIDE && h->head >= 0;
 }
 
 bool all_aligned(std::initializer_list<const void*> all) {
@@ -176,12 +177,11 @@ Plan plan_of(const cnn_selective_scan_shape& s, bool backward) {
   const int64_t per = s.D / s.G;
   const auto blocks = [&](int lanes) { return (per * lanes + 63) / 64; };
   double best = 0.0;
-  for (const int states : {16, 8, 4})
+  for (const int states : {8, 4})
     for (const int lanes : {1, 2, 4, 8, 16}) {
-      // whole divisions of the states, the fewest lanes that hold them
-      if (states * lanes < s.N || (lanes > 1 && states * lanes / 2 >= s.N) || (states > 4 && lanes == 1 && states / 2 >= s.N)) continue;
-      if ((states == 4 && lanes > 4) || (states == 16 && lanes > 8)) continue;
-      if (backward && states != 8 && !(states == 4 && lanes == 1)) continue;
+      // the fewest lanes that hold a channel's states, of those that have a kernel
+      if (states * lanes < s.N || (lanes > 1 && states * lanes / 2 >= s.N)) continue;
+      if (backward ? states == 8 && (lanes < 16 || s.N <= 64) : states == 8 ? lanes < 2 : lanes > 4) continue;
       const int64_t waves = (int64_t)s.B * s.G * blocks(lanes);
       const double cycles = states * 38.0 + 50.0 + 100.0 / lanes;
       for (int64_t length = 64; ; length *= 2) {
@@ -216,7 +216,7 @@ Args args_of(const cnn_selective_scan_shape& s, const Plan& p, void* workspace) 
   char* ws = static_cast<char*>(workspace);
   a.ends = reinterpret_cast<float*>(ws + p.ends), a.errors = reinterpret_cast<float*>(ws + p.errors), a.sums = reinterpret_cast<float*>(ws + p.sums);
   a.partial = reinterpret_cast<float*>(ws + p.partial), a.shared = reinterpret_cast<float*>(ws + p.shared);
-  a.T = s.T, a.length = p.length, a.B = s.B, a.D = s.D, a.N = s.N, a.G = s.G, a.per = s.D / s.G, a.blocks = p.blocks, a.segments = p.segments;
+  a.T = s.T, a.length = (int)p.length, a.B = s.B, a.D = s.D, a.N = s.N, a.G = s.G, a.per = s.D / s.G, a.blocks = p.blocks, a.segments = p.segments;
   a.softplus = s.softplus != 0;
   return a;
 }

@@ -114,9 +114,9 @@ def test_scan_refusals():
         assert fwd(s=s) == bwd(s=s) == EINVAL and L.cnn_selective_scan_fwd_workspace_bytes(s) == L.cnn_selective_scan_bwd_workspace_bytes(s) == 0, bad
         if bad.get("T", 1) == 1:
             assert step(s=scan(**{"T": 1, **bad})) == EINVAL, bad
-    for x in [None] + BAD_TOKENS:
+    for x in [None, tokens(token=(1 << 26) + 1)] + BAD_TOKENS:
         assert fwd(x=x) == fwd(dt=x) == bwd(x=x) == bwd(dt=x) == bwd(d=x) == step(x=x) == step(dt=x) == EINVAL
-    for h in [None] + BAD_HEADS:
+    for h in [None, heads(token=(1 << 26) + 1)] + BAD_HEADS:
         assert fwd(b=h) == fwd(c=h) == bwd(b=h) == bwd(c=h) == step(b=h) == step(c=h) == EINVAL
     for p in (nul, odd):
         assert fwd(a=p) == fwd(y=p) == bwd(a=p) == bwd(ws=p) == step(a=p) == step(st=p) == step(y=p) == EINVAL
