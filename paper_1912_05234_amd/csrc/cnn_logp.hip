@@ -58,15 +58,34 @@ __device__ __forceinline__ uint64_t key_of(float x, int64_t index) {
   if (x != x) order = 0xfffffffeu;  // above infinity, and no key is all ones
   return (uint64_t)order << 32 | (uint32_t)~(uint32_t)index;
 }
+__device__ __forceinline__ float value_of(uint64_t key) {
+  const uint32_t order = (uint32_t)(key >> 32);
+  return order == 0xfffffffeu ? __builtin_nanf("") : __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order);
+}
 __device__ __forceinline__ int64_t index_of(uint64_t key) { return (int64_t)(uint32_t)~(uint32_t)key; }
 
 __device__ __forceinline__ int64_t token_of(const void* tokens, int wide, int64_t i) {
   return wide ? static_cast<const int64_t*>(tokens)[i] : (int64_t) static_cast<const int32_t*>(tokens)[i];
 }
 
-// The row's results from its sums; lanes of one workgroup share the given tokens.
+// A given token's logit; `known` says whether it is one.
+struct Given {
+  float logit;
+  bool known;
+};
 template <class T>
-__device__ __forceinline__ float finish_row(const Args& a, const T* logits, int64_t n, const Sums& r) {
+__device__ __forceinline__ Given got_given(const Args& a, const T* logits, int64_t n, int j) {
+  Given g{0.0f, false};
+  if (j >= a.given) return g;
+  const int64_t token = token_of(a.tokens, a.wide, n * a.given + j);
+  g.known = token >= 0 && token < a.vocab;
+  if (g.known) g.logit = (float)logits[token];
+  return g;
+}
+
+// The row's results from its sums; the workgroup's lanes share the given tokens, of which each has asked for its first one's logit beforehand.
+template <class T>
+__device__ __forceinline__ float finish_row(const Args& a, const T* logits, int64_t n, const Sums& r, const Given& first) {
   const bool none = r.m == minus_infinity() && r.s == 0.0f;  // (a NaN would be in s)
   const float log_sum = none ? 0.0f : logf(r.s), base = none ? 0.0f : r.m;
   if (threadIdx.x == 0) {
@@ -76,12 +95,17 @@ __device__ __forceinline__ float finish_row(const Args& a, const T* logits, int6
     if (a.stats) a.stats[n * 3] = r.m, a.stats[n * 3 + 1] = log_sum, a.stats[n * 3 + 2] = h;
   }
   for (int j = threadIdx.x; j < a.given; j += blockDim.x) {
-    const int64_t token = token_of(a.tokens, a.wide, n * a.given + j);
-    float lp = 0.0f;
-    if (token >= 0 && token < a.vocab) lp = ((float)logits[token] - base) * a.scale - log_sum;
-    a.log_probs[n * a.given + j] = lp;
+    const Given g = j == (int)threadIdx.x ? first : got_given(a, logits, n, j);
+    a.log_probs[n * a.given + j] = g.known ? (g.logit - base) * a.scale - log_sum : 0.0f;
   }
   return log_sum;
+}
+
+// Rank `rank` of a row's top tokens.
+__device__ __forceinline__ void put_top(const Args& a, int64_t n, int rank, uint64_t key, const Sums& r, float log_sum) {
+  const float base = r.m == minus_infinity() ? 0.0f : r.m;
+  a.top_tokens[n * a.top + rank] = (int32_t)index_of(key);
+  a.top_log_probs[n * a.top + rank] = (value_of(key) - base) * a.scale - log_sum;
 }
 
 __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
@@ -101,14 +125,13 @@ struct TopShared {
   int count;
 };
 
-// Calls put(rank, key) for the `top` largest of the keys that each(fn) hands out (a thread its own), key 0 where there are fewer; `likely`
-// says which keys may be among them.  The whole workgroup calls it; keys are unique and not 0.
-template <int THREADS, class EACH, class LIKELY, class PUT>
-__device__ void top_keys(TopShared<THREADS>& sh, int top, EACH each, LIKELY likely, PUT put) {
+// Calls put(rank, key) for the `top` largest of the keys that each(fn) hands out, every thread its own, key 0 where there are fewer.  The whole
+// workgroup calls it; keys are unique and not 0.
+template <int THREADS, class EACH, class PUT>
+__device__ void top_keys(TopShared<THREADS>& sh, int top, EACH each, PUT put) {
   if (threadIdx.x == 0) sh.count = 0;
   __syncthreads();
   each([&](uint64_t key) {
-    if (!likely(key)) return;
     const int at = atomicAdd(&sh.count, 1);  // (their order in the list does not matter)
     if (at < TopShared<THREADS>::LIST) sh.list[at] = key;
   });
@@ -169,12 +192,18 @@ __global__ __launch_bounds__(THREADS) void logp_part_kernel(Args a) {
   const int64_t left = a.vocab - begin, length = left < a.part_length ? left : a.part_length;  // (every part has an element)
   const T* logits = static_cast<const T*>(a.logits) + n * a.row;
   const T* part = logits + begin;
+  const Given given = a.parts == 1 ? got_given(a, logits, n, threadIdx.x) : Given{0.0f, false};
   float x[PACKS][V];
+  Loose<T, V> raw[PACKS];
 #pragma unroll
   for (int p = 0; p < PACKS; ++p) {
     const int at = (p * THREADS + (int)threadIdx.x) * V;
-    const int count = (int)length - at;
-    get_loose(x[p], part + at, count);
+    raw[p] = got_loose<V>(part + at, (int)length - at);
+  }
+#pragma unroll
+  for (int p = 0; p < PACKS; ++p) {
+    const int at = (p * THREADS + (int)threadIdx.x) * V, count = (int)length - at;
+    widen(x[p], raw[p]);
     if (count < V)
 #pragma unroll
       for (int j = 0; j < V; ++j)
@@ -206,7 +235,7 @@ __global__ __launch_bounds__(THREADS) void logp_part_kernel(Args a) {
     for (int w = 1; w < WAVES; ++w) r = join(r, sums[w], c);
   }
   float log_sum = 0.0f;
-  if (a.parts == 1) log_sum = finish_row(a, logits, n, r);
+  if (a.parts == 1) log_sum = finish_row(a, logits, n, r, given);
   else if (threadIdx.x == 0) a.sums[workgroup()] = r;
   if (!a.top) return;
   float least;  // no fewer than `top` elements reach it
@@ -231,20 +260,14 @@ __global__ __launch_bounds__(THREADS) void logp_part_kernel(Args a) {
         if (!(x[p][j] < least) && at < length) fn(key_of(x[p][j], begin + at));
       }
   };
-  const float base = r.m == minus_infinity() ? 0.0f : r.m;
-  top_keys<THREADS>(sh, a.top, each, [](uint64_t) { return true; }, [&](int rank, uint64_t key) {
-    if (a.parts > 1) {
-      a.keys[workgroup() * a.top + rank] = key;
-    } else {
-      const int64_t v = index_of(key);
-      a.top_tokens[n * a.top + rank] = (int32_t)v;
-      a.top_log_probs[n * a.top + rank] = ((float)logits[v] - base) * a.scale - log_sum;
-    }
+  top_keys<THREADS>(sh, a.top, each, [&](int rank, uint64_t key) {
+    if (a.parts > 1) a.keys[workgroup() * a.top + rank] = key;
+    else put_top(a, n, rank, key, r, log_sum);
   });
 }
 
 // The parts of a row joined.
-constexpr int JOIN_THREADS = 256;
+constexpr int JOIN_THREADS = 256, JOIN_KEYS = 2;
 template <class T>
 __global__ __launch_bounds__(JOIN_THREADS) void logp_join_kernel(Args a) {
   __shared__ Sums sums[JOIN_THREADS / 64];
@@ -252,20 +275,33 @@ __global__ __launch_bounds__(JOIN_THREADS) void logp_join_kernel(Args a) {
   const int64_t n = workgroup();
   if (n >= a.rows) return;
   const T* logits = static_cast<const T*>(a.logits) + n * a.row;
+  const Given given = got_given(a, logits, n, threadIdx.x);
+  const uint64_t* keys = a.keys + n * a.parts * a.top;
+  const int count = a.parts * a.top;
+  uint64_t own[JOIN_KEYS], least = 0;  // the first keys of this lane; the largest of the parts' last ones, which `top` keys reach
+#pragma unroll
+  for (int k = 0; k < JOIN_KEYS; ++k) {
+    const int i = k * JOIN_THREADS + (int)threadIdx.x;
+    own[k] = i < count ? keys[i] : 0;
+  }
   const float c = a.scale * LOG2E;
   Sums r{minus_infinity(), 0.0f, 0.0f};
-  uint64_t least = 0;  // a part's last key: `top` others are no smaller
-  const uint64_t* keys = a.keys + n * a.parts * a.top;
-  for (int p = threadIdx.x; p < a.parts; p += JOIN_THREADS) {
-    r = join(r, a.sums[n * a.parts + p], c);
-    if (a.top) {
-      const uint64_t last = keys[(int64_t)p * a.top + a.top - 1];
-      least = last > least ? last : least;
-    }
-  }
+  for (int p = threadIdx.x; p < a.parts; p += JOIN_THREADS) r = join(r, a.sums[n * a.parts + p], c);
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) r = join(r, Sums{__shfl_xor(r.m, d), __shfl_xor(r.s, d), __shfl_xor(r.t, d)}, c);
-  least = wave_max(least);
+  const auto each = [&](auto fn) {
+#pragma unroll
+    for (int k = 0; k < JOIN_KEYS; ++k)
+      if (own[k]) fn(own[k], k * JOIN_THREADS + (int)threadIdx.x);
+    for (int i = JOIN_KEYS * JOIN_THREADS + (int)threadIdx.x; i < count; i += JOIN_THREADS)
+      if (keys[i]) fn(keys[i], i);
+  };
+  if (a.top) {
+    each([&](uint64_t key, int i) {
+      if (i % a.top == a.top - 1 && key > least) least = key;
+    });
+    least = wave_max(least);
+  }
   if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = r, sh.waves[0][threadIdx.x / 64] = least;
   __syncthreads();
   r = sums[0];
@@ -273,20 +309,15 @@ __global__ __launch_bounds__(JOIN_THREADS) void logp_join_kernel(Args a) {
   for (int w = 1; w < JOIN_THREADS / 64; ++w) r = join(r, sums[w], c);
 #pragma unroll
   for (int w = 0; w < JOIN_THREADS / 64; ++w) least = sh.waves[0][w] > least ? sh.waves[0][w] : least;
-  const float log_sum = finish_row(a, logits, n, r), base = r.m == minus_infinity() ? 0.0f : r.m;
+  const float log_sum = finish_row(a, logits, n, r, given);
   if (!a.top) return;
-  const auto each = [&](auto fn) {
-    for (int i = threadIdx.x; i < a.parts * a.top; i += JOIN_THREADS) {
-      const uint64_t key = keys[i];
-      if (key && key >= least) fn(key);
-    }
-  };
   __syncthreads();  // (top_keys writes sh.waves again)
-  top_keys<JOIN_THREADS>(sh, a.top, each, [](uint64_t) { return true; }, [&](int rank, uint64_t key) {
-    const int64_t v = index_of(key);
-    a.top_tokens[n * a.top + rank] = (int32_t)v;
-    a.top_log_probs[n * a.top + rank] = ((float)logits[v] - base) * a.scale - log_sum;
-  });
+  const auto likely = [&](auto fn) {
+    each([&](uint64_t key, int) {
+      if (key >= least) fn(key);
+    });
+  };
+  top_keys<JOIN_THREADS>(sh, a.top, likely, [&](int rank, uint64_t key) { put_top(a, n, rank, key, r, log_sum); });
 }
 
 // ---- backward ----------------------------------------------------------------------------------------------------------
@@ -301,28 +332,35 @@ struct BackArgs {
 };
 
 // One tile of a row: THREADS lanes with PACKS packs each, all on their way at once.
-template <class T, int THREADS, int PACKS>
+template <class T, int THREADS, int PACKS, bool PAST_CACHES>
 __global__ __launch_bounds__(THREADS) void logp_backward_kernel(BackArgs a) {
-  constexpr int V = sizeof(T) == 2 ? 8 : 4;
+  constexpr int V = sizeof(T) == 2 ? 8 : 4, TILE = THREADS * PACKS * V;
   __shared__ int64_t tokens[MOST_GIVEN];
   __shared__ float errors[MOST_GIVEN];
-  const int64_t n = workgroup() / a.tiles, begin = workgroup() % a.tiles * (THREADS * PACKS * V);
+  const int64_t n = workgroup() / a.tiles;
+  const int begin = (int)(workgroup() % a.tiles) * TILE, left = (int)a.vocab - begin;
   if (n >= a.rows) return;
   const T* logits = static_cast<const T*>(a.logits) + n * a.row;
   T* d_logits = static_cast<T*>(a.d_logits) + n * a.vocab;
-  const int64_t left = a.vocab - begin;
-  float x[PACKS][V];
+  const bool whole = left >= TILE;  // the same in all lanes: no branch for each pack
+  Loose<T, V> raw[PACKS];
+  const auto at = [&](int p) { return (p * THREADS + (int)threadIdx.x) * V; };
+  if (whole) {
 #pragma unroll
-  for (int p = 0; p < PACKS; ++p) {
-    const int at = (p * THREADS + (int)threadIdx.x) * V;
-    get_loose(x[p], logits + begin + at, (int)left - at);
+    for (int p = 0; p < PACKS; ++p) {
+      if constexpr (PAST_CACHES) raw[p] = got_loose_past_caches<V>(logits + begin + at(p));
+      else raw[p] = *reinterpret_cast<const Loose<T, V>*>(logits + begin + at(p));
+    }
+  } else {
+#pragma unroll
+    for (int p = 0; p < PACKS; ++p) raw[p] = got_loose<V>(logits + begin + at(p), left - at(p));
   }
   const float m = a.stats[n * 3], log_sum = a.stats[n * 3 + 1], h = a.stats[n * 3 + 2];
   const float d_h = a.d_entropy ? a.d_entropy[n] : 0.0f;
   const bool none = m == minus_infinity() && log_sum == 0.0f;
   const float base = none ? 0.0f : m;
   float total = 0.0f;  // of the given tokens' errors; the same in every wave
-  int64_t token = -1;  // of the only one
+  int64_t token = -1;  // the only one
   float error = 0.0f;
   if (a.given == 1) {
     token = token_of(a.tokens, a.wide, n);
@@ -346,19 +384,22 @@ __global__ __launch_bounds__(THREADS) void logp_backward_kernel(BackArgs a) {
     if (a.d_entropy) d -= d_h * weighted(p, z * LN2 + h);
     return none ? 0.0f : by * d;
   };
+  const int only = (int)token - begin;  // (below 0, or behind the tile, where it is not here)
 #pragma unroll
   for (int p = 0; p < PACKS; ++p) {
-    const int at = (p * THREADS + (int)threadIdx.x) * V;
-    const int64_t first = begin + at;
+    float x[V];
+    widen(x, raw[p]);
 #pragma unroll
-    for (int j = 0; j < V; ++j) x[p][j] = gradient(x[p][j], first + j == token ? error : 0.0f);
-    put_loose(d_logits + first, x[p], (int)left - at);
+    for (int j = 0; j < V; ++j) x[j] = gradient(x[j], at(p) + j == only ? error : 0.0f);
+    if (!whole) put_loose(d_logits + begin + at(p), x, left - at(p));
+    else if constexpr (PAST_CACHES) put_loose_past_caches(d_logits + begin + at(p), x);
+    else put_loose(d_logits + begin + at(p), x, V);
   }
   if (a.given == 1) return;
   __syncthreads();  // the rows' stores are done before a given token's element is written again
   for (int j = threadIdx.x; j < a.given; j += THREADS) {
     const int64_t t = tokens[j];
-    if (t < begin || t >= begin + THREADS * PACKS * V) continue;
+    if (t < begin || t >= begin + TILE) continue;
     bool before = false;
     float g = 0.0f;
     for (int i = 0; i < a.given; ++i) {
@@ -421,11 +462,11 @@ void launch_part(const Args& a, const Plan& p, hipStream_t st) {
   else logp_part_kernel<T, 1024, 32><<<grid, 1024, 0, st>>>(a);
 }
 
-template <class T, int THREADS, int PACKS>
+template <class T, int THREADS, int PACKS, bool PAST_CACHES>
 void launch_backward(BackArgs a, hipStream_t st) {
   constexpr int64_t TILE = THREADS * PACKS * (sizeof(T) == 2 ? 8 : 4);
   a.tiles = (int)((a.vocab + TILE - 1) / TILE);
-  logp_backward_kernel<T, THREADS, PACKS><<<grid_of(a.rows * a.tiles), THREADS, 0, st>>>(a);
+  logp_backward_kernel<T, THREADS, PACKS, PAST_CACHES><<<grid_of(a.rows * a.tiles), THREADS, 0, st>>>(a);
 }
 
 }  // namespace
@@ -472,9 +513,10 @@ int cnn_log_probs_bwd(const cnn_log_probs_shape* s, const cnn_rows* logits, cons
   return with_type(s->type, [&](auto t) {
     using T = decltype(t);
     constexpr int PACK = sizeof(T) == 2 ? 8 : 4;
-    if (s->vocab <= 64 * PACK) launch_backward<T, 64, 1>(a, st);
-    else if (s->vocab <= 256 * PACK) launch_backward<T, 256, 1>(a, st);
-    else launch_backward<T, 256, 32 / PACK>(a, st);
+    if (s->vocab <= 64 * PACK) launch_backward<T, 64, 1, false>(a, st);
+    else if (s->vocab <= 256 * PACK) launch_backward<T, 256, 1, false>(a, st);
+    else if (a.rows * a.vocab * (int64_t)sizeof(T) * 2 >= (int64_t)256 << 20) launch_backward<T, 256, 16 / PACK, true>(a, st);
+    else launch_backward<T, 256, 16 / PACK, false>(a, st);
     return launch_status();
   });
 }

@@ -293,9 +293,8 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(S == 1 ? 2 :
   if constexpr (ERRORS) from_d.get(next_d, p, p.t0);
   b.get(p, a, p.t0);
   if constexpr (NEEDS_C) c.get(p, a, p.t0);
-  const int stop = ENDS ? p.end : p.t1;
-  int turn = 0;
-  for (int t = p.t0; t < stop; t += U, turn ^= 1) {
+  int turn = 0, t = p.t0;
+  for (; t < p.end; t += U, turn ^= 1) {
     Once<float, S> z, delta, u, x, d_y, out;
     get_steps(a, p, t, bias, next_x, next_dt, z, delta, u, x);
     if constexpr (ERRORS) get_errors(p, t, next_d, d_y);
@@ -345,6 +344,12 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(S == 1 ? 2 :
       for (int i = 0; i < Own<S>::EACH; ++i) out.v[i] = t + i * S + p.s < p.end ? out.v[i] + skip * x.v[i] : 0.0f;
       put_tokens(static_cast<T*>(a.y), out, p, a, t, p.t1);
     }
+  }
+  if constexpr (!ENDS) {  // rows past the sequence
+    Once<float, S> zero;
+#pragma unroll
+    for (int i = 0; i < Own<S>::EACH; ++i) zero.v[i] = 0.0f;
+    for (; t < p.t1; t += U) put_tokens(static_cast<T*>(a.y), zero, p, a, t, p.t1);
   }
   if constexpr (ENDS) {
     const int64_t at = (int64_t)p.segment * a.B + p.b;

@@ -63,20 +63,29 @@ struct SharedArgs {
   int G, N, NP, blocks;
 };
 
-template <class T>
+// PARTS threads share a pack of four sums, each taking every PARTS-th wave's.
+template <class T, int PARTS>
 __global__ __launch_bounds__(256) void selective_shared_kernel(SharedArgs a) {
-  const int packs = 2 * a.NP / 4;
-  const int64_t i = workgroup() * 256 + threadIdx.x;
-  if (i >= a.rows * packs) return;
-  const int64_t row = i / packs, t = row / a.G % a.T, b = row / a.G / a.T;
-  const int at = (int)(i % packs) * 4, n = at % a.NP;
+  __shared__ f4 sums[PARTS > 1 ? 256 : 1];
+  constexpr int WIDE = 256 / PARTS;
+  const int packs = 2 * a.NP / 4, part = threadIdx.x / WIDE;
+  const int64_t i = workgroup() * WIDE + threadIdx.x % WIDE, row = i / packs;
   f4 sum{0.0f, 0.0f, 0.0f, 0.0f};
-  if (!a.lengths || t < a.lengths[b]) {
+  if (row < a.rows && (!a.lengths || row / a.G % a.T < a.lengths[row / a.G / a.T])) {
     const f4* from = reinterpret_cast<const f4*>(a.shared) + i;
-#pragma unroll 4
-    for (int k = 0; k < a.blocks; ++k) sum += from[k * a.rows * packs];
+#pragma unroll 8
+    for (int k = part; k < a.blocks; k += PARTS) sum += from[k * a.rows * packs];
   }
-  float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+  if constexpr (PARTS > 1) {
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    if (part) return;
+#pragma unroll
+    for (int k = 1; k < PARTS; ++k) sum += sums[k * WIDE + threadIdx.x];
+  }
+  if (row >= a.rows) return;
+  const int at = (int)(i % packs) * 4, n = at % a.NP;
+  const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
   put_loose<4>(static_cast<T*>(at < a.NP ? a.d_b : a.d_c) + row * a.N + n, v, a.N - n);
 }
 
@@ -284,7 +293,10 @@ int cnn_selective_scan_bwd(const cnn_selective_scan_shape* s, const cnn_tokens* 
   const SharedArgs g{a.shared, lengths, d_b, d_c, (int64_t)s->B * s->T * s->G, s->T, s->G, s->N, p.form.states * p.form.lanes, p.blocks};
   const int64_t packs = g.rows * (2 * g.NP / 4);
   const int status = with_type(s->type, [&](auto t) {
-    selective_shared_kernel<decltype(t)><<<grid_of((packs + 255) / 256), 256, 0, st>>>(g);
+    using T = decltype(t);
+    // (Two tokens of 31 sequences of 2496 channels, 156 waves to a sum: 31 us by one thread, 7 by eight.)
+    if (p.blocks > 8) selective_shared_kernel<T, 8><<<grid_of((packs + 31) / 32), 256, 0, st>>>(g);
+    else selective_shared_kernel<T, 1><<<grid_of((packs + 255) / 256), 256, 0, st>>>(g);
     return launch_status();
   });
   if (status != CNN_OK) return status;

@@ -64,26 +64,38 @@ __device__ __forceinline__ Part part_of(const Args& a) {
   return p;
 }
 
-template <class T, int K, int V>
+template <int K, int V>
 __device__ __forceinline__ void get_weights(const Args& a, const Part& p, float (&w)[K][V], float (&bias)[V]) {
+  const Loose<float, K * V> all = got_loose<K * V>(a.weight + p.c * K, p.count * K);
+  Loose<float, V> b{};
+  if (a.bias) b = got_loose<V>(a.bias + p.c, p.count);
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    bias[j] = a.bias && j < p.count ? a.bias[p.c + j] : 0.0f;
+    bias[j] = b.v[j];
 #pragma unroll
-    for (int k = 0; k < K; ++k) w[k][j] = j < p.count ? a.weight[(p.c + j) * K + k] : 0.0f;
+    for (int k = 0; k < K; ++k) w[k][j] = all.v[j * K + k];
   }
 }
 
 // Input at position t < n, which may lie in the state before the sequence.
 template <class T, int K, int V>
-__device__ __forceinline__ void get_input(const Args& a, const Part& p, int64_t t, float (&to)[V]) {
-  if (t >= 0) {
-    get_loose(to, static_cast<const T*>(a.x.data) + p.b * a.x.batch + t * a.x.token + p.c, p.count);
-  } else if (a.first) {
-    get_loose(to, static_cast<const T*>(a.first) + (p.b * (K - 1) + t + K - 1) * a.D + p.c, p.count);
+__device__ __forceinline__ Loose<T, V> got_input(const Args& a, const Part& p, int64_t t) {
+  if (t >= 0) return got_loose<V>(static_cast<const T*>(a.x.data) + p.b * a.x.batch + t * a.x.token + p.c, p.count);
+  if (a.first) return got_loose<V>(static_cast<const T*>(a.first) + (p.b * (K - 1) + t + K - 1) * a.D + p.c, p.count);
+  return got_loose<V>(static_cast<const T*>(nullptr), 0);
+}
+
+// AHEAD tokens from t on: their loads together, without a branch for each where the whole chunk is inside the sequence.
+template <class T, int V, int AHEAD>
+__device__ __forceinline__ void get_tokens(Loose<T, V> (&to)[AHEAD], const T* at, int64_t token, int64_t t, int64_t end, int count) {
+  const T* row = at + t * token;
+  if (t + AHEAD <= end && count >= V) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) to[i] = *reinterpret_cast<const Loose<T, V>*>(row + i * token);
   } else {
 #pragma unroll
-    for (int j = 0; j < V; ++j) to[j] = 0.0f;
+    for (int i = 0; i < AHEAD; ++i)
+      if (t + i < end) to[i] = got_loose<V>(row + i * token, count);
   }
 }
 
@@ -93,41 +105,56 @@ __global__ __launch_bounds__(THREADS) void conv_tokens_kernel(Args a) {
   const Part p = part_of<V>(a);
   if (p.count <= 0) return;
   float w[K][V], bias[V], seen[AHEAD + K - 1][V];
-  get_weights<T>(a, p, w, bias);
+  get_weights(a, p, w, bias);
 #pragma unroll
   for (int i = 0; i < K - 1; ++i) {
     const int64_t t = p.t0 - (K - 1) + i;
-    if (t < p.n) get_input<T, K>(a, p, t, seen[i]);
+    if (t < p.n) widen(seen[i], got_input<T, K, V>(a, p, t));
   }
+  const T* x = static_cast<const T*>(a.x.data) + p.b * a.x.batch + p.c;
+  Loose<T, V> next[AHEAD];
+  get_tokens(next, x, a.x.token, p.t0, p.n, p.count);
   T* y = static_cast<T*>(a.out) + p.b * a.T * a.D + p.c;
-  for (int64_t t = p.t0; t < p.t1; t += AHEAD) {
+  // INSIDE: all AHEAD tokens are the sequence's and the chunk's, and the pack is whole.
+  const auto walk = [&](int64_t t, auto inside) {
+    constexpr bool INSIDE = decltype(inside)::value;
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
-      if (t + i < p.n && t + i < p.t1) get_input<T, K>(a, p, t + i, seen[K - 1 + i]);
+    for (int i = 0; i < AHEAD; ++i) widen(seen[K - 1 + i], next[i]);
+    if (t + AHEAD < p.t1) get_tokens(next, x, a.x.token, t + AHEAD, p.n, p.count);
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
-      if (t + i >= p.t1) break;
+      if (!INSIDE && t + i >= p.t1) break;
       float out[V];
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         float s = bias[j];
 #pragma unroll
         for (int k = 0; k < K; ++k) s += w[k][j] * seen[i + k][j];
-        if (a.silu) s *= logistic(s);
-        out[j] = t + i < p.n ? s : 0.0f;
+        out[j] = s;
       }
-      put_loose(y + (t + i) * a.D, out, p.count);
+      if (a.silu)
+#pragma unroll
+        for (int j = 0; j < V; ++j) out[j] *= logistic(out[j]);
+      if (!INSIDE && t + i >= p.n)
+#pragma unroll
+        for (int j = 0; j < V; ++j) out[j] = 0.0f;
+      put_loose(y + (t + i) * a.D, out, INSIDE ? V : p.count);
     }
 #pragma unroll
     for (int i = 0; i < K - 1; ++i)
 #pragma unroll
       for (int j = 0; j < V; ++j) seen[i][j] = seen[AHEAD + i][j];
+  };
+  const int64_t within = p.n < p.t1 ? p.n : p.t1;
+  for (int64_t t = p.t0; t < p.t1; t += AHEAD) {
+    if (t + AHEAD <= within && p.count >= V) walk(t, std::true_type{});
+    else walk(t, std::false_type{});
   }
   if (a.last && p.t0 == 0)
 #pragma unroll
     for (int i = 0; i < K - 1; ++i) {
       float v[V];
-      get_input<T, K>(a, p, p.n - (K - 1) + i, v);
+      widen(v, got_input<T, K, V>(a, p, p.n - (K - 1) + i));
       put_loose(static_cast<T*>(a.last) + (p.b * (K - 1) + i) * a.D + p.c, v, p.count);
     }
 }
@@ -146,50 +173,58 @@ __global__ __launch_bounds__(THREADS) void conv_tokens_backward_kernel(Args a) {
   }
   if (p.count > 0) {
     float w[K][V], bias[V], seen[AHEAD + K - 1][V], error[AHEAD + K - 1][V];
-    get_weights<T>(a, p, w, bias);
+    get_weights(a, p, w, bias);
 #pragma unroll
     for (int i = 0; i < K - 1; ++i) {
       const int64_t t = p.t0 - (K - 1) + i;
-      if (t < p.n) get_input<T, K>(a, p, t, seen[i]);
+      if (t < p.n) widen(seen[i], got_input<T, K, V>(a, p, t));
 #pragma unroll
       for (int j = 0; j < V; ++j) error[i][j] = 0.0f;
     }
     const T* d_y = static_cast<const T*>(a.d_y.data) + p.b * a.d_y.batch + p.c;
     T* d_x = static_cast<T*>(a.out) + p.b * a.T * a.D + p.c;
     const int64_t end = p.t1 + K - 1;  // token s completes the error of input s - K + 1
-    for (int64_t t = p.t0; t < end; t += AHEAD) {
+    const T* x = static_cast<const T*>(a.x.data) + p.b * a.x.batch + p.c;
+    Loose<T, V> next_x[AHEAD], next_d[AHEAD];
+    get_tokens(next_x, x, a.x.token, p.t0, p.n, p.count), get_tokens(next_d, d_y, a.d_y.token, p.t0, p.n, p.count);
+    // INSIDE: all AHEAD tokens are the sequence's and the chunk's, the errors that they complete the chunk's, and the pack is whole.
+    const auto walk = [&](int64_t t, auto inside) {
+      constexpr bool INSIDE = decltype(inside)::value;
       float d[AHEAD][V];
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i)
-        if (t + i < p.n && t + i < end) {
-          get_input<T, K>(a, p, t + i, seen[K - 1 + i]);
-          get_loose(d[i], d_y + (t + i) * a.d_y.token, p.count);
-        }
+      for (int i = 0; i < AHEAD; ++i) widen(seen[K - 1 + i], next_x[i]), widen(d[i], next_d[i]);
+      if (t + AHEAD < end) {
+        get_tokens(next_x, x, a.x.token, t + AHEAD, p.n, p.count), get_tokens(next_d, d_y, a.d_y.token, t + AHEAD, p.n, p.count);
+      }
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
         const int64_t s = t + i, u = s - (K - 1);
-        if (s >= end) break;
+        if (!INSIDE && s >= end) break;
+        float e[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          float e = 0.0f;
-          if (s < p.n) {
-            e = d[i][j];
-            if (a.silu) {
-              float pre = bias[j];
+        for (int j = 0; j < V; ++j) e[j] = d[i][j];
+        if (a.silu)
 #pragma unroll
-              for (int k = 0; k < K; ++k) pre += w[k][j] * seen[i + k][j];
-              const float sigmoid = logistic(pre);
-              e *= sigmoid * (1.0f + pre * (1.0f - sigmoid));
-            }
-            if (s < p.t1) {
-              d_b[j] += e;
+          for (int j = 0; j < V; ++j) {
+            float pre = bias[j];
 #pragma unroll
-              for (int k = 0; k < K; ++k) d_w[k][j] += e * seen[i + k][j];
-            }
+            for (int k = 0; k < K; ++k) pre += w[k][j] * seen[i + k][j];
+            const float sigmoid = logistic(pre);
+            e[j] *= sigmoid * (1.0f + pre * (1.0f - sigmoid));
           }
-          error[K - 1 + i][j] = e;
-        }
-        if (u < p.t0 && !(p.t0 == 0 && a.last)) continue;  // an earlier chunk's, or one that nobody asked for
+        if (!INSIDE && s >= p.n)
+#pragma unroll
+          for (int j = 0; j < V; ++j) e[j] = 0.0f;
+        if (INSIDE || (s < p.n && s < p.t1))
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            d_b[j] += e[j];
+#pragma unroll
+            for (int k = 0; k < K; ++k) d_w[k][j] += e[j] * seen[i + k][j];
+          }
+#pragma unroll
+        for (int j = 0; j < V; ++j) error[K - 1 + i][j] = e[j];
+        if (!INSIDE && u < p.t0 && !(p.t0 == 0 && a.last)) continue;  // an earlier chunk's, or one that nobody asked for
         float out[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -197,6 +232,10 @@ __global__ __launch_bounds__(THREADS) void conv_tokens_backward_kernel(Args a) {
 #pragma unroll
           for (int k = 0; k < K; ++k) sum += w[K - 1 - k][j] * error[i + k][j];
           out[j] = sum;
+        }
+        if constexpr (INSIDE) {
+          put_loose(d_x + u * a.D, out, V);
+          continue;
         }
         const int64_t kept = u - (p.n - (K - 1));  // its place in the final state
         if (a.d_last && kept >= 0 && kept < K - 1) {
@@ -218,6 +257,11 @@ __global__ __launch_bounds__(THREADS) void conv_tokens_backward_kernel(Args a) {
       for (int i = 0; i < K - 1; ++i)
 #pragma unroll
         for (int j = 0; j < V; ++j) seen[i][j] = seen[AHEAD + i][j], error[i][j] = error[AHEAD + i][j];
+    };
+    const int64_t within = p.n < p.t1 ? p.n : p.t1;
+    for (int64_t t = p.t0; t < end; t += AHEAD) {
+      if (t + AHEAD <= within && t - (K - 1) >= p.t0 && p.count >= V) walk(t, std::true_type{});
+      else walk(t, std::false_type{});
     }
   }
   // [lanes][V] for each chunk beside the others, one tap after the other

@@ -44,17 +44,60 @@ struct Loose {
   T v[N];
 };
 
-// The first `count` of N elements as floats, zeros behind them; and their stores.  A whole pack is one access.
+// The first `count` of N elements, zeros behind them; a whole pack is one access.  Nothing looks at them here, so several packs that are got one after
+// the other are on their way together (a conversion would wait for each).
 template <int N, class T>
-__device__ __forceinline__ void get_loose(float (&to)[N], const T* at, int count) {
+__device__ __forceinline__ Loose<T, N> got_loose(const T* at, int count) {
+  Loose<T, N> p;
   if (count >= N) {
-    const Loose<T, N> p = *reinterpret_cast<const Loose<T, N>*>(at);
-#pragma unroll
-    for (int j = 0; j < N; ++j) to[j] = (float)p.v[j];
+    p = *reinterpret_cast<const Loose<T, N>*>(at);
   } else {
 #pragma unroll
-    for (int j = 0; j < N; ++j) to[j] = j < count ? (float)at[j] : 0.0f;
+    for (int j = 0; j < N; ++j) p.v[j] = j < count ? at[j] : (T)0.0f;
   }
+  return p;
+}
+template <int N, class T>
+__device__ __forceinline__ void widen(float (&to)[N], const Loose<T, N>& p) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) to[j] = (float)p.v[j];
+}
+// Whole packs past the caches.
+template <int N, class T>
+__device__ __forceinline__ Loose<T, N> got_loose_past_caches(const T* at) {
+  static_assert(N * sizeof(T) % 16 == 0, "packs of whole sixteen bytes");
+  using Words = uint32_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  struct All {
+    uint32_t __attribute__((ext_vector_type(4))) w[N * sizeof(T) / 16];
+  } all;
+#pragma unroll
+  for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i) all.w[i] = __builtin_nontemporal_load(reinterpret_cast<const Words*>(at) + i);
+  using To = Loose<T, N>;
+  return __builtin_bit_cast(To, all);
+}
+template <int N, class T>
+__device__ __forceinline__ void put_loose_past_caches(T* at, const float (&from)[N]) {
+  using Words = uint32_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  Loose<T, N> p;
+#pragma unroll
+  for (int j = 0; j < N; ++j) p.v[j] = (T)from[j];
+  struct All {
+    uint32_t __attribute__((ext_vector_type(4))) w[N * sizeof(T) / 16];
+  };
+  const All all = __builtin_bit_cast(All, p);
+#pragma unroll
+  for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i) __builtin_nontemporal_store(all.w[i], reinterpret_cast<Words*>(at) + i);
+}
+template <int N, class T>
+__device__ __forceinline__ Loose<T, N> got_loose(const T* at, int count, bool past_caches) {
+  if constexpr (N * sizeof(T) % 16 == 0)
+    if (past_caches && count >= N) return got_loose_past_caches<N>(at);
+  return got_loose<N>(at, count);
+}
+// The same as floats, for a pack that is needed at once; and stores.
+template <int N, class T>
+__device__ __forceinline__ void get_loose(float (&to)[N], const T* at, int count) {
+  widen(to, got_loose<N>(at, count));
 }
 template <int N, class T>
 __device__ __forceinline__ void put_loose(T* at, const float (&from)[N], int count) {
@@ -68,6 +111,13 @@ __device__ __forceinline__ void put_loose(T* at, const float (&from)[N], int cou
     for (int j = 0; j < N; ++j)
       if (j < count) at[j] = (T)from[j];
   }
+}
+
+template <int N, class T>
+__device__ __forceinline__ void put_loose(T* at, const float (&from)[N], int count, bool past_caches) {
+  if constexpr (N * sizeof(T) % 16 == 0)
+    if (past_caches && count >= N) return put_loose_past_caches(at, from);
+  put_loose(at, from, count);
 }
 
 // Calls fn with a value of the element type that `type` names.
