@@ -3,16 +3,17 @@
 //   z = scale l,  m = max z,  ln p_v = z_v - m - ln sum exp(z - m),  H = - sum p ln p
 //   d_l_v = scale ( sum_j g_j [v = token_j] - p_v sum_j g_j - d_H p_v (ln p_v + H) )
 //
-// Memory bounds both: a pass reads the logits once.  A workgroup holds its part of a row in registers, at most 32 elements to a lane,
+// Memory bounds both: a pass reads the logits once.  A workgroup holds its part of a row in registers, at most 64 elements to a lane (of floats 32),
 // so the maximum, the two sums (of e = exp(z - m) and of e (z - m), from which the entropy comes without cancellation: both of its
-// terms have one sign) and the choice of the largest elements all work on them.  Rows longer than 32768 are cut into parts, more
-// of them where rows are few, which a second kernel joins.
+// terms have one sign) and the choice of the largest elements all work on them.  Rows longer than 65536 (16384 floats; 32768 where rows are few) are cut into
+// parts, more of them where rows are few, which a second kernel joins.
 //
 // The k largest: the k-th largest of the maxima of 64 (128) groups of lanes is a lower bound that few elements reach (24 are expected
 // for k = 20 of 64 groups); those go into a list in LDS, and each finds its place by counting the larger ones.  Keys are unique,
 // the value's bits in order above the complement of the index, so equal values keep the order of their tokens.  Where the list
 // overflows (rows of equal logits) the workgroup takes the largest key k times instead.
 #include "cnn_common.h"
+#include "cnn_lanes.h"
 #include "cnn_types.h"
 
 namespace cnn {
@@ -44,8 +45,15 @@ __device__ __forceinline__ float minus_infinity() { return -__builtin_inff(); }
 // e d for e = 2^d, which is 0 for d = -inf.  (A NaN of d is in e.)
 __device__ __forceinline__ float weighted(float e, float d) { return e * fmaxf(d, -1e30f); }
 
-// Adds another piece's sums: the maximum of the two, sums rescaled.  Pieces without a possible token have m = -inf, s = t = 0.
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {  // c = scale log2(e)
+// The sums of a wave's pieces, one to a lane, relative to the largest maximum; c = scale log2(e).  Pieces without a possible token have
+// m = -inf, s = t = 0.
+__device__ __forceinline__ Sums joined(const Sums& a, float c) {
+  const float m = max_over<64>(a.m), ref = m == minus_infinity() ? 0.0f : m;
+  const float d = (a.m - ref) * c, e = __builtin_amdgcn_exp2f(d);
+  return {m, sum_over<64>(a.s * e), sum_over<64>(e * (a.t + weighted(a.s, d)))};
+}
+// Pieces one after the other.
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {
   const float m = fmaxf(a.m, b.m), ref = m == minus_infinity() ? 0.0f : m;
   const float da = (a.m - ref) * c, db = (b.m - ref) * c;
   const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
@@ -83,19 +91,20 @@ __device__ __forceinline__ Given got_given(const Args& a, const T* logits, int64
   return g;
 }
 
-// The row's results from its sums; the workgroup's lanes share the given tokens, of which each has asked for its first one's logit beforehand.
-template <class T>
+// The row's results from its sums; its lanes share the given tokens, of which each has asked for its first one's logit beforehand.
+template <int THREADS, class T>
 __device__ __forceinline__ float finish_row(const Args& a, const T* logits, int64_t n, const Sums& r, const Given& first) {
+  const int lane = threadIdx.x % THREADS;
   const bool none = r.m == minus_infinity() && r.s == 0.0f;  // (a NaN would be in s)
   const float log_sum = none ? 0.0f : logf(r.s), base = none ? 0.0f : r.m;
-  if (threadIdx.x == 0) {
+  if (lane == 0) {
     // (a row with an infinite or NaN logit has s = NaN)
     const float h = none ? 0.0f : log_sum - r.t * LN2 / r.s;
     if (a.entropy) a.entropy[n] = h;
     if (a.stats) a.stats[n * 3] = r.m, a.stats[n * 3 + 1] = log_sum, a.stats[n * 3 + 2] = h;
   }
-  for (int j = threadIdx.x; j < a.given; j += blockDim.x) {
-    const Given g = j == (int)threadIdx.x ? first : got_given(a, logits, n, j);
+  for (int j = lane; j < a.given; j += THREADS) {
+    const Given g = j == lane ? first : got_given(a, logits, n, j);
     a.log_probs[n * a.given + j] = g.known ? (g.logit - base) * a.scale - log_sum : 0.0f;
   }
   return log_sum;
@@ -109,12 +118,18 @@ __device__ __forceinline__ void put_top(const Args& a, int64_t n, int rank, uint
 }
 
 __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint64_t o = __shfl_xor(v, d);
-    v = o > v ? o : v;
+  return over_lanes<64>(v, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+}
+
+// Waits for the lanes that share a row.  (A wave's own accesses to LDS are in order.)
+template <int THREADS>
+__device__ __forceinline__ void row_sync() {
+  if constexpr (THREADS > 64) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
-  return v;
 }
 
 template <int THREADS>
@@ -125,26 +140,27 @@ struct TopShared {
   int count;
 };
 
-// Calls put(rank, key) for the `top` largest of the keys that each(fn) hands out, every thread its own, key 0 where there are fewer.  The whole
-// workgroup calls it; keys are unique and not 0.
-template <int THREADS, class EACH, class PUT>
-__device__ void top_keys(TopShared<THREADS>& sh, int top, EACH each, PUT put) {
-  if (threadIdx.x == 0) sh.count = 0;
-  __syncthreads();
-  each([&](uint64_t key) {
+// Calls put(rank, key) for the `top` largest of the keys that each(fn) hands out, every thread its own, key 0 where there are fewer; likely(fn) hands out
+// some of them, the `top` largest among these.  All of a row's lanes call it; keys are unique and not 0.
+template <int THREADS, class LIKELY, class EACH, class PUT>
+__device__ void top_keys(TopShared<THREADS>& sh, int top, LIKELY likely, EACH each, PUT put) {
+  const int lane = threadIdx.x % THREADS;
+  if (lane == 0) sh.count = 0;
+  row_sync<THREADS>();
+  likely([&](uint64_t key) {
     const int at = atomicAdd(&sh.count, 1);  // (their order in the list does not matter)
     if (at < TopShared<THREADS>::LIST) sh.list[at] = key;
   });
-  __syncthreads();
+  row_sync<THREADS>();
   const int count = sh.count;
   if (count <= TopShared<THREADS>::LIST) {
-    for (int i = threadIdx.x; i < count; i += THREADS) {
+    for (int i = lane; i < count; i += THREADS) {
       const uint64_t key = sh.list[i];
       int rank = 0;
       for (int j = 0; j < count; ++j) rank += sh.list[j] > key;
       if (rank < top) put(rank, key);
     }
-    for (int i = count + (int)threadIdx.x; i < top; i += THREADS) put(i, (uint64_t)0);
+    for (int i = count + lane; i < top; i += THREADS) put(i, (uint64_t)0);
     return;
   }
   uint64_t last = ~(uint64_t)0;
@@ -154,11 +170,11 @@ __device__ void top_keys(TopShared<THREADS>& sh, int top, EACH each, PUT put) {
       if (key < last && key > best) best = key;
     });
     best = wave_max(best);
-    if (threadIdx.x % 64 == 0) sh.waves[r & 1][threadIdx.x / 64] = best;
-    __syncthreads();
+    if (lane % 64 == 0) sh.waves[r & 1][lane / 64] = best;
+    row_sync<THREADS>();
 #pragma unroll
     for (int w = 0; w < THREADS / 64; ++w) best = sh.waves[r & 1][w] > best ? sh.waves[r & 1][w] : best;
-    if (threadIdx.x == 0) put(r, best);
+    if (lane == 0) put(r, best);
     last = best;
   }
 }
@@ -181,87 +197,115 @@ __device__ __forceinline__ float kth_largest(const float (&v)[PER], int k) {
   return __uint_as_float(found & 0x80000000u ? found ^ 0x80000000u : ~found);
 }
 
-template <class T, int THREADS, int EACH>
-__global__ __launch_bounds__(THREADS) void logp_part_kernel(Args a) {
-  constexpr int V = sizeof(T) == 2 ? 8 : 4, PACKS = EACH / V, WAVES = THREADS / 64;
+// Packs as they were loaded, sixteen-bit ones two elements to a register: what is widened before the fence is not kept for behind it.
+template <class P>
+__device__ __forceinline__ void forget(P& pack) {
+  if constexpr (sizeof(P) == 16) {
+    using Four = uint32_t __attribute__((ext_vector_type(4)));
+    Four w = __builtin_bit_cast(Four, pack);
+    uint32_t x = w[0], y = w[1], z = w[2], u = w[3];
+    asm volatile("" : "+v"(x), "+v"(y), "+v"(z), "+v"(u));
+    pack = __builtin_bit_cast(P, Four{x, y, z, u});
+  }
+}
+
+// One part of a row to THREADS lanes; where these are a wave, a workgroup has four rows.
+template <class T, int THREADS, int EACH, bool TOP>
+__global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) __attribute__((amdgpu_waves_per_eu(EACH * sizeof(T) > 64 ? 4 : 8))) void logp_part_kernel(Args a) {
+  constexpr int V = sizeof(T) == 2 ? 8 : 4, PACKS = EACH / V, WAVES = THREADS / 64, ROWS = THREADS == 64 ? 4 : 1;
   __shared__ Sums sums[WAVES];
-  __shared__ float groups[128];
-  __shared__ TopShared<THREADS> sh;
-  const int64_t n = workgroup() / a.parts, begin = workgroup() % a.parts * a.part_length;
-  if (n >= a.rows) return;
-  const int64_t left = a.vocab - begin, length = left < a.part_length ? left : a.part_length;  // (every part has an element)
+  const int lane = threadIdx.x % THREADS;
+  const int64_t unit = workgroup() * ROWS + threadIdx.x / THREADS, n = unit / a.parts, begin = unit % a.parts * a.part_length;
+  if (n >= a.rows) return;  // (all lanes of a row)
+  const int64_t left = a.vocab - begin;
+  const int length = (int)(left < a.part_length ? left : a.part_length);  // (every part has an element)
   const T* logits = static_cast<const T*>(a.logits) + n * a.row;
   const T* part = logits + begin;
-  const Given given = a.parts == 1 ? got_given(a, logits, n, threadIdx.x) : Given{0.0f, false};
-  float x[PACKS][V];
+  const auto at = [&](int p) { return (p * THREADS + lane) * V; };
   Loose<T, V> raw[PACKS];
 #pragma unroll
   for (int p = 0; p < PACKS; ++p) {
-    const int at = (p * THREADS + (int)threadIdx.x) * V;
-    raw[p] = got_loose<V>(part + at, (int)length - at);
-  }
-#pragma unroll
-  for (int p = 0; p < PACKS; ++p) {
-    const int at = (p * THREADS + (int)threadIdx.x) * V, count = (int)length - at;
-    widen(x[p], raw[p]);
-    if (count < V)
+    raw[p] = got_loose<V>(part + at(p), length - at(p));
+    if (length - at(p) < V)
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        if (j >= count) x[p][j] = minus_infinity();
+        if (j >= length - at(p)) raw[p].v[j] = (T)minus_infinity();
   }
+  const Given given = a.parts == 1 ? got_given(a, logits, n, lane) : Given{0.0f, false};
   float mine = minus_infinity();
 #pragma unroll
-  for (int p = 0; p < PACKS; ++p)
+  for (int p = 0; p < PACKS; ++p) {
+    float x[V];
+    widen(x, raw[p]);
 #pragma unroll
-    for (int j = 0; j < V; ++j) mine = fmaxf(mine, x[p][j]);
-  Sums r{mine, 0.0f, 0.0f};
+    for (int j = 0; j < V; ++j) mine = fmaxf(mine, x[j]);
+  }
+  Sums r{max_over<64>(mine), 0.0f, 0.0f};
+  // Exponents d = x c - ref', one operation: ref' is ref c rounded, and what the rounding left out, ref c = ref' + rest, is the same for all of them.
+  const float c = a.scale * LOG2E, ref = r.m == minus_infinity() ? 0.0f : r.m, ref_c = ref * c;
+  const bool far = !(__builtin_fabsf(ref_c) < 0x1p100f);  // (products past the range of numbers have no rest)
+  const float rest = far ? 0.0f : __builtin_fmaf(ref, c, -ref_c);
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) r.m = fmaxf(r.m, __shfl_xor(r.m, d));
-  const float c = a.scale * LOG2E, ref = r.m == minus_infinity() ? 0.0f : r.m;
-#pragma unroll
-  for (int p = 0; p < PACKS; ++p)
+  for (int p = 0; p < PACKS; ++p) {
+    float x[V];
+    __builtin_amdgcn_sched_barrier(0);  // (all packs' exponentials side by side take too many registers)
+    forget(raw[p]);
+    widen(x, raw[p]);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const float d = (x[p][j] - ref) * c, e = __builtin_amdgcn_exp2f(d);
+      const float d = far ? (x[j] - ref) * c : __builtin_fmaf(x[j], c, -ref_c), e = __builtin_amdgcn_exp2f(d);
       r.s += e, r.t += weighted(e, d);
     }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) r.s += __shfl_xor(r.s, d), r.t += __shfl_xor(r.t, d);
+  }
+  const float by = __builtin_amdgcn_exp2f(-rest);
+  r.t = by * (r.t - rest * r.s), r.s *= by;
+  r.s = sum_over<64>(r.s), r.t = sum_over<64>(r.t);
   if constexpr (WAVES > 1) {
     if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = r;
     __syncthreads();
-    r = sums[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) r = join(r, sums[w], c);
+    const int w = threadIdx.x % 64;
+    r = joined(w < WAVES ? sums[w] : Sums{minus_infinity(), 0.0f, 0.0f}, c);
   }
   float log_sum = 0.0f;
-  if (a.parts == 1) log_sum = finish_row(a, logits, n, r, given);
-  else if (threadIdx.x == 0) a.sums[workgroup()] = r;
-  if (!a.top) return;
+  if (a.parts == 1) log_sum = finish_row<THREADS>(a, logits, n, r, given);
+  else if (lane == 0) a.sums[unit] = r;
+  if constexpr (!TOP) return;
+  __shared__ float groups[128];
+  __shared__ TopShared<THREADS> shared[ROWS];
   float least;  // no fewer than `top` elements reach it
   if constexpr (WAVES == 1) {
     const float one[1] = {mine};
     least = kth_largest(one, a.top);
   } else {
     constexpr int LANES = THREADS / 128;  // of a group
-#pragma unroll
-    for (int d = 1; d < LANES; d *= 2) mine = fmaxf(mine, __shfl_xor(mine, d));
-    if (threadIdx.x % LANES == 0) groups[threadIdx.x / LANES] = mine;
+    mine = max_over<LANES>(mine);
+    if (lane % LANES == 0) groups[lane / LANES] = mine;
     __syncthreads();
-    const float two[2] = {groups[threadIdx.x % 64], groups[threadIdx.x % 64 + 64]};
+    const float two[2] = {groups[lane % 64], groups[lane % 64 + 64]};
     least = kth_largest(two, a.top);
   }
-  const auto each = [&](auto fn) {
+  // The few that reach it are read again, from the caches; so are all of them where the list overflows.
+  const auto likely = [&](auto fn) {
 #pragma unroll
-    for (int p = 0; p < PACKS; ++p)
+    for (int p = 0; p < PACKS; ++p) {
+      float x[V];
+      forget(raw[p]);
+      widen(x, raw[p]);
+      uint32_t reach = 0;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int at = (p * THREADS + (int)threadIdx.x) * V + j;
-        if (!(x[p][j] < least) && at < length) fn(key_of(x[p][j], begin + at));
+      for (int j = 0; j < V; ++j) reach |= (uint32_t)!(x[j] < least) << j;
+      for (; reach; reach &= reach - 1) {
+        const int i = at(p) + __builtin_ctz(reach);
+        if (i < length) fn(key_of((float)part[i], begin + i));
       }
+    }
   };
-  top_keys<THREADS>(sh, a.top, each, [&](int rank, uint64_t key) {
-    if (a.parts > 1) a.keys[workgroup() * a.top + rank] = key;
+  const auto each = [&](auto fn) {
+#pragma unroll 4
+    for (int i = lane; i < length; i += THREADS) fn(key_of((float)part[i], begin + i));
+  };
+  top_keys<THREADS>(shared[threadIdx.x / THREADS], a.top, likely, each, [&](int rank, uint64_t key) {
+    if (a.parts > 1) a.keys[unit * a.top + rank] = key;
     else put_top(a, n, rank, key, r, log_sum);
   });
 }
@@ -287,8 +331,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void logp_join_kernel(Args a) {
   const float c = a.scale * LOG2E;
   Sums r{minus_infinity(), 0.0f, 0.0f};
   for (int p = threadIdx.x; p < a.parts; p += JOIN_THREADS) r = join(r, a.sums[n * a.parts + p], c);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) r = join(r, Sums{__shfl_xor(r.m, d), __shfl_xor(r.s, d), __shfl_xor(r.t, d)}, c);
+  r = joined(r, c);
   const auto each = [&](auto fn) {
 #pragma unroll
     for (int k = 0; k < JOIN_KEYS; ++k)
@@ -309,15 +352,16 @@ __global__ __launch_bounds__(JOIN_THREADS) void logp_join_kernel(Args a) {
   for (int w = 1; w < JOIN_THREADS / 64; ++w) r = join(r, sums[w], c);
 #pragma unroll
   for (int w = 0; w < JOIN_THREADS / 64; ++w) least = sh.waves[0][w] > least ? sh.waves[0][w] : least;
-  const float log_sum = finish_row(a, logits, n, r, given);
+  const float log_sum = finish_row<JOIN_THREADS>(a, logits, n, r, given);
   if (!a.top) return;
   __syncthreads();  // (top_keys writes sh.waves again)
+  const auto all = [&](auto fn) { each([&](uint64_t key, int) { fn(key); }); };
   const auto likely = [&](auto fn) {
     each([&](uint64_t key, int) {
       if (key >= least) fn(key);
     });
   };
-  top_keys<JOIN_THREADS>(sh, a.top, likely, [&](int rank, uint64_t key) { put_top(a, n, rank, key, r, log_sum); });
+  top_keys<JOIN_THREADS>(sh, a.top, likely, all, [&](int rank, uint64_t key) { put_top(a, n, rank, key, r, log_sum); });
 }
 
 // ---- backward ----------------------------------------------------------------------------------------------------------
@@ -374,8 +418,7 @@ __global__ __launch_bounds__(THREADS) void logp_backward_kernel(BackArgs a) {
       total += g;
       if (threadIdx.x < 64) tokens[j] = known ? t : -1, errors[j] = g;
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
+    total = sum_over<64>(total);
   }
   const float by = a.scale, c = by * LOG2E, log2_sum = log_sum * LOG2E;
   const auto gradient = [&](float l, float g) {
@@ -430,13 +473,16 @@ struct Plan {
 // One part where a workgroup holds the row.  Else the second kernel is needed anyway, and parts are as short as a thousand workgroups ask.
 Plan plan_of(const cnn_log_probs_shape& s) {
   Plan p{};
-  constexpr struct { int threads, each; } FORMS[] = {{64, 8}, {64, 16}, {64, 32}, {256, 16}, {256, 32}, {1024, 32}};
+  constexpr struct { int threads, each; } FORMS[] = {{64, 8}, {64, 16}, {64, 32}, {256, 16}, {256, 32}, {1024, 16}, {1024, 32}, {1024, 64}};
+  const int most_each = s.type != CNN_F32 ? 64 : s.rows <= 256 ? 32 : 16;
+  const int64_t longest = 1024 * most_each;
   int64_t want = s.vocab;
-  if (want > 32768) {
+  if (want > longest) {
     want = s.rows * s.vocab / 1024;
-    want = want < 4096 ? 4096 : want > 32768 ? 32768 : want;
+    want = want < 4096 ? 4096 : want > longest ? longest : want;
   }
   for (const auto& f : FORMS) {
+    if (f.each > most_each) continue;
     p.threads = f.threads, p.each = f.each;
     if (want <= (int64_t)f.threads * f.each) break;
   }
@@ -451,15 +497,21 @@ Plan plan_of(const cnn_log_probs_shape& s) {
   return p;
 }
 
-template <class T>
+template <class T, bool TOP>
 void launch_part(const Args& a, const Plan& p, hipStream_t st) {
-  const dim3 grid = grid_of(a.rows * a.parts);
-  if (p.threads == 64 && p.each == 8) logp_part_kernel<T, 64, 8><<<grid, 64, 0, st>>>(a);
-  else if (p.threads == 64 && p.each == 16) logp_part_kernel<T, 64, 16><<<grid, 64, 0, st>>>(a);
-  else if (p.threads == 64) logp_part_kernel<T, 64, 32><<<grid, 64, 0, st>>>(a);
-  else if (p.threads == 256 && p.each == 16) logp_part_kernel<T, 256, 16><<<grid, 256, 0, st>>>(a);
-  else if (p.threads == 256) logp_part_kernel<T, 256, 32><<<grid, 256, 0, st>>>(a);
-  else logp_part_kernel<T, 1024, 32><<<grid, 1024, 0, st>>>(a);
+  const int64_t units = a.rows * a.parts;
+  const dim3 grid = grid_of(units), fours = grid_of((units + 3) / 4);
+  if constexpr (sizeof(T) == 2)
+    if (p.each == 64) return logp_part_kernel<T, 1024, 64, TOP><<<grid, 1024, 0, st>>>(a);
+  if (p.each == 32) {
+    if (p.threads == 64) return logp_part_kernel<T, 64, 32, TOP><<<fours, 256, 0, st>>>(a);
+    if (p.threads == 256) return logp_part_kernel<T, 256, 32, TOP><<<grid, 256, 0, st>>>(a);
+    return logp_part_kernel<T, 1024, 32, TOP><<<grid, 1024, 0, st>>>(a);
+  }
+  if (p.threads == 64 && p.each == 8) logp_part_kernel<T, 64, 8, TOP><<<fours, 256, 0, st>>>(a);
+  else if (p.threads == 64) logp_part_kernel<T, 64, 16, TOP><<<fours, 256, 0, st>>>(a);
+  else if (p.threads == 256) logp_part_kernel<T, 256, 16, TOP><<<grid, 256, 0, st>>>(a);
+  else logp_part_kernel<T, 1024, 16, TOP><<<grid, 1024, 0, st>>>(a);
 }
 
 template <class T, int THREADS, int PACKS, bool PAST_CACHES>
@@ -493,7 +545,8 @@ int cnn_log_probs_fwd(const cnn_log_probs_shape* s, const cnn_rows* logits, cons
   hipStream_t st = (hipStream_t)hip_stream;
   return with_type(s->type, [&](auto t) {
     using T = decltype(t);
-    launch_part<T>(a, p, st);
+    if (a.top) launch_part<T, true>(a, p, st);
+    else launch_part<T, false>(a, p, st);
     if (launch_status() != CNN_OK) return CNN_EHIP;
     if (p.parts == 1) return CNN_OK;
     logp_join_kernel<T><<<grid_of(a.rows), JOIN_THREADS, 0, st>>>(a);

@@ -15,6 +15,7 @@
 #pragma once
 
 #include "cnn_common.h"
+#include "cnn_lanes.h"
 #include "cnn_types.h"
 
 namespace cnn {
@@ -54,9 +55,7 @@ struct TeamSum {
   float buffer[LANES > 64 ? 2 : 1][LANES > 64 ? WAVES : 1][COUNT];
   __device__ __forceinline__ void sum(float (&v)[COUNT], int turn) {
 #pragma unroll
-    for (int c = 0; c < COUNT; ++c)
-#pragma unroll
-      for (int d = 1; d < (LANES < 64 ? LANES : 64); d *= 2) v[c] += __shfl_xor(v[c], d);
+    for (int c = 0; c < COUNT; ++c) v[c] = sum_over<(LANES < 64 ? LANES : 64)>(v[c]);
     if constexpr (LANES > 64) {
       // (turns use the two buffers by turns: whoever writes one again has passed the barrier of the turn between)
       float(&b)[WAVES][COUNT] = buffer[turn & 1];

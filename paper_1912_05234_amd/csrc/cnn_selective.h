@@ -24,6 +24,7 @@
 #include <type_traits>
 
 #include "cnn_common.h"
+#include "cnn_lanes.h"
 #include "cnn_types.h"
 
 namespace cnn {
@@ -56,22 +57,6 @@ __device__ __forceinline__ int length_of(const Args& a, int b) {
   if (!a.lengths) return a.T;
   const int n = a.lengths[b];
   return n < 0 ? 0 : n > a.T ? a.T : n;
-}
-
-template <int CTRL>
-__device__ __forceinline__ float lane_moved(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-constexpr int SWAP_1 = 0xB1, SWAP_2 = 0x4E, HALF_MIRROR = 0x141, MIRROR = 0x140, ROTATE_8 = 0x128;
-
-// The sum over S neighbouring lanes, in all of them.
-template <int S>
-__device__ __forceinline__ float shared_sum(float v) {
-  if constexpr (S > 1) v += lane_moved<SWAP_1>(v);
-  if constexpr (S > 2) v += lane_moved<SWAP_2>(v);
-  if constexpr (S > 4) v += lane_moved<HALF_MIRROR>(v);
-  if constexpr (S > 8) v += lane_moved<MIRROR>(v);
-  return v;
 }
 
 // Lane k's value of S neighbouring lanes, in all of them.
@@ -335,7 +320,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(S == 1 ? 2 :
         }
       }
       if constexpr (!ENDS) {
-        y_t = shared_sum<S>(y_t);
+        y_t = sum_over<S>(y_t);
         if (p.s == K % S) out.v[K / S] = y_t;
       }
     });
@@ -539,7 +524,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void se
         d_a[i] += d * along;
         by_a += a2[i] * along;
       }
-      by_b = shared_sum<S>(by_b), by_a = shared_sum<S>(by_a);
+      by_b = sum_over<S>(by_b), by_a = sum_over<S>(by_a);
       if (p.s == K % S) sum_b.v[K / S] = by_b, sum_a.v[K / S] = by_a;
       Sums::sum(v);
 #pragma unroll
@@ -572,7 +557,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void se
     }
   }
   if (a.last && p.segment == 0) put_states(a.last + p.b * states, q, p, a);
-  d_skip = shared_sum<S>(d_skip), d_bias = shared_sum<S>(d_bias);
+  d_skip = sum_over<S>(d_skip), d_bias = sum_over<S>(d_bias);
   float* partial = a.partial + (at * a.D + p.channel) * (a.N + 2);
   if (p.mine) {
 #pragma unroll

@@ -170,6 +170,6 @@ def test_log_probs_refusals():
 def test_log_probs_workspaces():
     """None for rows that a workgroup holds; sums and keys of the parts of longer ones."""
     q = binding.lib().cnn_log_probs_fwd_workspace_bytes
-    assert q(logp(vocab=32768)) == 0 and q(None) == 0
-    assert q(logp(rows=1, vocab=32769, top=0)) >= 2 * 12
+    assert q(logp(vocab=65536)) == q(logp(vocab=32768, type_=0)) == q(logp(rows=1000, vocab=16384, type_=0)) == 0 and q(None) == 0
+    assert q(logp(rows=1, vocab=65537, top=0)) >= 2 * 12 and q(logp(rows=1, vocab=32769, top=0, type_=0)) >= 2 * 12
     assert q(logp(rows=1, vocab=1 << 24, top=64)) >= 512 * (12 + 64 * 8)
