@@ -117,8 +117,9 @@ __device__ __forceinline__ void put_top(const Args& a, int64_t n, int rank, uint
   a.top_log_probs[n * a.top + rank] = (value_of(key) - base) * a.scale - log_sum;
 }
 
-__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-  return over_lanes<64>(v, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+template <int LANES>
+__device__ __forceinline__ uint64_t largest_over(uint64_t v) {
+  return over_lanes<LANES>(v, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
 }
 
 // Waits for the lanes that share a row.  (A wave's own accesses to LDS are in order.)
@@ -134,9 +135,9 @@ __device__ __forceinline__ void row_sync() {
 
 template <int THREADS>
 struct TopShared {
-  static constexpr int LIST = THREADS > 64 ? 1024 : 256;
+  static constexpr int LIST = THREADS > 64 ? 1024 : THREADS * 8;
   uint64_t list[LIST];
-  uint64_t waves[2][THREADS / 64];
+  uint64_t waves[2][THREADS > 64 ? THREADS / 64 : 1];
   int count;
 };
 
@@ -169,19 +170,21 @@ __device__ void top_keys(TopShared<THREADS>& sh, int top, LIKELY likely, EACH ea
     each([&](uint64_t key) {
       if (key < last && key > best) best = key;
     });
-    best = wave_max(best);
-    if (lane % 64 == 0) sh.waves[r & 1][lane / 64] = best;
-    row_sync<THREADS>();
+    best = largest_over<(THREADS < 64 ? THREADS : 64)>(best);
+    if constexpr (THREADS > 64) {
+      if (lane % 64 == 0) sh.waves[r & 1][lane / 64] = best;
+      row_sync<THREADS>();
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) best = sh.waves[r & 1][w] > best ? sh.waves[r & 1][w] : best;
+      for (int w = 0; w < THREADS / 64; ++w) best = sh.waves[r & 1][w] > best ? sh.waves[r & 1][w] : best;
+    }
     if (lane == 0) put(r, best);
     last = best;
   }
 }
 
-// A lower bound of the k-th largest (k <= 64 * PER) of 64 * PER values, PER to a lane, the same in every lane of a wave: the sixteen high bits of its
-// key, found bit by bit.  NaN, to which nothing compares as smaller, where that is -inf.
-template <int PER>
+// A lower bound of the k-th largest of LANES * PER values, PER to a lane, the same in these lanes: the sixteen high bits of its key, found bit
+// by bit.  NaN, to which nothing compares as smaller, where that is -inf or there are fewer than k.
+template <int LANES, int PER>
 __device__ __forceinline__ float kth_largest(const float (&v)[PER], int k) {
   uint32_t key[PER], found = 0;
 #pragma unroll
@@ -191,7 +194,11 @@ __device__ __forceinline__ float kth_largest(const float (&v)[PER], int k) {
     const uint32_t now = found | 1u << bit;
     int reach = 0;
 #pragma unroll
-    for (int p = 0; p < PER; ++p) reach += __popcll(__ballot(key[p] >= now));
+    for (int p = 0; p < PER; ++p) {
+      uint64_t lanes = __ballot(key[p] >= now);
+      if constexpr (LANES < 64) lanes = lanes >> (threadIdx.x & 63 & ~(LANES - 1)) & ((1ull << (LANES & 63)) - 1);
+      reach += __popcll(lanes);
+    }
     if (reach >= k) found = now;
   }
   return __uint_as_float(found & 0x80000000u ? found ^ 0x80000000u : ~found);
@@ -209,10 +216,10 @@ __device__ __forceinline__ void forget(P& pack) {
   }
 }
 
-// One part of a row to THREADS lanes; where these are a wave, a workgroup has four rows.
+// One part of a row to THREADS lanes; where these are a wave or less, a workgroup has several rows.
 template <class T, int THREADS, int EACH, bool TOP>
 __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) __attribute__((amdgpu_waves_per_eu(EACH * sizeof(T) > 64 ? 4 : 8))) void logp_part_kernel(Args a) {
-  constexpr int V = sizeof(T) == 2 ? 8 : 4, PACKS = EACH / V, WAVES = THREADS / 64, ROWS = THREADS == 64 ? 4 : 1;
+  constexpr int V = sizeof(T) == 2 ? 8 : 4, PACKS = EACH / V, LANES = THREADS < 64 ? THREADS : 64, WAVES = THREADS / LANES, ROWS = THREADS > 64 ? 1 : 256 / THREADS;
   __shared__ Sums sums[WAVES];
   const int lane = threadIdx.x % THREADS;
   const int64_t unit = workgroup() * ROWS + threadIdx.x / THREADS, n = unit / a.parts, begin = unit % a.parts * a.part_length;
@@ -240,7 +247,7 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) __attribute__((amdgp
 #pragma unroll
     for (int j = 0; j < V; ++j) mine = fmaxf(mine, x[j]);
   }
-  Sums r{max_over<64>(mine), 0.0f, 0.0f};
+  Sums r{max_over<LANES>(mine), 0.0f, 0.0f};
   // Exponents d = x c - ref', one operation: ref' is ref c rounded, and what the rounding left out, ref c = ref' + rest, is the same for all of them.
   const float c = a.scale * LOG2E, ref = r.m == minus_infinity() ? 0.0f : r.m, ref_c = ref * c;
   const bool far = !(__builtin_fabsf(ref_c) < 0x1p100f);  // (products past the range of numbers have no rest)
@@ -259,7 +266,7 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) __attribute__((amdgp
   }
   const float by = __builtin_amdgcn_exp2f(-rest);
   r.t = by * (r.t - rest * r.s), r.s *= by;
-  r.s = sum_over<64>(r.s), r.t = sum_over<64>(r.t);
+  r.s = sum_over<LANES>(r.s), r.t = sum_over<LANES>(r.t);
   if constexpr (WAVES > 1) {
     if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = r;
     __syncthreads();
@@ -275,14 +282,14 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) __attribute__((amdgp
   float least;  // no fewer than `top` elements reach it
   if constexpr (WAVES == 1) {
     const float one[1] = {mine};
-    least = kth_largest(one, a.top);
+    least = kth_largest<LANES>(one, a.top);
   } else {
-    constexpr int LANES = THREADS / 128;  // of a group
-    mine = max_over<LANES>(mine);
-    if (lane % LANES == 0) groups[lane / LANES] = mine;
+    constexpr int GROUP = THREADS / 128;  // lanes
+    mine = max_over<GROUP>(mine);
+    if (lane % GROUP == 0) groups[lane / GROUP] = mine;
     __syncthreads();
     const float two[2] = {groups[lane % 64], groups[lane % 64 + 64]};
-    least = kth_largest(two, a.top);
+    least = kth_largest<64>(two, a.top);
   }
   // The few that reach it are read again, from the caches; so are all of them where the list overflows.
   const auto likely = [&](auto fn) {
@@ -343,7 +350,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void logp_join_kernel(Args a) {
     each([&](uint64_t key, int i) {
       if (i % a.top == a.top - 1 && key > least) least = key;
     });
-    least = wave_max(least);
+    least = largest_over<64>(least);
   }
   if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = r, sh.waves[0][threadIdx.x / 64] = least;
   __syncthreads();
@@ -473,7 +480,7 @@ struct Plan {
 // One part where a workgroup holds the row.  Else the second kernel is needed anyway, and parts are as short as a thousand workgroups ask.
 Plan plan_of(const cnn_log_probs_shape& s) {
   Plan p{};
-  constexpr struct { int threads, each; } FORMS[] = {{64, 8}, {64, 16}, {64, 32}, {256, 16}, {256, 32}, {1024, 16}, {1024, 32}, {1024, 64}};
+  constexpr struct { int threads, each; } FORMS[] = {{16, 8}, {32, 8}, {64, 8}, {64, 16}, {64, 32}, {256, 16}, {256, 32}, {1024, 16}, {1024, 32}, {1024, 64}};
   const int most_each = s.type != CNN_F32 ? 64 : s.rows <= 256 ? 32 : 16;
   const int64_t longest = 1024 * most_each;
   int64_t want = s.vocab;
@@ -499,19 +506,21 @@ Plan plan_of(const cnn_log_probs_shape& s) {
 
 template <class T, bool TOP>
 void launch_part(const Args& a, const Plan& p, hipStream_t st) {
-  const int64_t units = a.rows * a.parts;
-  const dim3 grid = grid_of(units), fours = grid_of((units + 3) / 4);
-  if constexpr (sizeof(T) == 2)
-    if (p.each == 64) return logp_part_kernel<T, 1024, 64, TOP><<<grid, 1024, 0, st>>>(a);
-  if (p.each == 32) {
-    if (p.threads == 64) return logp_part_kernel<T, 64, 32, TOP><<<fours, 256, 0, st>>>(a);
-    if (p.threads == 256) return logp_part_kernel<T, 256, 32, TOP><<<grid, 256, 0, st>>>(a);
-    return logp_part_kernel<T, 1024, 32, TOP><<<grid, 1024, 0, st>>>(a);
-  }
-  if (p.threads == 64 && p.each == 8) logp_part_kernel<T, 64, 8, TOP><<<fours, 256, 0, st>>>(a);
-  else if (p.threads == 64) logp_part_kernel<T, 64, 16, TOP><<<fours, 256, 0, st>>>(a);
-  else if (p.threads == 256) logp_part_kernel<T, 256, 16, TOP><<<grid, 256, 0, st>>>(a);
-  else logp_part_kernel<T, 1024, 16, TOP><<<grid, 1024, 0, st>>>(a);
+  const auto with = [&](auto threads, auto each) {
+    constexpr int THREADS = decltype(threads)::value, ROWS = THREADS > 64 ? 1 : 256 / THREADS;
+    if (p.threads != THREADS || p.each != decltype(each)::value) return;
+    logp_part_kernel<T, THREADS, decltype(each)::value, TOP><<<grid_of((a.rows * a.parts + ROWS - 1) / ROWS), THREADS * ROWS, 0, st>>>(a);
+  };
+  using std::integral_constant;
+  const integral_constant<int, 8> e8;
+  const integral_constant<int, 16> e16, lanes16;
+  const integral_constant<int, 32> e32, lanes32;
+  const integral_constant<int, 64> lanes64;
+  const integral_constant<int, 256> lanes256;
+  const integral_constant<int, 1024> lanes1024;
+  with(lanes16, e8), with(lanes32, e8), with(lanes64, e8), with(lanes64, e16), with(lanes64, e32);
+  with(lanes256, e16), with(lanes256, e32), with(lanes1024, e16), with(lanes1024, e32);
+  if constexpr (sizeof(T) == 2) with(lanes1024, integral_constant<int, 64>{});
 }
 
 template <class T, int THREADS, int PACKS, bool PAST_CACHES>
