@@ -46,11 +46,12 @@ struct Args {
   const int32_t* lengths;
   const float *first, *d_last;  // [B][D][N], nullable
   void *y, *d_x, *d_dt;         // [B][T][D]
+  void *d_b, *d_c;              // [B][T][G][N]
   float* last;                  // the final state, or the error of the first; nullable
   float *ends, *errors, *sums;  // of the segments: [segments][B][D][N], the same, [segments][B][D]
-  float *partial, *shared;      // backward: [segments][B][D][N + 2], [channel blocks][B][T][G][2][NP]
+  float *partial, *shared;      // backward: [segments][B][D][N + 2]; [workgroups][B][T][G][2][NP] where these are several
   int T, length;                // of a segment
-  int B, D, N, G, per, blocks, segments, softplus;  // per: channels of a group; blocks: waves that these take
+  int B, D, N, G, per, blocks, workgroups, segments, softplus;  // per: channels of a group; blocks: waves that these take; workgroups: backward
 };
 
 __device__ __forceinline__ int length_of(const Args& a, int b) {
@@ -68,31 +69,36 @@ __device__ __forceinline__ float from_lane(float v) {
   else return __shfl(v, (int)(threadIdx.x & ~(S - 1)) + K);
 }
 
-// softplus(z) = ln(1 + e^z).  ln(1 + e) for small e by Kahan's formula e ln(w) / (w - 1) with w = 1 + e rounded (Goldberg, "What every
-// computer scientist should know about floating-point arithmetic", theorem 4).
-__device__ __forceinline__ float softplus_of(float z) {
+// softplus(z) = ln(1 + e^z), and its slope e^z / (1 + e^z).  ln(1 + e) for small e by Kahan's formula e ln(w) / (w - 1) with w = 1 + e rounded (Goldberg,
+// "What every computer scientist should know about floating-point arithmetic", theorem 4).
+__device__ __forceinline__ float softplus_of(float z, float& slope) {
   const float e = __builtin_amdgcn_exp2f(z * -NEG_LOG2E), w = 1.0f + e;
   const float l = __builtin_amdgcn_logf(w) * 0.69314718055994530942f;
   const float r = w == 1.0f ? e : e * l * __builtin_amdgcn_rcpf(w - 1.0f);
+  slope = z > 20.0f ? 1.0f : e * __builtin_amdgcn_rcpf(w);
   return z > 20.0f ? z : r;  // (z + e^-z: the same float)
 }
+__device__ __forceinline__ float softplus_of(float z) {
+  float slope;
+  return softplus_of(z, slope);
+}
 
-// A wave's place: its channel and states, the tokens of its segment.
+// A lane's place: its channel and states, the tokens of its wave's segment.
 struct Place {
   int b, t0, t1, end;  // tokens t0 .. t1 - 1, of which those from `end` on are past the sequence
   int segment, group, channel, state, s, block;
   bool mine;  // a channel of the group (else the lane has the last one's parameters, inputs and errors of zero, and stores nothing)
 };
 
-template <int NL, int S>
-__device__ __forceinline__ Place place_of(const Args& a) {
-  constexpr int CHANNELS = 64 / S;
+template <int NL, int S, int WAVES>
+__device__ __forceinline__ Place place_of(const Args& a, int blocks) {
+  constexpr int CHANNELS = WAVES * 64 / S;
   Place p;
   int64_t w = workgroup();
-  p.block = (int)(w % a.blocks), w /= a.blocks;
+  p.block = (int)(w % blocks), w /= blocks;
   p.group = (int)(w % a.G), w /= a.G;
   p.b = (int)(w % a.B), p.segment = (int)(w / a.B);
-  const int lane = threadIdx.x, in = p.block * CHANNELS + lane / S;
+  const int lane = threadIdx.x, in = p.block * CHANNELS + lane / S;  // (of all waves)
   p.mine = in < a.per;
   p.channel = p.group * a.per + (p.mine ? in : a.per - 1);
   p.s = lane % S, p.state = p.s * NL;
@@ -178,9 +184,9 @@ __device__ __forceinline__ void put_tokens(T* to, const Once<float, S>& from, co
 }
 
 // Rows of B and C of U tokens on their way through LDS, as floats; zeros past N.
-template <class T, int NP>
+template <class T, int NP, int THREADS = 64>
 struct Row {
-  static constexpr int EACH = U * NP >= 64 ? U * NP / 64 : 1;
+  static constexpr int EACH = U * NP >= THREADS ? U * NP / THREADS : 1;
   const T* base;
   int64_t token;
   T v[EACH];
@@ -191,14 +197,14 @@ struct Row {
     const T* row = base + t * token;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int e = i * 64 + (int)threadIdx.x, k = e / NP % U, n = e % NP, last = p.end - 1 - t;
+      const int e = i * THREADS + (int)threadIdx.x, k = e / NP % U, n = e % NP, last = p.end - 1 - t;
       v[i] = row[(uint32_t)(k < last ? k : last) * (uint32_t)token + (uint32_t)(n < a.N ? n : a.N - 1)];
     }
   }
   __device__ __forceinline__ void put(float* to, const Args& a) const {
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int e = i * 64 + (int)threadIdx.x;
+      const int e = i * THREADS + (int)threadIdx.x;
       if (e < U * NP) to[e] = e % NP < a.N ? (float)v[i] : 0.0f;
     }
   }
@@ -230,15 +236,16 @@ __device__ __forceinline__ void get_decays(float (&a2)[NL], const Args& a, const
   for (int i = 0; i < NL; ++i) a2[i] *= -NEG_LOG2E;
 }
 
-// D_t and D_t x_t of a lane's own tokens, and x_t; zeros past the sequence (there the state stays) and for channels that are none.
+// D_t, its slope, D_t x_t and x_t of a lane's own tokens; zeros past the sequence (there the state stays) and for channels that are none.
 template <class T, int S>
-__device__ __forceinline__ void get_steps(const Args& a, const Place& p, int t, float bias, const Once<T, S>& x, const Once<T, S>& dt, Once<float, S>& z,
+__device__ __forceinline__ void get_steps(const Args& a, const Place& p, int t, float bias, const Once<T, S>& x, const Once<T, S>& dt, Once<float, S>& slope,
                                           Once<float, S>& delta, Once<float, S>& u, Once<float, S>& input) {
 #pragma unroll
   for (int i = 0; i < Own<S>::EACH; ++i) {
     const bool there = p.mine && t + i * S + p.s < p.end;
-    z.v[i] = (float)dt.v[i] + bias;
-    delta.v[i] = there ? (a.softplus ? softplus_of(z.v[i]) : z.v[i]) : 0.0f;
+    const float z = (float)dt.v[i] + bias;
+    slope.v[i] = 1.0f;
+    delta.v[i] = there ? (a.softplus ? softplus_of(z, slope.v[i]) : z) : 0.0f;
     input.v[i] = there ? (float)x.v[i] : 0.0f;
     u.v[i] = delta.v[i] * input.v[i];
   }
@@ -257,7 +264,7 @@ template <class T, int NL, int S, bool ENDS, bool ERRORS>
 __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(S == 1 ? 2 : S == 16 ? 3 : 4))) void selective_tokens_kernel(Args a) {
   constexpr int NP = NL * S;
   __shared__ __align__(16) float rows[2][2][U * NP];
-  const Place p = place_of<NL, S>(a);
+  const Place p = place_of<NL, S, 1>(a, a.blocks);
   float a2[NL], h[NL], q[ERRORS ? NL : 1], run[ERRORS ? NL : 1];
   get_decays(a2, a, p);
   const int64_t states = (int64_t)a.D * a.N;
@@ -280,8 +287,8 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(S == 1 ? 2 :
   if constexpr (NEEDS_C) c.get(p, a, p.t0);
   int turn = 0, t = p.t0;
   for (; t < p.end; t += U, turn ^= 1) {
-    Once<float, S> z, delta, u, x, d_y, out;
-    get_steps(a, p, t, bias, next_x, next_dt, z, delta, u, x);
+    Once<float, S> slope, delta, u, x, d_y, out;
+    get_steps(a, p, t, bias, next_x, next_dt, slope, delta, u, x);
     if constexpr (ERRORS) get_errors(p, t, next_d, d_y);
     b.put(rows[turn][0], a);
     if constexpr (NEEDS_C) c.put(rows[turn][1], a);
@@ -399,7 +406,7 @@ struct ChannelSums {
     if constexpr (BITS > 5) v[0] = add_across<1>(v[0]);
   }
   static __device__ __forceinline__ int first() {
-    const int lane = threadIdx.x;
+    const int lane = threadIdx.x;  // (its low six bits)
     int at = 0;
     if (lane & 32) at += COUNT / 2;
     if (lane & 16) at += COUNT / 4;
@@ -413,13 +420,16 @@ struct ChannelSums {
   }
 };
 
-template <class T, int NL, int S>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void selective_gradient_kernel(Args a) {
-  constexpr int NP = NL * S, EACH = Own<S>::EACH;
+// WAVES waves to a workgroup, of neighbouring channels: they share the rows of B and C, and their sums over channels meet in LDS.
+template <class T, int NL, int S, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void selective_gradient_kernel(Args a) {
+  constexpr int NP = NL * S, EACH = Own<S>::EACH, THREADS = 64 * WAVES;
   using Sums = ChannelSums<S, 2 * NL>;
   __shared__ __align__(16) float rows[2][2][U * NP];
-  __shared__ __align__(16) f4 kept[LONGEST / U][NL / 4][64];
-  const Place p = place_of<NL, S>(a);
+  __shared__ __align__(16) f4 kept[WAVES][LONGEST / U][NL / 4][64];
+  __shared__ float sums[2][WAVES][U * 2 * NP];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const Place p = place_of<NL, S, WAVES>(a, a.workgroups);
   float a2[NL], h[NL], q[NL], d_a[NL], d_skip = 0.0f, d_bias = 0.0f;
   get_decays(a2, a, p);
   const int64_t states = (int64_t)a.D * a.N, at = (int64_t)p.segment * a.B + p.b;
@@ -433,17 +443,17 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void se
   const int chunks = (p.end - p.t0 + U - 1) / U;
   const Source<T, S> from_x(a.x, p), from_dt(a.dt, p), from_d(a.d_y, p);
   Once<T, S> next_x, next_dt, next_d;
-  Once<float, S> z, delta, u, x, d_y;
-  Row<T, NP> b(a.b, p), c(a.c, p);
+  Once<float, S> slope, delta, u, x, d_y;
+  Row<T, NP, THREADS> b(a.b, p), c(a.c, p);
   int turn = 0;
   // forwards: the state in front of every chunk
   from_x.get(next_x, p, p.t0), from_dt.get(next_dt, p, p.t0), b.get(p, a, p.t0);
   for (int j = 0; j < chunks; ++j, turn ^= 1) {
     const int t = p.t0 + j * U;
 #pragma unroll
-    for (int i = 0; i < NL; i += 4) kept[j][i / 4][threadIdx.x] = f4{h[i], h[i + 1], h[i + 2], h[i + 3]};
+    for (int i = 0; i < NL; i += 4) kept[wave][j][i / 4][lane] = f4{h[i], h[i + 1], h[i + 2], h[i + 3]};
     if (j == chunks - 1) break;
-    get_steps(a, p, t, bias, next_x, next_dt, z, delta, u, x);
+    get_steps(a, p, t, bias, next_x, next_dt, slope, delta, u, x);
     b.put(rows[turn][0], a);
     __syncthreads();
     from_x.get(next_x, p, t + U), from_dt.get(next_dt, p, t + U), b.get(p, a, t + U);
@@ -465,21 +475,33 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void se
   // backwards; next_x, next_dt and b hold the last chunk
   const int last = p.t0 + (chunks - 1) * U;
   from_d.get(next_d, p, last), c.get(p, a, last);
-  const int value = Sums::first(), row = value < NL ? 0 : 1, state = p.state + value - row * NL;
-  float* shared = a.shared + (((int64_t)p.block * a.B + p.b) * a.T * a.G + p.group) * 2 * NP;
-  const uint32_t shared_lane = row * NP + state, shared_token = (uint32_t)a.G * 2 * NP;
+  const int value = Sums::first(), sum_at = (value < NL ? 0 : NP - NL) + p.state + value;
+  // The sums of the chunk from token t on, which every wave has left in sums[from]: one after the other, U tokens of 2 NP values to the workgroup.
+  const auto put_sums = [&](int t, int from) {
+    for (int e = threadIdx.x; e < U * 2 * NP; e += THREADS) {
+      const int k = e / (2 * NP), which = e / NP % 2, n = e % NP;
+      if (t + k >= p.end) break;
+      float s = sums[from][0][e];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) s += sums[from][w][e];
+      const int64_t row = ((int64_t)p.b * a.T + t + k) * a.G + p.group;
+      if (a.workgroups > 1) a.shared[((int64_t)p.block * a.B * a.T * a.G + row) * 2 * NP + e % (2 * NP)] = s;
+      else if (n < a.N) static_cast<T*>(which ? a.d_c : a.d_b)[row * a.N + n] = (T)s;
+    }
+  };
   for (int j = chunks - 1; j >= 0; --j, turn ^= 1) {
     const int t = p.t0 + j * U;
-    get_steps(a, p, t, bias, next_x, next_dt, z, delta, u, x);
+    get_steps(a, p, t, bias, next_x, next_dt, slope, delta, u, x);
     get_errors(p, t, next_d, d_y);
     b.put(rows[turn][0], a), c.put(rows[turn][1], a);
     __syncthreads();
+    if (j < chunks - 1) put_sums(t + U, turn ^ 1);
     from_x.get(next_x, p, t - U), from_dt.get(next_dt, p, t - U), from_d.get(next_d, p, t - U);
     b.get(p, a, t - U), c.get(p, a, t - U);
     float before[U + 1][NL], decay[U][NL];  // before[k]: the state in front of token k
 #pragma unroll
     for (int i = 0; i < NL; i += 4) {
-      const f4 v = kept[j][i / 4][threadIdx.x];
+      const f4 v = kept[wave][j][i / 4][lane];
 #pragma unroll
       for (int l = 0; l < 4; ++l) before[0][i + l] = v[l];
     }
@@ -530,26 +552,29 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void se
 #pragma unroll
       for (int i = 0; i < Sums::LEFT; ++i) over_channels[K][i] = v[i];
     });
-    if (Sums::writes()) {
-      float* to = shared + t * (int64_t)shared_token;
+    if (Sums::writes())
 #pragma unroll
       for (int k = 0; k < U; ++k)
-        if (t + k < p.end)
 #pragma unroll
-          for (int i = 0; i < Sums::LEFT; ++i) to[shared_lane + k * shared_token + i] = over_channels[k][i];
-    }
+        for (int i = 0; i < Sums::LEFT; ++i) sums[turn][wave][k * 2 * NP + sum_at + i] = over_channels[k][i];
     Once<float, S> to_x, to_dt;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       const float d_delta = x.v[i] * sum_b.v[i] + sum_a.v[i] * 0.69314718055994530942f;
-      const float slope = a.softplus ? logistic(z.v[i]) : 1.0f;
-      to_x.v[i] = delta.v[i] * sum_b.v[i] + skip * d_y.v[i], to_dt.v[i] = d_delta * slope;
+      to_x.v[i] = delta.v[i] * sum_b.v[i] + skip * d_y.v[i], to_dt.v[i] = d_delta * slope.v[i];
       const bool there = (S <= U || p.s < U) && t + i * S + p.s < p.end;
       d_skip += there ? d_y.v[i] * x.v[i] : 0.0f, d_bias += there ? to_dt.v[i] : 0.0f;
     }
     put_tokens(static_cast<T*>(a.d_x), to_x, p, a, t, p.end);
     put_tokens(static_cast<T*>(a.d_dt), to_dt, p, a, t, p.end);
   }
+  __syncthreads();
+  if (chunks > 0) put_sums(p.t0, turn ^ 1);
+  if (a.workgroups == 1)  // (else the kernel that adds up the workgroups' sums clears what is past the sequence)
+    for (int64_t e = threadIdx.x; e < (int64_t)(p.t1 - p.end) * a.N; e += THREADS) {
+      const int64_t to = (((int64_t)p.b * a.T + p.end + e / a.N) * a.G + p.group) * a.N + e % a.N;
+      static_cast<T*>(a.d_b)[to] = (T)0.0f, static_cast<T*>(a.d_c)[to] = (T)0.0f;
+    }
   if (p.mine && p.s == 0) {
     for (int k = p.end; k < p.t1; ++k) {
       const int64_t to = ((int64_t)p.b * a.T + k) * a.D + p.channel;
@@ -570,6 +595,9 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void se
 // ---- launches, one source to an element type ---------------------------------------------------------------------------------
 enum Pass { TOKENS, ENDS, ENDS_AND_ERRORS, GRADIENT };
 
+// Of a workgroup of the backward pass, by the states that a channel's lanes hold: as many as LDS holds checkpoints and sums of two workgroups for.
+constexpr int waves_of(int states) { return states <= 16 ? 4 : states <= 32 ? 2 : 1; }
+
 struct Form {  // states to a lane, lanes to a channel
   int states, lanes;
 };
@@ -586,7 +614,8 @@ void launch_form(const Args& a, Pass pass, dim3 grid, hipStream_t st) {
   // or four where there are no more or more waves are wanted.
   if constexpr (NL == 4 || S == 16) {
     if (pass == ENDS_AND_ERRORS) return selective_tokens_kernel<T, NL, S, true, true><<<grid, 64, 0, st>>>(a);
-    if (pass == GRADIENT) return selective_gradient_kernel<T, NL, S><<<grid, 64, 0, st>>>(a);
+    constexpr int WAVES = waves_of(NL * S);
+    if (pass == GRADIENT) return selective_gradient_kernel<T, NL, S, WAVES><<<grid, 64 * WAVES, 0, st>>>(a);
   }
   if constexpr (NL == 8 || S < 8) {
     if (pass == ENDS) selective_tokens_kernel<T, NL, S, true, false><<<grid, 64, 0, st>>>(a);

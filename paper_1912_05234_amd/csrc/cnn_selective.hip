@@ -54,7 +54,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void selective_join_kernel(Args a, bo
   }
 }
 
-// ---- d_b and d_c: sums over the waves of a group's channels -------------------------------------------------------------------
+// ---- d_b and d_c: sums over the workgroups of a group's channels -------------------------------------------------------------------
 struct SharedArgs {
   const float* shared;  // [blocks][rows][2][NP]
   const int32_t* lengths;
@@ -63,7 +63,7 @@ struct SharedArgs {
   int G, N, NP, blocks;
 };
 
-// PARTS threads share a pack of four sums, each taking every PARTS-th wave's.
+// PARTS threads share a pack of four sums, each taking every PARTS-th workgroup's.
 template <class T, int PARTS>
 __global__ __launch_bounds__(256) void selective_shared_kernel(SharedArgs a) {
   __shared__ f4 sums[PARTS > 1 ? 256 : 1];
@@ -168,7 +168,7 @@ bool all_aligned(std::initializer_list<const void*> all) {
 
 struct Plan {
   Form form;
-  int blocks, segments;
+  int blocks, workgroups, segments;
   int64_t length;
   size_t ends, errors, sums, partial, shared, bytes;  // offsets in the workspace
 };
@@ -204,6 +204,8 @@ Plan plan_of(const cnn_selective_scan_shape& s, bool backward) {
       }
     }
   p.blocks = (int)blocks(p.form.lanes);
+  const int waves = waves_of(p.form.states * p.form.lanes);
+  p.workgroups = (p.blocks + waves - 1) / waves;
   const size_t states = rounded((size_t)p.segments * s.B * s.D * s.N * 4);
   p.ends = 0;
   if (p.segments > 1) {
@@ -212,7 +214,7 @@ Plan plan_of(const cnn_selective_scan_shape& s, bool backward) {
   }
   if (backward) {
     p.partial = p.bytes, p.shared = p.partial + rounded((size_t)p.segments * s.B * s.D * (s.N + 2) * 4);
-    p.bytes = p.shared + (size_t)p.blocks * s.B * s.T * s.G * 2 * p.form.states * p.form.lanes * 4;
+    p.bytes = p.shared + (p.workgroups > 1 ? (size_t)p.workgroups * s.B * s.T * s.G * 2 * p.form.states * p.form.lanes * 4 : 0);
   }
   return p;
 }
@@ -225,7 +227,7 @@ Args args_of(const cnn_selective_scan_shape& s, const Plan& p, void* workspace) 
   char* ws = static_cast<char*>(workspace);
   a.ends = reinterpret_cast<float*>(ws + p.ends), a.errors = reinterpret_cast<float*>(ws + p.errors), a.sums = reinterpret_cast<float*>(ws + p.sums);
   a.partial = reinterpret_cast<float*>(ws + p.partial), a.shared = reinterpret_cast<float*>(ws + p.shared);
-  a.T = s.T, a.length = (int)p.length, a.B = s.B, a.D = s.D, a.N = s.N, a.G = s.G, a.per = s.D / s.G, a.blocks = p.blocks, a.segments = p.segments;
+  a.T = s.T, a.length = (int)p.length, a.B = s.B, a.D = s.D, a.N = s.N, a.G = s.G, a.per = s.D / s.G, a.blocks = p.blocks, a.workgroups = p.workgroups, a.segments = p.segments;
   a.softplus = s.softplus != 0;
   return a;
 }
@@ -239,7 +241,7 @@ int run(const Args& a, const Plan& p, int type, bool backward, hipStream_t st) {
     selective_join_kernel<<<grid_of(((int64_t)a.B * a.D * a.N + JOIN_THREADS - 1) / JOIN_THREADS), JOIN_THREADS, 0, st>>>(a, backward);
     if (launch_status() != CNN_OK) return CNN_EHIP;
   }
-  launch(a, backward ? GRADIENT : TOKENS, p.form, grid, st);
+  launch(a, backward ? GRADIENT : TOKENS, p.form, backward ? grid_of((int64_t)p.workgroups * a.G * a.B * p.segments) : grid, st);
   return launch_status();
 }
 
@@ -286,16 +288,16 @@ int cnn_selective_scan_bwd(const cnn_selective_scan_shape* s, const cnn_tokens* 
   Args a = args_of(*s, p, workspace);
   a.x = tokens_of(x), a.dt = tokens_of(dt), a.b = tokens_of(b), a.c = tokens_of(c), a.d_y = tokens_of(d_y);
   a.a = a_, a.skip = skip, a.dt_bias = dt_bias, a.lengths = lengths, a.first = initial_state, a.d_last = d_final_state;
-  a.d_x = d_x, a.d_dt = d_dt, a.last = d_initial_state;
+  a.d_x = d_x, a.d_dt = d_dt, a.d_b = d_b, a.d_c = d_c, a.last = d_initial_state;
   hipStream_t st = (hipStream_t)hip_stream;
   const int rc = run(a, p, s->type, true, st);
   if (rc != CNN_OK) return rc;
-  const SharedArgs g{a.shared, lengths, d_b, d_c, (int64_t)s->B * s->T * s->G, s->T, s->G, s->N, p.form.states * p.form.lanes, p.blocks};
+  const SharedArgs g{a.shared, lengths, d_b, d_c, (int64_t)s->B * s->T * s->G, s->T, s->G, s->N, p.form.states * p.form.lanes, p.workgroups};
   const int64_t packs = g.rows * (2 * g.NP / 4);
-  const int status = with_type(s->type, [&](auto t) {
+  const int status = p.workgroups == 1 ? CNN_OK : with_type(s->type, [&](auto t) {
     using T = decltype(t);
-    // (Two tokens of 31 sequences of 2496 channels, 156 waves to a sum: 31 us by one thread, 7 by eight.)
-    if (p.blocks > 8) selective_shared_kernel<T, 8><<<grid_of((packs + 31) / 32), 256, 0, st>>>(g);
+    // (Two tokens of 31 sequences of 2496 channels, 39 workgroups to a sum.)
+    if (g.blocks > 8) selective_shared_kernel<T, 8><<<grid_of((packs + 31) / 32), 256, 0, st>>>(g);
     else selective_shared_kernel<T, 1><<<grid_of((packs + 255) / 256), 256, 0, st>>>(g);
     return launch_status();
   });
