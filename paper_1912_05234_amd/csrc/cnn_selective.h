@@ -422,7 +422,7 @@ struct ChannelSums {
 
 // WAVES waves to a workgroup, of neighbouring channels: they share the rows of B and C, and their sums over channels meet in LDS.
 template <class T, int NL, int S, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void selective_gradient_kernel(Args a) {
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NL == 4 && S > 2 ? 3 : 2))) void selective_gradient_kernel(Args a) {
   constexpr int NP = NL * S, EACH = Own<S>::EACH, THREADS = 64 * WAVES;
   using Sums = ChannelSums<S, 2 * NL>;
   __shared__ __align__(16) float rows[2][2][U * NP];

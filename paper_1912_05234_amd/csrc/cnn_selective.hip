@@ -13,44 +13,47 @@ constexpr float LOG2E = 1.44269504088896340736f;
 
 // ---- states between segments ---------------------------------------------------------------------------------------------
 // ends[j] holds what segment j leaves of a state of zero, errors[j] what reaches its first token's state from its own tokens; afterwards the state
-// that segment j starts from, and the error that it gets from the next.
+// that segment j starts from, and (backwards, by the second half of the grid) the error that it gets from the next.  A chain along the segments, whose loads are a batch
+// ahead of it.
 constexpr int JOIN_THREADS = 256, JOIN_AHEAD = 8;
-__global__ __launch_bounds__(JOIN_THREADS) void selective_join_kernel(Args a, bool errors) {
-  const int64_t states = (int64_t)a.D * a.N, i = workgroup() * JOIN_THREADS + threadIdx.x;
-  if (i >= a.B * states) return;
-  const int64_t b = i / states, dn = i % states, d = dn / a.N;
+template <bool ERRORS>
+__device__ __forceinline__ void join_segments(const Args& a, int64_t i) {
+  const int64_t states = (int64_t)a.D * a.N, b = i / states, dn = i % states;
   const float a2 = a.a[dn] * LOG2E;
-  const float* sums = a.sums + b * a.D + d;
   const int64_t each = a.B * states, every = (int64_t)a.B * a.D;
-  float run = a.first ? a.first[i] : 0.0f;
-  for (int j0 = 0; j0 < a.segments; j0 += JOIN_AHEAD) {
-    float own[JOIN_AHEAD], by[JOIN_AHEAD];
+  float* all = (ERRORS ? a.errors : a.ends) + i;
+  const float* sums = a.sums + b * a.D + dn / a.N;
+  const auto place = [&](int j) { return ERRORS ? a.segments - 1 - j : j; };
+  float own[JOIN_AHEAD], by[JOIN_AHEAD], next_own[JOIN_AHEAD], next_by[JOIN_AHEAD];
+  const auto get = [&](int j0) {
 #pragma unroll
     for (int k = 0; k < JOIN_AHEAD; ++k)
-      if (j0 + k < a.segments) own[k] = a.ends[(j0 + k) * each + i], by[k] = __builtin_amdgcn_exp2f(sums[(j0 + k) * every] * a2);
+      if (j0 + k < a.segments) next_own[k] = all[place(j0 + k) * each], next_by[k] = sums[place(j0 + k) * every];
+  };
+  const float* first = ERRORS ? a.d_last : a.first;
+  float run = first ? first[i] : 0.0f;
+  get(0);
+  for (int j0 = 0; j0 < a.segments; j0 += JOIN_AHEAD) {
+#pragma unroll
+    for (int k = 0; k < JOIN_AHEAD; ++k) own[k] = next_own[k], by[k] = next_by[k];
+    get(j0 + JOIN_AHEAD);
 #pragma unroll
     for (int k = 0; k < JOIN_AHEAD; ++k)
       if (j0 + k < a.segments) {
-        a.ends[(j0 + k) * each + i] = run;
-        run = run * by[k] + own[k];
+        all[place(j0 + k) * each] = run;
+        run = run * __builtin_amdgcn_exp2f(by[k] * a2) + own[k];
       }
   }
-  if (!errors) {
-    if (a.last) a.last[i] = run;
-    return;
-  }
-  run = a.d_last ? a.d_last[i] : 0.0f;
-  for (int j0 = a.segments - 1; j0 >= 0; j0 -= JOIN_AHEAD) {
-    float own[JOIN_AHEAD], by[JOIN_AHEAD];
-#pragma unroll
-    for (int k = 0; k < JOIN_AHEAD; ++k)
-      if (j0 - k >= 0) own[k] = a.errors[(j0 - k) * each + i], by[k] = __builtin_amdgcn_exp2f(sums[(j0 - k) * every] * a2);
-#pragma unroll
-    for (int k = 0; k < JOIN_AHEAD; ++k)
-      if (j0 - k >= 0) {
-        a.errors[(j0 - k) * each + i] = run;
-        run = run * by[k] + own[k];
-      }
+  if (!ERRORS && a.last) a.last[i] = run;
+}
+
+__global__ __launch_bounds__(JOIN_THREADS) void selective_join_kernel(Args a, bool backward) {
+  const int64_t all = a.B * ((int64_t)a.D * a.N), i = workgroup() * JOIN_THREADS + threadIdx.x, groups = (all + JOIN_THREADS - 1) / JOIN_THREADS;
+  if (backward) a.last = nullptr;  // (there the error of the first state)
+  if (i < groups * JOIN_THREADS) {
+    if (i < all) join_segments<false>(a, i);
+  } else if (backward) {
+    if (i - groups * JOIN_THREADS < all) join_segments<true>(a, i - groups * JOIN_THREADS);
   }
 }
 
@@ -175,10 +178,11 @@ struct Plan {
 
 size_t rounded(size_t b) { return (b + 255) & ~(size_t)255; }
 
-// About how long a pass takes, in a SIMD's cycles: waves share the 1024 SIMDs, and one alone leaves its SIMD waiting a third of the time.
-double pass_cost(int64_t waves, int64_t length, double cycles) {
+// About how long a pass takes, in a SIMD's cycles: `alone` a token for a wave that has a SIMD to itself, `shared` for each of several.  (Measured forward,
+// 4096 tokens by one wave to a SIMD: four states to a lane 315, eight 475; 2 x 4096 x 2048 x 16 states by eight waves to a SIMD: 190 and 360.)
+double pass_cost(int64_t waves, int64_t length, double alone, double shared) {
   const double load = (double)((waves + 1023) / 1024);
-  return (load > 1.0 ? load : 1.5) * (double)length * cycles;
+  return (double)length * (load * shared > alone ? load * shared : alone) + 3000.0;
 }
 
 Plan plan_of(const cnn_selective_scan_shape& s, bool backward) {
@@ -192,13 +196,15 @@ Plan plan_of(const cnn_selective_scan_shape& s, bool backward) {
       if (states * lanes < s.N || (lanes > 1 && states * lanes / 2 >= s.N)) continue;
       if (backward ? states == 8 && (lanes < 16 || s.N <= 64) : states == 8 ? lanes < 2 : lanes > 4) continue;
       const int64_t waves = (int64_t)s.B * s.G * blocks(lanes);
-      const double cycles = states * 38.0 + 50.0 + 100.0 / lanes;
-      for (int64_t length = 64; ; length *= 2) {
+      const double alone = 180.0 + 40.0 * states, shared = 20.0 + 38.0 * states;
+      for (int64_t length = 16; ; length *= 2) {
         if (backward && length > LONGEST) break;
         if (length > s.T) length = (s.T + U - 1) / U * U;
         const int64_t segments = (s.T + length - 1) / length;
-        double cost = pass_cost(waves * segments, length, backward ? 3.0 * cycles : cycles);
-        if (segments > 1) cost += pass_cost(waves * segments, length, cycles * 0.8) + 8000.0 + (double)s.B * s.D * s.N * segments * 0.006;
+        double cost = pass_cost(waves * segments, length, alone * (backward ? 2.9 : 1.0), shared * (backward ? 4.2 : 1.0));
+        if (segments > 1)  // the first pass, two more launches, the chain along the segments and its bytes
+          cost += pass_cost(waves * segments, length, alone * (backward ? 1.1 : 0.75), shared * (backward ? 1.4 : 0.75)) + 13000.0 +
+                  2500.0 * (double)((segments + 7) / 8) + (double)s.B * s.D * s.N * segments * (backward ? 0.012 : 0.006);
         if (best == 0.0 || cost < best) best = cost, p.form = {states, lanes}, p.length = length, p.segments = (int)segments;
         if (length >= s.T) break;
       }
@@ -238,7 +244,8 @@ int run(const Args& a, const Plan& p, int type, bool backward, hipStream_t st) {
   if (p.segments > 1) {
     launch(a, backward ? ENDS_AND_ERRORS : ENDS, p.form, grid, st);
     if (launch_status() != CNN_OK) return CNN_EHIP;
-    selective_join_kernel<<<grid_of(((int64_t)a.B * a.D * a.N + JOIN_THREADS - 1) / JOIN_THREADS), JOIN_THREADS, 0, st>>>(a, backward);
+    const int64_t groups = ((int64_t)a.B * a.D * a.N + JOIN_THREADS - 1) / JOIN_THREADS;
+    selective_join_kernel<<<grid_of(backward ? 2 * groups : groups), JOIN_THREADS, 0, st>>>(a, backward);
     if (launch_status() != CNN_OK) return CNN_EHIP;
   }
   launch(a, backward ? GRADIENT : TOKENS, p.form, backward ? grid_of((int64_t)p.workgroups * a.G * a.B * p.segments) : grid, st);
