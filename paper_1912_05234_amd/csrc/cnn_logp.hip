@@ -221,8 +221,8 @@ template <class T, int THREADS, int EACH, bool TOP>
 __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) __attribute__((amdgpu_waves_per_eu(EACH * sizeof(T) > 64 ? 4 : 8))) void logp_part_kernel(Args a) {
   constexpr int V = sizeof(T) == 2 ? 8 : 4, PACKS = EACH / V, LANES = THREADS < 64 ? THREADS : 64, WAVES = THREADS / LANES, ROWS = THREADS > 64 ? 1 : 256 / THREADS;
   __shared__ Sums sums[WAVES];
-  const int lane = threadIdx.x % THREADS;
-  const int64_t unit = workgroup() * ROWS + threadIdx.x / THREADS, n = unit / a.parts, begin = unit % a.parts * a.part_length;
+  const int lane = threadIdx.x % THREADS, beside = ROWS > 1 ? threadIdx.x / THREADS : 0;
+  const int64_t unit = workgroup() * ROWS + beside, n = unit / a.parts, begin = unit % a.parts * a.part_length;
   if (n >= a.rows) return;  // (all lanes of a row)
   const int64_t left = a.vocab - begin;
   const int length = (int)(left < a.part_length ? left : a.part_length);  // (every part has an element)
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) __attribute__((amdgp
 #pragma unroll 4
     for (int i = lane; i < length; i += THREADS) fn(key_of((float)part[i], begin + i));
   };
-  top_keys<THREADS>(shared[threadIdx.x / THREADS], a.top, likely, each, [&](int rank, uint64_t key) {
+  top_keys<THREADS>(shared[beside], a.top, likely, each, [&](int rank, uint64_t key) {
     if (a.parts > 1) a.keys[unit * a.top + rank] = key;
     else put_top(a, n, rank, key, r, log_sum);
   });
@@ -382,20 +382,25 @@ struct BackArgs {
   float scale;
 };
 
-// One tile of a row: THREADS lanes with PACKS packs each, all on their way at once.
+// One tile of a row: THREADS lanes with PACKS packs each, all on their way at once; of a wave's lanes or fewer, a workgroup has several rows (of
+// fewer, each given one token).
 template <class T, int THREADS, int PACKS, bool PAST_CACHES>
-__global__ __launch_bounds__(THREADS) void logp_backward_kernel(BackArgs a) {
-  constexpr int V = sizeof(T) == 2 ? 8 : 4, TILE = THREADS * PACKS * V;
-  __shared__ int64_t tokens[MOST_GIVEN];
-  __shared__ float errors[MOST_GIVEN];
-  const int64_t n = workgroup() / a.tiles;
-  const int begin = (int)(workgroup() % a.tiles) * TILE, left = (int)a.vocab - begin;
+__global__ __launch_bounds__(THREADS > 64 ? THREADS : 256) void logp_backward_kernel(BackArgs a) {
+  constexpr int V = sizeof(T) == 2 ? 8 : 4, TILE = THREADS * PACKS * V, ROWS = THREADS > 64 ? 1 : 256 / THREADS;
+  constexpr bool MANY = THREADS >= 64;
+  __shared__ int64_t all_tokens[MANY ? ROWS : 1][MANY ? MOST_GIVEN : 1];
+  __shared__ float all_errors[MANY ? ROWS : 1][MANY ? MOST_GIVEN : 1];
+  const int lane = threadIdx.x % THREADS, beside = ROWS > 1 ? threadIdx.x / THREADS : 0;
+  int64_t* tokens = all_tokens[MANY ? beside : 0];
+  float* errors = all_errors[MANY ? beside : 0];
+  const int64_t unit = workgroup() * ROWS + beside, n = unit / a.tiles;
+  const int begin = (int)(unit % a.tiles) * TILE, left = (int)a.vocab - begin;
   if (n >= a.rows) return;
   const T* logits = static_cast<const T*>(a.logits) + n * a.row;
   T* d_logits = static_cast<T*>(a.d_logits) + n * a.vocab;
   const bool whole = left >= TILE;  // the same in all lanes: no branch for each pack
   Loose<T, V> raw[PACKS];
-  const auto at = [&](int p) { return (p * THREADS + (int)threadIdx.x) * V; };
+  const auto at = [&](int p) { return (p * THREADS + lane) * V; };
   if (whole) {
 #pragma unroll
     for (int p = 0; p < PACKS; ++p) {
@@ -413,17 +418,17 @@ __global__ __launch_bounds__(THREADS) void logp_backward_kernel(BackArgs a) {
   float total = 0.0f;  // of the given tokens' errors; the same in every wave
   int64_t token = -1;  // the only one
   float error = 0.0f;
-  if (a.given == 1) {
+  if (!MANY || a.given == 1) {
     token = token_of(a.tokens, a.wide, n);
     if (token >= 0 && token < a.vocab && !none) total = error = a.d_log_probs[n];
     else token = -1;
   } else {
-    for (int j = threadIdx.x % 64; j < a.given; j += 64) {
+    for (int j = lane % 64; j < a.given; j += 64) {
       const int64_t t = token_of(a.tokens, a.wide, n * a.given + j);
       const bool known = t >= 0 && t < a.vocab && !none;
       const float g = known ? a.d_log_probs[n * a.given + j] : 0.0f;
       total += g;
-      if (threadIdx.x < 64) tokens[j] = known ? t : -1, errors[j] = g;
+      if (lane < 64) tokens[j] = known ? t : -1, errors[j] = g;
     }
     total = sum_over<64>(total);
   }
@@ -445,9 +450,11 @@ __global__ __launch_bounds__(THREADS) void logp_backward_kernel(BackArgs a) {
     else if constexpr (PAST_CACHES) put_loose_past_caches(d_logits + begin + at(p), x);
     else put_loose(d_logits + begin + at(p), x, V);
   }
-  if (a.given == 1) return;
-  __syncthreads();  // the rows' stores are done before a given token's element is written again
-  for (int j = threadIdx.x; j < a.given; j += THREADS) {
+  if (!MANY || a.given == 1) return;
+  // the row's stores are done before a given token's element is written again
+  if constexpr (ROWS > 1) __threadfence_block(), __builtin_amdgcn_wave_barrier();
+  else __syncthreads();
+  for (int j = lane; j < a.given; j += THREADS) {
     const int64_t t = tokens[j];
     if (t < begin || t >= begin + TILE) continue;
     bool before = false;
@@ -527,7 +534,8 @@ template <class T, int THREADS, int PACKS, bool PAST_CACHES>
 void launch_backward(BackArgs a, hipStream_t st) {
   constexpr int64_t TILE = THREADS * PACKS * (sizeof(T) == 2 ? 8 : 4);
   a.tiles = (int)((a.vocab + TILE - 1) / TILE);
-  logp_backward_kernel<T, THREADS, PACKS, PAST_CACHES><<<grid_of(a.rows * a.tiles), THREADS, 0, st>>>(a);
+  constexpr int ROWS = THREADS > 64 ? 1 : 256 / THREADS;
+  logp_backward_kernel<T, THREADS, PACKS, PAST_CACHES><<<grid_of((a.rows * a.tiles + ROWS - 1) / ROWS), THREADS * ROWS, 0, st>>>(a);
 }
 
 }  // namespace
@@ -575,7 +583,9 @@ int cnn_log_probs_bwd(const cnn_log_probs_shape* s, const cnn_rows* logits, cons
   return with_type(s->type, [&](auto t) {
     using T = decltype(t);
     constexpr int PACK = sizeof(T) == 2 ? 8 : 4;
-    if (s->vocab <= 64 * PACK) launch_backward<T, 64, 1, false>(a, st);
+    if (s->vocab <= 16 * PACK && s->given == 1) launch_backward<T, 16, 1, false>(a, st);
+    else if (s->vocab <= 32 * PACK && s->given == 1) launch_backward<T, 32, 1, false>(a, st);
+    else if (s->vocab <= 64 * PACK) launch_backward<T, 64, 1, false>(a, st);
     else if (s->vocab <= 256 * PACK) launch_backward<T, 256, 1, false>(a, st);
     else if (a.rows * a.vocab * (int64_t)sizeof(T) * 2 >= (int64_t)256 << 20) launch_backward<T, 256, 16 / PACK, true>(a, st);
     else launch_backward<T, 256, 16 / PACK, false>(a, st);

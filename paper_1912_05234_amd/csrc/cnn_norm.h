@@ -108,7 +108,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void norm_forward_kernel(Args a)
   using R = typename TY::S;
   constexpr int V = TY::PACK, TEAMS = threads_of(LANES) / LANES;
   __shared__ TeamSum<LANES, 1> shared;
-  const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
+  const int lane = threadIdx.x % LANES, team = TEAMS > 1 ? threadIdx.x / LANES : 0;
   const int64_t rb = workgroup() / a.group_blocks;
   const int group = (int)(workgroup() % a.group_blocks) * a.at_once + team % a.at_once, beside = team / a.at_once;
   if (rb >= a.row_blocks) return;                                       // (the whole workgroup)
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void norm_backward_kernel(Args a
   constexpr bool KEEPS = LANES < 1024;
   __shared__ TeamSum<LANES, 2> shared;
   __shared__ float sums[TEAMS > 1 ? TEAMS * LANES * PACKS * V : 1];
-  const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
+  const int lane = threadIdx.x % LANES, team = TEAMS > 1 ? threadIdx.x / LANES : 0;
   const int64_t rb = workgroup() / a.group_blocks;
   const int group0 = (int)(workgroup() % a.group_blocks) * a.at_once, group = group0 + team % a.at_once, beside = team / a.at_once;
   if (rb >= a.row_blocks) return;  // (the whole workgroup)

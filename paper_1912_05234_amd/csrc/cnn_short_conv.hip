@@ -161,7 +161,7 @@ __global__ __launch_bounds__(THREADS) void conv_tokens_kernel(Args a) {
 
 template <class T, int K, int V>
 __global__ __launch_bounds__(THREADS) void conv_tokens_backward_kernel(Args a) {
-  constexpr int AHEAD = 4;
+  constexpr int AHEAD = 8;
   __shared__ float sums[THREADS * V];
   const Part p = part_of<V>(a);
   float d_w[K][V], d_b[V];
@@ -357,8 +357,8 @@ struct Plan {
 };
 
 // Lanes along the channels: as many as leave at most an eighth of them idle, else the number that leaves fewest.  Chunks: as long as enough threads
-// remain, which each want a few tokens on their way (forward 262144, backward, where a chunk goes K - 1 tokens further and leaves a row of
-// partial sums, half of it).
+// remain, which each want a few tokens on their way: forward 262144; backward, where a chunk goes K - 1 tokens further and leaves a row of
+// partial sums, 65536 (4 x 4093 x 2048 bfloat16 69 us, with 131072 76, with 262144 79).
 Plan plan_of(const cnn_causal_conv_shape& s, int pack, bool backward) {
   Plan p{};
   const int64_t packs = (s.D + pack - 1) / pack;
@@ -367,7 +367,7 @@ Plan plan_of(const cnn_causal_conv_shape& s, int pack, bool backward) {
   for (int lanes = THREADS / 2; lanes >= 8 && taken(p.lanes) * 7 > packs * 8; lanes /= 2)
     if (taken(lanes) < taken(p.lanes)) p.lanes = lanes;
   p.channel_blocks = (int)((packs + p.lanes - 1) / p.lanes);
-  const int64_t want = backward ? 131072 : 262144, all = (int64_t)s.B * s.T * packs;
+  const int64_t want = backward ? 65536 : 262144, all = (int64_t)s.B * s.T * packs;
   p.chunk = backward ? 16 : 8;
   while (p.chunk < 128 && all / (p.chunk * 2) >= want) p.chunk *= 2;
   p.chunks = (s.T + p.chunk - 1) / p.chunk;
@@ -397,7 +397,9 @@ void with_taps(int taps, FN fn) {
   at(std::integral_constant<int, 6>{}), at(std::integral_constant<int, 7>{}), at(std::integral_constant<int, 8>{});
 }
 
-constexpr int BACK_PACK = 4;
+// Two channels to a lane and eight tokens ahead backward: 4 x 4093 x 2048 bfloat16 69 us, 4 x 4093 x 2048 floats 92, 2 x 645 x 112 13.4; four
+// channels and four tokens 68, 96 and 19, two and four 86, 89 and 13.3.
+constexpr int BACK_PACK = 2;
 int pack_of(int type) { return type == CNN_F32 ? 4 : 8; }
 
 }  // namespace

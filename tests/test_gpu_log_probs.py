@@ -16,7 +16,7 @@ DEV = "cuda:0"
 U = ref.U
 INF = float("inf")
 # rows, vocabulary, given, top: one token; a wave's limits; a workgroup's; rows cut into parts, few and many of them
-SHAPES = [(1, 1, 1, 1), (3, 7, 1, 7), (70, 256, 1, 5), (9, 511, 3, 64), (5, 513, 1, 20), (4, 2049, 64, 3), (6, 4100, 1, 33), (3, 8193, 2, 64), (2, 32003, 1, 20),
+SHAPES = [(1, 1, 1, 1), (3, 7, 1, 7), (37, 60, 1, 33), (11, 128, 2, 40), (21, 129, 1, 50), (70, 256, 1, 5), (9, 511, 3, 64), (5, 513, 1, 20), (4, 2049, 64, 3), (6, 4100, 1, 33), (3, 8193, 2, 64), (2, 32003, 1, 20),
           (3, 32769, 1, 64), (2, 50021, 5, 20), (1, 200003, 256, 40), (300, 40007, 1, 0), (2, 65536, 1, 64), (3, 65537, 2, 7), (2, 131101, 1, 64), (300, 33000, 3, 5)]
 
 
