@@ -478,6 +478,10 @@ bool rows_ok(const cnn_rows* r, int type) {
   return r && r->data && reinterpret_cast<uintptr_t>(r->data) % type_bytes(type) == 0 && r->row >= 0;
 }
 
+// The small inputs are read one by one and need only be aligned to their element: slices of a batch serve.
+bool element_aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+size_t token_bytes(const cnn_log_probs_shape* s) { return s->wide_tokens ? 8 : 4; }
+
 struct Plan {
   int threads, each, parts;
   int64_t part_length;
@@ -551,7 +555,8 @@ int cnn_log_probs_fwd(const cnn_log_probs_shape* s, const cnn_rows* logits, cons
   using namespace cnn;
   using namespace cnn::logp;
   if (!shape_ok(s) || !rows_ok(logits, s->type) || !tokens || !log_probs || (s->top && (!top_log_probs || !top_tokens))) return CNN_EINVAL;
-  for (const void* p : {(const void*)tokens, (const void*)log_probs, (const void*)entropy, (const void*)stats, (const void*)top_log_probs,
+  if (!element_aligned(tokens, token_bytes(s))) return CNN_EINVAL;
+  for (const void* p : {(const void*)log_probs, (const void*)entropy, (const void*)stats, (const void*)top_log_probs,
                         (const void*)top_tokens, (const void*)workspace})
     if (!aligned16(p)) return CNN_EINVAL;
   const Plan p = plan_of(*s);
@@ -576,8 +581,8 @@ int cnn_log_probs_bwd(const cnn_log_probs_shape* s, const cnn_rows* logits, cons
   using namespace cnn;
   using namespace cnn::logp;
   if (!shape_ok(s) || !rows_ok(logits, s->type) || !tokens || !stats || !d_log_probs || !d_logits) return CNN_EINVAL;
-  for (const void* p : {(const void*)tokens, (const void*)stats, (const void*)d_log_probs, (const void*)d_entropy, (const void*)d_logits})
-    if (!aligned16(p)) return CNN_EINVAL;
+  if (!element_aligned(tokens, token_bytes(s)) || !element_aligned(stats, 4) || !element_aligned(d_log_probs, 4) || !element_aligned(d_entropy, 4)) return CNN_EINVAL;
+  if (!aligned16(d_logits)) return CNN_EINVAL;
   const BackArgs a{logits->data, logits->row, s->rows, s->vocab, tokens, stats, d_log_probs, d_entropy, d_logits, 1, s->given, s->wide_tokens != 0, s->scale};
   hipStream_t st = (hipStream_t)hip_stream;
   return with_type(s->type, [&](auto t) {

@@ -265,6 +265,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(S == 1 ? 2 :
   constexpr int NP = NL * S;
   __shared__ __align__(16) float rows[2][2][U * NP];
   const Place p = place_of<NL, S, 1>(a, a.blocks);
+  if (p.segment >= a.segments) return;  // (a grid of two dimensions may have more workgroups than are wanted)
   float a2[NL], h[NL], q[ERRORS ? NL : 1], run[ERRORS ? NL : 1];
   get_decays(a2, a, p);
   const int64_t states = (int64_t)a.D * a.N;
@@ -430,6 +431,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NL =
   __shared__ float sums[2][WAVES][U * 2 * NP];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const Place p = place_of<NL, S, WAVES>(a, a.workgroups);
+  if (p.segment >= a.segments) return;  // (the whole workgroup, as above)
   float a2[NL], h[NL], q[NL], d_a[NL], d_skip = 0.0f, d_bias = 0.0f;
   get_decays(a2, a, p);
   const int64_t states = (int64_t)a.D * a.N, at = (int64_t)p.segment * a.B + p.b;

@@ -164,6 +164,7 @@ __global__ __launch_bounds__(THREADS) void conv_tokens_backward_kernel(Args a) {
   constexpr int AHEAD = 8;
   __shared__ float sums[THREADS * V];
   const Part p = part_of<V>(a);
+  if (workgroup() / a.channel_blocks * (THREADS / a.lanes) >= a.rows) return;  // (the whole workgroup: a grid of two dimensions may have more than are wanted)
   float d_w[K][V], d_b[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {

@@ -160,8 +160,10 @@ def test_log_probs_refusals():
     for r in BAD_ROWS:
         assert fwd(x=r) == bwd(x=r) == EINVAL
     for p in (nul, odd):
-        assert fwd(t=p) == fwd(lp=p) == fwd(tl=p) == fwd(tt=p) == bwd(t=p) == bwd(st=p) == bwd(d=p) == bwd(o=p) == EINVAL
-    assert fwd(h=odd) == fwd(st=odd) == fwd(ws=odd) == bwd(dh=odd) == EINVAL
+        assert fwd(t=p) == fwd(lp=p) == fwd(tl=p) == fwd(tt=p) == bwd(t=p) == bwd(o=p) == EINVAL  # (tokens of eight bytes)
+    half = ctypes.c_void_p(0x1002)
+    assert bwd(st=nul) == bwd(d=nul) == bwd(st=half) == bwd(d=half) == bwd(dh=half) == fwd(s=logp(wide=0), t=half) == EINVAL
+    assert fwd(h=odd) == fwd(st=odd) == fwd(ws=odd) == EINVAL
     long = logp(vocab=100000)
     need = L.cnn_log_probs_fwd_workspace_bytes(long)
     assert need and fwd(s=long, n=need - 1) == fwd(s=long, ws=nul) == EWS
