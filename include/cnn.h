@@ -421,7 +421,7 @@ int cnn_causal_conv_step(const cnn_causal_conv_shape* shape, const cnn_tokens* x
  * d_y) as cnn_tokens of `type`; b and c [B,T,G,N] as cnn_heads, tokens at most 2^26 elements apart; D a multiple of G, D / G
  * consecutive channels to a group.  Results y, d_x, d_dt [B,T,D] and
  * d_b, d_c [B,T,G,N] are contiguous; states [B,D,N] are fp32, an initial or final one may be NULL (zero; not wanted), and they may be the same memory.  lengths
- * as for cnn_causal_conv_fwd.  1 <= N <= 128, B * D <= 2^24, B * T < 2^31, D <= 2^20.  Inputs up to a sequence's length must be finite: one that is not
+ * as for cnn_causal_conv_fwd.  1 <= N <= 128, B * D <= 2^24, B * T < 2^31 - 64, D <= 2^20.  Inputs up to a sequence's length must be finite: one that is not
  * makes results NaN that the formulas leave finite, also of tokens before it, of its own channel and, backward, its group's d_b and d_c.  Everything is
  * computed in fp32 and rounded once; a decay below 2^-126 counts as 0.  `workspace` holds states of pieces of the sequences, and backward partial sums; its size query returns 0 where none is
  * needed and for refused shapes. */

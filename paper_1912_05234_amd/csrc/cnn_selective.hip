@@ -115,45 +115,58 @@ struct OneArgs {
   int B, D, N, per, lanes, softplus;
 };
 
-// Four states to a lane, so many lanes to a channel; neighbouring lanes' states are neighbours in memory, which bounds it.
+// Four states to a lane, so many lanes to a channel; neighbouring lanes' states are neighbours in memory, which bounds it.  A lane takes AHEAD
+// channels, whose loads are on their way together.
 constexpr int ONE_THREADS = 256;
-template <class T>
+template <class T, int AHEAD>
 __global__ __launch_bounds__(ONE_THREADS) void selective_one_token_kernel(OneArgs a) {
-  const int lane = (int)threadIdx.x % a.lanes, n = lane * 4, channels = ONE_THREADS / a.lanes;
-  const int64_t b = workgroup() / ((a.D + channels - 1) / channels);
-  const int channel = (int)(workgroup() % ((a.D + channels - 1) / channels)) * channels + (int)threadIdx.x / a.lanes;
-  if (b >= a.B || channel >= a.D) return;  // (a channel's lanes together)
-  T* y = static_cast<T*>(a.y) + b * a.D + channel;
+  const int lane = (int)threadIdx.x % a.lanes, n = lane * 4, channels = ONE_THREADS / a.lanes, blocks = (a.D + AHEAD * channels - 1) / (AHEAD * channels);
+  const int64_t b = workgroup() / blocks;
+  const int first = (int)(workgroup() % blocks) * AHEAD * channels + (int)threadIdx.x / a.lanes, count = a.N - n;
+  if (b >= a.B) return;
   const int64_t slot = a.slots ? a.slots[b] : b;
-  if (slot < 0 || slot >= a.pool) {  // no sequence here
-    if (lane == 0) *y = (T)0.0f;
-    return;
-  }
-  const int group = channel / a.per, count = a.N - n;
-  float* state = a.state + (slot * a.D + channel) * a.N + n;
-  float h[4], a4[4], B[4], C[4];
-  get_loose(h, state, count);
-  get_loose(a4, a.a + (int64_t)channel * a.N + n, count);
-  get_loose(B, static_cast<const T*>(a.b.data) + b * a.b.batch + group * a.b.group + n, count);
-  get_loose(C, static_cast<const T*>(a.c.data) + b * a.c.batch + group * a.c.group + n, count);
-  const float x = (float)static_cast<const T*>(a.x.data)[b * a.x.batch + channel];
-  const float z = (float)static_cast<const T*>(a.dt.data)[b * a.dt.batch + channel] + (a.dt_bias ? a.dt_bias[channel] : 0.0f);
-  const float delta = a.softplus ? softplus_of(z) : z, u = delta * x;
-  float sum = 0.0f;
+  const bool there = slot >= 0 && slot < a.pool;  // (else no sequence here)
+  Loose<float, 4> h[AHEAD], decays[AHEAD];
+  Loose<T, 4> B[AHEAD], C[AHEAD];
+  T x[AHEAD], dt[AHEAD];
+  float bias[AHEAD], skip[AHEAD];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    h[j] = __builtin_amdgcn_exp2f(delta * (a4[j] * LOG2E)) * h[j] + u * B[j];
-    sum += C[j] * h[j];
+  for (int k = 0; k < AHEAD; ++k) {
+    const int channel = first + k * channels;
+    if (!there || channel >= a.D) continue;  // (a channel's lanes together)
+    const int group = channel / a.per;
+    h[k] = got_loose<4>(a.state + (slot * a.D + channel) * a.N + n, count);
+    decays[k] = got_loose<4>(a.a + (int64_t)channel * a.N + n, count);
+    B[k] = got_loose<4>(static_cast<const T*>(a.b.data) + b * a.b.batch + group * a.b.group + n, count);
+    C[k] = got_loose<4>(static_cast<const T*>(a.c.data) + b * a.c.batch + group * a.c.group + n, count);
+    x[k] = static_cast<const T*>(a.x.data)[b * a.x.batch + channel], dt[k] = static_cast<const T*>(a.dt.data)[b * a.dt.batch + channel];
+    bias[k] = a.dt_bias ? a.dt_bias[channel] : 0.0f, skip[k] = a.skip ? a.skip[channel] : 0.0f;
   }
-  put_loose(state, h, count);
-  for (int d = 1; d < a.lanes; d *= 2) sum += __shfl_xor(sum, d);
-  if (lane == 0) *y = (T)(sum + (a.skip ? a.skip[channel] * x : 0.0f));
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) {
+    const int channel = first + k * channels;
+    if (channel >= a.D) return;
+    float sum = 0.0f;
+    if (there) {
+      const float z = (float)dt[k] + bias[k], delta = a.softplus ? softplus_of(z) : z, u = delta * (float)x[k];
+      float state[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        state[j] = __builtin_amdgcn_exp2f(delta * (decays[k].v[j] * LOG2E)) * h[k].v[j] + u * (float)B[k].v[j];
+        sum += (float)C[k].v[j] * state[j];
+      }
+      put_loose(a.state + (slot * a.D + channel) * a.N + n, state, count);
+      for (int d = 1; d < a.lanes; d *= 2) sum += __shfl_xor(sum, d);
+      sum += skip[k] * (float)x[k];
+    }
+    if (lane == 0) static_cast<T*>(a.y)[b * a.D + channel] = (T)sum;
+  }
 }
 
 // ---- plans -----------------------------------------------------------------------------------------------------------------
 bool shape_ok(const cnn_selective_scan_shape* s) {
   return s && s->B >= 1 && s->T >= 1 && s->D >= 1 && s->D <= MOST_CHANNELS && s->N >= 1 && s->N <= MOST_STATES && s->G >= 1 && s->D % s->G == 0 &&
-         type_known(s->type) && (int64_t)s->B * s->D <= 1 << 24 && (int64_t)s->B * s->T < (int64_t)1 << 31;
+         type_known(s->type) && (int64_t)s->B * s->D <= 1 << 24 && (int64_t)s->B * s->T <= INT32_MAX - 64;
 }
 
 bool tokens_ok(const cnn_tokens* t, int type) {
@@ -323,8 +336,11 @@ int cnn_selective_scan_step(const cnn_selective_scan_shape* s, const cnn_tokens*
   while (lanes * 4 < s->N) lanes *= 2;
   const OneArgs a{tokens_of(x), tokens_of(dt), tokens_of(b), tokens_of(c), a_, skip, dt_bias, state, slots, y, pool, s->B, s->D, s->N, s->D / s->G, lanes, s->softplus != 0};
   const int channels = ONE_THREADS / lanes;
+  const auto grid = [&](int ahead) { return grid_of((int64_t)s->B * ((s->D + ahead * channels - 1) / (ahead * channels))); };
   return with_type(s->type, [&](auto t) {
-    selective_one_token_kernel<decltype(t)><<<grid_of((int64_t)s->B * ((s->D + channels - 1) / channels)), ONE_THREADS, 0, (hipStream_t)hip_stream>>>(a);
+    using T = decltype(t);
+    if ((int64_t)s->B * s->D / channels < 2048) selective_one_token_kernel<T, 1><<<grid(1), ONE_THREADS, 0, (hipStream_t)hip_stream>>>(a);
+    else selective_one_token_kernel<T, 2><<<grid(2), ONE_THREADS, 0, (hipStream_t)hip_stream>>>(a);
     return launch_status();
   });
 }

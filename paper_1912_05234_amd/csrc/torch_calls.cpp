@@ -720,7 +720,7 @@ const at::Tensor& tokens_tensor(PyObject* o, int dims, cnn_tokens* tokens) {
   for (int i = 0; i < dims; ++i)
     if (t.size(i) > INT_MAX) raise(PyExc_ValueError, "a dimension is too large");
   if (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1) raise(PyExc_ValueError, "expected a last dimension without gaps");
-  *tokens = {t.data_ptr(), t.stride(0), dims == 3 ? t.stride(1) : 0};
+  *tokens = {t.data_ptr(), t.stride(0), dims == 3 && t.size(1) > 1 ? t.stride(1) : 0};  // (a single token's stride may be anything)
   return t;
 }
 
@@ -843,7 +843,12 @@ Scan scan_of(PyObject* const* a, int dims) {  // x, dt, a, b, c, skip or None, d
   if (w.sizes() != at::IntArrayRef({D, N})) raise(PyExc_ValueError, "expected a of as many rows as channels and as many columns as b and c");
   const float* skip = static_cast<const float*>(optional_on(a[5], {D}, at::kFloat, device, "a skip"));
   const float* bias = static_cast<const float*>(optional_on(a[6], {D}, at::kFloat, device, "a bias"));
-  return {{(int)B, (int)T, (int)D, (int)N, (int)G, code, integer(a[7]) != 0}, x, dt, heads_of(b), heads_of(c), data(w), skip, bias, t, device, type, B, T, D, N, G};
+  const auto bc = [&](const at::Tensor& h) {
+    cnn_heads v = heads_of(h);
+    if (T == 1) v.token = 0;
+    return v;
+  };
+  return {{(int)B, (int)T, (int)D, (int)N, (int)G, code, integer(a[7]) != 0}, x, dt, bc(b), bc(c), data(w), skip, bias, t, device, type, B, T, D, N, G};
 }
 
 CALL(selective_scan_fwd, 11)  // as scan_of, lengths or None, initial state or None, want_state

@@ -132,6 +132,16 @@ def test_state_may_be_updated_in_place():
         assert torch.equal(y, want[0]) and torch.equal(state, want[1])
 
 
+def test_a_single_token_of_any_stride():
+    """Tokens cut out of something long: their stride is never used, however large."""
+    x, a, b = torch.ones(2, 1, 8, device=DEV), -torch.ones(8, 4, device=DEV), torch.ones(2, 1, 2, 4, device=DEV)
+    far = lambda t: t.as_strided(t.shape, (t.stride(0), 1 << 40, *t.stride()[2:]))  # noqa: E731
+    want, got = binding.selective_scan_fwd(x, x, a, b, b, want_state=True), binding.selective_scan_fwd(far(x), far(x), a, far(b), far(b), want_state=True)
+    assert all(torch.equal(v, w) for v, w in zip(want, got))
+    w = torch.ones(8, 4, device=DEV)
+    assert torch.equal(binding.causal_conv_fwd(far(x), w)[0], binding.causal_conv_fwd(x, w)[0])
+
+
 def test_extreme_steps():
     """Steps of thousands (the state is forgotten), of next to nothing, a of zero, far negative dt: no NaN, and softplus keeps its small values."""
     D, N = 6, 16
