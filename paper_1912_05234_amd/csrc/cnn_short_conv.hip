@@ -303,7 +303,8 @@ struct OneArgs {
   int silu;
 };
 
-// A thread moves a pack of a row's state on by one input.
+// A thread moves a pack of a row's state on by one input.  Latency bounds it: the slot, then the state; the weights come meanwhile.
+constexpr int ONE_PACK = 4;
 template <class T, int K, int V>
 __global__ __launch_bounds__(THREADS) void conv_one_token_kernel(OneArgs a) {
   const int64_t i = workgroup() * THREADS + threadIdx.x;
@@ -311,22 +312,28 @@ __global__ __launch_bounds__(THREADS) void conv_one_token_kernel(OneArgs a) {
   const int64_t b = i / a.packs, c = i % a.packs * V, left = a.D - c;
   const int count = left < V ? (int)left : V;
   const int64_t slot = a.slots ? a.slots[b] : b;
+  const Loose<float, K * V> w = got_loose<K * V>(a.weight + c * K, count * K);
+  const Loose<T, V> x = got_loose<V>(static_cast<const T*>(a.x) + b * a.batch + c, count);
+  Loose<float, V> bias{};
+  if (a.bias) bias = got_loose<V>(a.bias + c, count);
   T* y = static_cast<T*>(a.y) + b * a.D + c;
   float out[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) out[j] = 0.0f;
   if (slot >= 0 && slot < a.pool) {
     T* state = static_cast<T*>(a.state) + slot * (K - 1) * a.D + c;
+    Loose<T, V> raw[K];
+#pragma unroll
+    for (int k = 0; k < K - 1; ++k) raw[k] = got_loose<V>(state + k * a.D, count);
+    raw[K - 1] = x;
     float seen[K][V];
 #pragma unroll
-    for (int k = 0; k < K - 1; ++k) get_loose(seen[k], state + k * a.D, count);
-    get_loose(seen[K - 1], static_cast<const T*>(a.x) + b * a.batch + c, count);
+    for (int k = 0; k < K; ++k) widen(seen[k], raw[k]);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      if (j >= count) continue;
-      float s = a.bias ? a.bias[c + j] : 0.0f;
+      float s = bias.v[j];
 #pragma unroll
-      for (int k = 0; k < K; ++k) s += a.weight[(c + j) * K + k] * seen[k][j];
+      for (int k = 0; k < K; ++k) s += w.v[j * K + k] * seen[k][j];
       out[j] = a.silu ? s * logistic(s) : s;
     }
 #pragma unroll
@@ -459,13 +466,12 @@ int cnn_causal_conv_step(const cnn_causal_conv_shape* s, const cnn_tokens* x, co
   using namespace cnn::short_conv;
   if (!shape_ok(s) || s->T != 1 || !tokens_ok(x, s->type) || !weight || !state || !y || !all_aligned({weight, bias, state, slots, y})) return CNN_EINVAL;
   if (pool < 1 || pool > 1 << 30 || (!slots && pool < s->B)) return CNN_EINVAL;
-  const int pack = pack_of(s->type);
-  const int64_t packs = (s->D + pack - 1) / pack, total = packs * s->B;
+  const int64_t packs = (s->D + ONE_PACK - 1) / ONE_PACK, total = packs * s->B;
   const OneArgs a{x->data, x->batch, pool, total, packs, s->D, weight, bias, state, y, slots, s->silu != 0};
   return with_type(s->type, [&](auto t) {
     using T = decltype(t);
     with_taps(s->K, [&](auto k) {
-      conv_one_token_kernel<T, decltype(k)::value, sizeof(T) == 4 ? 4 : 8><<<grid_of((total + THREADS - 1) / THREADS), THREADS, 0, (hipStream_t)hip_stream>>>(a);
+      conv_one_token_kernel<T, decltype(k)::value, ONE_PACK><<<grid_of((total + THREADS - 1) / THREADS), THREADS, 0, (hipStream_t)hip_stream>>>(a);
     });
     return launch_status();
   });
