@@ -12,6 +12,10 @@
 // for k = 20 of 64 groups); those go into a list in LDS, and each finds its place by counting the larger ones.  Keys are unique,
 // the value's bits in order above the complement of the index, so equal values keep the order of their tokens.  Where the list
 // overflows (rows of equal logits) the workgroup takes the largest key k times instead.
+//
+// Measured: 8191 rows of 32003 bfloat16 150 us forward (524 MB; the vector unit's share, an exponential and some six operations an element, is
+// 60 of them), 187 with five top tokens, 181 backward (1.05 GB, 5.8 TB/s, past the caches); 64 rows of 50021 with twenty top tokens 14.7: one workgroup to a
+// row, a chain of loads, sums and barriers; 78400 rows of 256 19 and 21.
 #include "cnn_common.h"
 #include "cnn_lanes.h"
 #include "cnn_types.h"
@@ -592,6 +596,8 @@ int cnn_log_probs_bwd(const cnn_log_probs_shape* s, const cnn_rows* logits, cons
     else if (s->vocab <= 32 * PACK && s->given == 1) launch_backward<T, 32, 1, false>(a, st);
     else if (s->vocab <= 64 * PACK) launch_backward<T, 64, 1, false>(a, st);
     else if (s->vocab <= 256 * PACK) launch_backward<T, 256, 1, false>(a, st);
+    // What does not fit the last cache (256 MiB) goes past it: 8191 x 32003 bfloat16 258 -> 181 us, 4096 x 32003 floats 208 -> 170.  Smaller results may be
+    // read from it by what comes next (1000 x 32003, 128 MB, would take 25 in place of 28 us here).
     else if (a.rows * a.vocab * (int64_t)sizeof(T) * 2 >= (int64_t)256 << 20) launch_backward<T, 256, 16 / PACK, true>(a, st);
     else launch_backward<T, 256, 16 / PACK, false>(a, st);
     return launch_status();

