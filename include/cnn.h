@@ -370,7 +370,7 @@ int cnn_norm_gate_bwd(const cnn_norm_shape* shape, const cnn_rows* d_y, const cn
  *   entropy[rows]           - sum p ln p (nullable)
  *   top_tokens, top_log_probs[rows,top]   the `top` largest logits in descending order, equal ones (0 and -0 among them) in the order of their tokens
  *   stats[rows,3]           what the backward call needs: max l, ln sum exp(scale * (l - max)), the entropy (nullable)
- * Results are fp32.  A logit of -inf is an impossible token: p = 0.  A row of nothing else has log_probs and top_log_probs of -inf and an entropy of 0,
+ * Results are fp32; the sum is one of fp32 numbers, so a log probability or entropy next to 0 is exact to some 2^-22, not relative to itself.  A logit of -inf is an impossible token: p = 0.  A row of nothing else has log_probs and top_log_probs of -inf and an entropy of 0,
  * and its gradient is zero.  A NaN or +inf makes its row's results NaN, except that top_tokens are tokens of the row and padding's log_probs are 0.
  * 1 <= rows < 2^31, 1 <= vocab <= 2^24, 1 <= given <= 256, 0 <= top <= min(64, vocab).  Logits as a cnn_rows of `type`;
  * tokens, stats and the errors need only be aligned to their element. */

@@ -49,9 +49,13 @@ __device__ __forceinline__ T over_lanes(T v, OP op) {
   if constexpr (LANES > 32) v = across_rows<true>(v, op);
   return v;
 }
+// (A product that is summed is rounded first: fused into the addition, each lane would have its own unrounded and the others' rounded.)
 template <int LANES>
 __device__ __forceinline__ float sum_over(float v) {
-  return over_lanes<LANES>(v, [](float a, float b) { return a + b; });
+  return over_lanes<LANES>(v, [](float a, float b) {
+#pragma clang fp contract(off)
+    return a + b;
+  });
 }
 template <int LANES>
 __device__ __forceinline__ float max_over(float v) {

@@ -238,6 +238,9 @@ __global__ __launch_bounds__(threads_of(LANES)) void norm_backward_kernel(Args a
     }
     shared.sum(sum, turn);
     const float rstd = inverse_root(sum[0] * a.by_width + a.eps), mean = sum[1] * a.by_width * rstd;
+    // A group of one element is 1 or -1 but for eps: d - n (d n) = d (1 - n^2) = d eps rstd^2, of which the difference would leave nothing.
+    const bool alone = a.width == 1;
+    const float left = a.eps * rstd * rstd;
     const int64_t to = n * a.groups * a.width + first;
 #pragma unroll
     for (int p = 0; p < PACKS; ++p) {
@@ -252,7 +255,8 @@ __global__ __launch_bounds__(threads_of(LANES)) void norm_backward_kernel(Args a
       for (int j = 0; j < V; ++j) {
         const float hat = v[p][j] * rstd, error = d[p][j], by = factor(p, j);
         dw[p][j] += error * hat * by;
-        v[p][j] = rstd * (error * w[p][j] * by - hat * mean);
+        const float d_n = error * w[p][j] * by;
+        v[p][j] = rstd * (alone ? d_n * left : d_n - hat * mean);
         if (MODE == ADD && a.d_r.data) v[p][j] += z[p][j];
         if (MODE == GATE && a.gate.data) {
           const float s = sigmoid[p][j];

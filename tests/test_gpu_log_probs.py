@@ -172,6 +172,18 @@ def test_far_logits_keep_their_differences():
     assert (sharp[0] == 0.0).all() and (sharp[1] == 0.0).all()
 
 
+@pytest.mark.parametrize("V", [100, 250, 2584, 40000, 70001])
+@pytest.mark.parametrize("type_", list(seq.TYPES))
+def test_repeated_calls_give_the_same_bits(V, type_):
+    """Whichever lane finds a top token, and whichever writes a given one's result: the same token given and found has one log probability."""
+    logits = (torch.randn(700, V, generator=torch.Generator().manual_seed(V)) * 2.5).to(seq.TYPES[type_]).to(DEV)
+    tokens = torch.zeros(700, 5, dtype=torch.int32, device=DEV)
+    first = binding.log_probs_fwd(logits, tokens, 0.8, 5)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(binding.log_probs_fwd(logits, tokens, 0.8, 5), first))
+    assert torch.equal(binding.log_probs_fwd(logits, first[4], 0.8)[0], first[3])
+
+
 def test_captured_calls_replay():
     gen = torch.Generator().manual_seed(9)
     logits, tokens = torch.randn(5, 70001, generator=gen).to(DEV), torch.randint(0, 70001, (5, 3), generator=gen).to(DEV)

@@ -115,6 +115,22 @@ def test_slices_and_leading_dimensions(types):
     assert torch.equal(binding.add_norm_fwd(row, w)[0], binding.add_norm_fwd(row[None], w)[0][0])
 
 
+@pytest.mark.parametrize("types", TYPES, ids=str)
+def test_gradients_of_groups_of_one_element(types):
+    """d (1 - n^2) with n next to 1 or -1: what eps leaves is exact to (3 rstd, 12 products and roundings) 60 u of itself, and the type's rounding."""
+    type_, stream = (seq.TYPES[t] for t in types)
+    gen = torch.Generator().manual_seed(6)
+    r, w, d = normal(gen, 9, 20, dtype=stream, by=4.0), normal(gen, 20, dtype=torch.float32), normal(gen, 9, 20, dtype=type_, by=1000.0)
+    r64, w64, d64 = wide(r, w, d)
+    eps = scale_of(1e-3)
+    want = d64 * w64 * eps / (r64 * r64 + eps) ** 1.5
+    near(binding.add_norm_bwd(d, r, w, eps=1e-3, groups=20)[1], want, 60 * U * want.abs(), "d_residual")
+    x, gate = r.to(type_), normal(gen, 9, 20, dtype=type_)
+    x64, z64 = wide(x, gate)
+    want = d64 * w64 * ref.silu(z64) * eps / (x64 * x64 + eps) ** 1.5
+    near(binding.norm_gate_bwd(d, x, w, gate, eps=1e-3, groups=20)[0], want, (70 + 2 * z64.abs()) * U * want.abs(), "d_x")
+
+
 def test_a_bad_element_stays_in_its_group():
     x, w = torch.ones(6, 96, device=DEV), torch.ones(96, device=DEV)
     x[2, 40], x[4, 90] = float("nan"), float("inf")
