@@ -73,14 +73,13 @@ __device__ __forceinline__ float from_lane(float v) {
   else return __shfl(v, (int)(threadIdx.x & ~(S - 1)) + K);
 }
 
-// softplus(z) = ln(1 + e^z), and its slope e^z / (1 + e^z).  ln(1 + e) for small e by Kahan's formula e ln(w) / (w - 1) with w = 1 + e rounded (Goldberg,
-// "What every computer scientist should know about floating-point arithmetic", theorem 4).
+// softplus(z) = ln(1 + e^z) = max(z, 0) + ln(1 + e) with e = exp(-|z|), and its slope 1 / (1 + e^-z).  With w = 1 + e rounded, ln(1 + e) = ln w + (1 + e - w) / w up to
+// the square of the last term; what the rounding left out, 1 + e - w, is exact in two subtractions and at most 2^-24, so that its division by
+// w (1 to 2, and 1 where e is small) is left out.
 __device__ __forceinline__ float softplus_of(float z, float& slope) {
-  const float e = __builtin_amdgcn_exp2f(z * -NEG_LOG2E), w = 1.0f + e;
-  const float l = __builtin_amdgcn_logf(w) * 0.69314718055994530942f;
-  const float r = w == 1.0f ? e : e * l * __builtin_amdgcn_rcpf(w - 1.0f);
-  slope = z > 20.0f ? 1.0f : e * __builtin_amdgcn_rcpf(w);
-  return z > 20.0f ? z : r;  // (z + e^-z: the same float)
+  const float e = __builtin_amdgcn_exp2f(__builtin_fabsf(z) * NEG_LOG2E), w = 1.0f + e, rest = e - (w - 1.0f);
+  slope = (z < 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(w);
+  return fmaxf(z, 0.0f) + __builtin_fmaf(__builtin_amdgcn_logf(w), 0.69314718055994530942f, rest);
 }
 __device__ __forceinline__ float softplus_of(float z) {
   float slope;
@@ -244,9 +243,10 @@ __device__ __forceinline__ void get_decays(float (&a2)[NL], const Args& a, const
 template <class T, int S>
 __device__ __forceinline__ void get_steps(const Args& a, const Place& p, int t, float bias, const Once<T, S>& x, const Once<T, S>& dt, Once<float, S>& slope,
                                           Once<float, S>& delta, Once<float, S>& u, Once<float, S>& input) {
+  const bool whole = t + U <= p.end;  // the same in all lanes
 #pragma unroll
   for (int i = 0; i < Own<S>::EACH; ++i) {
-    const bool there = p.mine && t + i * S + p.s < p.end;
+    const bool there = p.mine && (whole || t + i * S + p.s < p.end);
     const float z = (float)dt.v[i] + bias;
     slope.v[i] = 1.0f;
     delta.v[i] = there ? (a.softplus ? softplus_of(z, slope.v[i]) : z) : 0.0f;
