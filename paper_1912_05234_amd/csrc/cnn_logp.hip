@@ -208,18 +208,6 @@ __device__ __forceinline__ float kth_largest(const float (&v)[PER], int k) {
   return __uint_as_float(found & 0x80000000u ? found ^ 0x80000000u : ~found);
 }
 
-// Packs as they were loaded, sixteen-bit ones two elements to a register: what is widened before the fence is not kept for behind it.
-template <class P>
-__device__ __forceinline__ void forget(P& pack) {
-  if constexpr (sizeof(P) == 16) {
-    using Four = uint32_t __attribute__((ext_vector_type(4)));
-    Four w = __builtin_bit_cast(Four, pack);
-    uint32_t x = w[0], y = w[1], z = w[2], u = w[3];
-    asm volatile("" : "+v"(x), "+v"(y), "+v"(z), "+v"(u));
-    pack = __builtin_bit_cast(P, Four{x, y, z, u});
-  }
-}
-
 // One part of a row to THREADS lanes; where these are a wave or less, a workgroup has several rows.
 template <class T, int THREADS, int EACH, bool TOP>
 __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) __attribute__((amdgpu_waves_per_eu(EACH * sizeof(T) > 64 ? 4 : 8))) void logp_part_kernel(Args a) {

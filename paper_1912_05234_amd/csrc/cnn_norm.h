@@ -180,7 +180,8 @@ __global__ __launch_bounds__(threads_of(LANES)) void norm_backward_kernel(Args a
   constexpr int V = TY::PACK, TEAMS = threads_of(LANES) / LANES;
   using X = typename std::conditional<MODE == ADD, R, T>::type;  // of what was normalised
   using D = typename std::conditional<MODE == ADD, T, R>::type;  // of y
-  // Sixteen waves share the registers of a compute unit's four SIMDs: there weights and gates are taken again where they are used.
+  // Sixteen waves share the registers of a compute unit's four SIMDs: there weights and gates are taken again where they are used, and elements kept as they
+  // were loaded.
   constexpr bool KEEPS = LANES < 1024;
   __shared__ TeamSum<LANES, 2> shared;
   __shared__ float sums[TEAMS > 1 ? TEAMS * LANES * PACKS * V : 1];
@@ -208,7 +209,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void norm_backward_kernel(Args a
     const T* gate = static_cast<const T*>(a.gate.data) + n * a.gate.row + first;
     Loose<X, V> raw_x[PACKS];
     Loose<D, V> raw_d[PACKS];
-    Loose<typename std::conditional<MODE == ADD, R, T>::type, V> raw_z[PACKS];
+    Loose<typename std::conditional<MODE == ADD, R, T>::type, V> raw_z[PACKS] = {};
 #pragma unroll
     for (int p = 0; p < PACKS; ++p) {
       raw_x[p] = got_loose<V>(x + slot[p].at, slot[p].count, a.past_caches);
@@ -247,6 +248,9 @@ __global__ __launch_bounds__(threads_of(LANES)) void norm_backward_kernel(Args a
       float d_gate[V];
       if constexpr (!KEEPS) {
         get_loose(w[p], a.weight + first + slot[p].at, slot[p].count);
+        forget(raw_x[p]), forget(raw_d[p]), forget(raw_z[p]);
+        widen(v[p], raw_x[p]), widen(d[p], raw_d[p]);
+        if (MODE == ADD ? a.d_r.data : a.gate.data) widen(z[p], raw_z[p]);
 #pragma unroll
         for (int j = 0; j < V; ++j)
           if (MODE == GATE && a.gate.data) sigmoid[p][j] = logistic(z[p][j]);

@@ -120,6 +120,18 @@ __device__ __forceinline__ void put_loose(T* at, const float (&from)[N], int cou
   put_loose(at, from, count);
 }
 
+// Packs as they were loaded, sixteen-bit elements two to a register: what is widened before this is not kept in registers for behind it.
+template <class P>
+__device__ __forceinline__ void forget(P& pack) {
+  static_assert(sizeof(P) % 4 == 0, "packs of whole words");
+  struct All {
+    uint32_t w[sizeof(P) / 4];
+  } all = __builtin_bit_cast(All, pack);
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(P) / 4); ++i) asm volatile("" : "+v"(all.w[i]));
+  pack = __builtin_bit_cast(P, all);
+}
+
 // Calls fn with a value of the element type that `type` names.
 template <class FN>
 auto with_type(int type, FN fn) {
