@@ -241,8 +241,10 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) __attribute__((amdgp
   }
   Sums r{max_over<LANES>(mine), 0.0f, 0.0f};
   // Exponents d = x c - ref', one operation: ref' is ref c rounded, and what the rounding left out, ref c = ref' + rest, is the same for all of them.
+  // The largest exponent is rest, at most half a step of ref c: 2^-9 here, but 128 and more past 2^31, where exp2(rest) is no number.  Farther out (a large
+  // scale, or a wave whose logits are all masked by a large number) the difference comes first, exact where the exponential is not 0: an operation more.
   const float c = a.scale * LOG2E, ref = r.m == minus_infinity() ? 0.0f : r.m, ref_c = ref * c;
-  const bool far = !(__builtin_fabsf(ref_c) < 0x1p100f);  // (products past the range of numbers have no rest)
+  const bool far = !(__builtin_fabsf(ref_c) < 0x1p16f);
   const float rest = far ? 0.0f : __builtin_fmaf(ref, c, -ref_c);
 #pragma unroll
   for (int p = 0; p < PACKS; ++p) {
