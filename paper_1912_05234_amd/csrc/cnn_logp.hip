@@ -49,17 +49,20 @@ __device__ __forceinline__ float minus_infinity() { return -__builtin_inff(); }
 // e d for e = 2^d, which is 0 for d = -inf.  (A NaN of d is in e.)
 __device__ __forceinline__ float weighted(float e, float d) { return e * fmaxf(d, -1e30f); }
 
+// scale (l - base) from half the difference and twice the scale: rounded as the difference is, but a number where that passes the largest one.
+__device__ __forceinline__ float scaled_apart(float l, float base, float scale) { return __builtin_fmaf(l, 0.5f, -0.5f * base) * (2.0f * scale); }
+
 // The sums of a wave's pieces, one to a lane, relative to the largest maximum; c = scale log2(e).  Pieces without a possible token have
 // m = -inf, s = t = 0.
 __device__ __forceinline__ Sums joined(const Sums& a, float c) {
   const float m = max_over<64>(a.m), ref = m == minus_infinity() ? 0.0f : m;
-  const float d = (a.m - ref) * c, e = __builtin_amdgcn_exp2f(d);
+  const float d = scaled_apart(a.m, ref, c), e = __builtin_amdgcn_exp2f(d);
   return {m, sum_over<64>(a.s * e), sum_over<64>(e * (a.t + weighted(a.s, d)))};
 }
 // Pieces one after the other.
 __device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {
   const float m = fmaxf(a.m, b.m), ref = m == minus_infinity() ? 0.0f : m;
-  const float da = (a.m - ref) * c, db = (b.m - ref) * c;
+  const float da = scaled_apart(a.m, ref, c), db = scaled_apart(b.m, ref, c);
   const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
   return {m, a.s * ea + b.s * eb, ea * (a.t + weighted(a.s, da)) + eb * (b.t + weighted(b.s, db))};
 }
@@ -109,7 +112,7 @@ __device__ __forceinline__ float finish_row(const Args& a, const T* logits, int6
   }
   for (int j = lane; j < a.given; j += THREADS) {
     const Given g = j == lane ? first : got_given(a, logits, n, j);
-    a.log_probs[n * a.given + j] = g.known ? (g.logit - base) * a.scale - log_sum : 0.0f;
+    a.log_probs[n * a.given + j] = g.known ? scaled_apart(g.logit, base, a.scale) - log_sum : 0.0f;
   }
   return log_sum;
 }
@@ -118,7 +121,7 @@ __device__ __forceinline__ float finish_row(const Args& a, const T* logits, int6
 __device__ __forceinline__ void put_top(const Args& a, int64_t n, int rank, uint64_t key, const Sums& r, float log_sum) {
   const float base = r.m == minus_infinity() ? 0.0f : r.m;
   a.top_tokens[n * a.top + rank] = (int32_t)index_of(key);
-  a.top_log_probs[n * a.top + rank] = (value_of(key) - base) * a.scale - log_sum;
+  a.top_log_probs[n * a.top + rank] = scaled_apart(value_of(key), base, a.scale) - log_sum;
 }
 
 template <int LANES>
@@ -242,7 +245,8 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) __attribute__((amdgp
   Sums r{max_over<LANES>(mine), 0.0f, 0.0f};
   // Exponents d = x c - ref', one operation: ref' is ref c rounded, and what the rounding left out, ref c = ref' + rest, is the same for all of them.
   // The largest exponent is rest, at most half a step of ref c: 2^-9 here, but 128 and more past 2^31, where exp2(rest) is no number.  Farther out (a large
-  // scale, or a wave whose logits are all masked by a large number) the difference comes first, exact where the exponential is not 0: an operation more.
+  // scale, or a wave whose logits are all masked by a large number) the difference comes first, exact where the exponential is not 0
+  // (and past the largest number only where it is): an operation more.
   const float c = a.scale * LOG2E, ref = r.m == minus_infinity() ? 0.0f : r.m, ref_c = ref * c;
   const bool far = !(__builtin_fabsf(ref_c) < 0x1p16f);
   const float rest = far ? 0.0f : __builtin_fmaf(ref, c, -ref_c);
@@ -428,7 +432,7 @@ __global__ __launch_bounds__(THREADS > 64 ? THREADS : 256) void logp_backward_ke
   }
   const float by = a.scale, c = by * LOG2E, log2_sum = log_sum * LOG2E;
   const auto gradient = [&](float l, float g) {
-    const float z = (l - base) * c - log2_sum, p = __builtin_amdgcn_exp2f(z);
+    const float z = scaled_apart(l, base, c) - log2_sum, p = __builtin_amdgcn_exp2f(z);
     float d = g - p * total;
     if (a.d_entropy) d -= d_h * weighted(p, z * LN2 + h);
     return none ? 0.0f : by * d;

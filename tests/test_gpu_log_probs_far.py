@@ -1,4 +1,4 @@
-"""Log probabilities of logits and scales far from 1, all of them finite: masks that are numbers, temperatures next to 0.
+"""Log probabilities of logits and scales far from 1, all of them finite: masks that are numbers, temperatures next to 0, differences past the largest number.
 
 What counts are differences: the bounds are those of test_gpu_log_probs.py, in roundings of the scaled difference z to the row's largest logit, however large
 logits and scale are.  Where a single exponential and a factor behind the sum stand for exp(z), their exponents are off by at most 2^-9, which costs the
@@ -15,6 +15,7 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 # of a few lanes, a wave, several waves, a workgroup's last form, several parts
 VOCABULARIES = [3, 200, 5000, 32003, 70001]
+LOWEST = {"fp32": -torch.finfo(torch.float32).max, "bf16": -torch.finfo(torch.bfloat16).max, "fp16": -torch.finfo(torch.float16).max}
 
 
 def run(logits, tokens, type_, scale, top):
@@ -45,7 +46,7 @@ def test_masks_that_are_numbers(type_, value, scale, V):
 @pytest.mark.parametrize("scale", [1.0, 0.3, 1e5, 3e6])
 def test_masks_of_halves(scale, V):
     """Their lowest value is -65504: past 2^32 with such scales."""
-    run(*masked(V, -65504.0, torch.Generator().manual_seed(V)), "fp16", scale, min(V, 20))
+    run(*masked(V, LOWEST["fp16"], torch.Generator().manual_seed(V)), "fp16", scale, min(V, 20))
 
 
 @pytest.mark.parametrize("V", VOCABULARIES)
@@ -64,7 +65,7 @@ def test_temperatures_next_to_0(type_, scale, V):
 
 
 @pytest.mark.parametrize("V", VOCABULARIES)
-@pytest.mark.parametrize("size", [1e8, 1e10, 1e16, 1e25, 1e30])
+@pytest.mark.parametrize("size", [1e8, 1e10, 1e16, 1e25, 1e30, 3e38])
 @pytest.mark.parametrize("type_", ["fp32", "bf16"])
 def test_large_logits(type_, size, V):
     """A large maximum among ordinary logits; all of them large, alike to a few roundings or of either sign, at scales that leave differences of some units too."""
@@ -76,6 +77,21 @@ def test_large_logits(type_, size, V):
     logits[3] = (logits[3].clamp(-3, 3) / 3) * size
     tokens = torch.randint(0, V, (4, 2), generator=gen)
     for scale in (1.0, 30.0 / size):
+        if size * scale * 2 < 3e38:  # (else log probabilities are no numbers)
+            run(logits, tokens, type_, scale, min(V, 5))
+
+
+@pytest.mark.parametrize("V", VOCABULARIES)
+@pytest.mark.parametrize("type_", ["fp32", "bf16"])
+def test_differences_past_the_largest_number(type_, V):
+    """The type's lowest value and its largest in one row: their difference is no number, its product with a scale below 1/2 is one."""
+    gen = torch.Generator().manual_seed(V)
+    logits = torch.where(torch.rand(3, V, generator=gen) < 0.5, LOWEST[type_], -LOWEST[type_])
+    logits[0] = LOWEST[type_]
+    logits[0, V // 2] = -LOWEST[type_]
+    logits[:, 0] = LOWEST[type_]
+    tokens = torch.stack([torch.zeros(3, dtype=torch.int64), torch.full((3,), V // 2)], 1)
+    for scale in (0.4, 1e-30, 1e-38):
         run(logits, tokens, type_, scale, min(V, 5))
 
 
