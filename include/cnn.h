@@ -336,7 +336,7 @@ int cnn_linear_attention_step(const cnn_linear_shape* shape, const cnn_heads* q,
 /* Norms around a block, for rows of groups * width elements: n = v / sqrt(mean(v^2) + eps) for each group of `width` consecutive ones, times
  * weight[groups * width] (fp32).  Two element types: `type` of what goes into and comes out of the block, `stream_type` (the same, or
  * CNN_F32) of the residual stream.  Inputs are given with the distance of their rows, in elements, not negative, and need only be aligned to
- * their element; results are contiguous.  1 <= rows < 2^31, 1 <= width <= 16384, groups * width <= 2^20, 0 < eps.  Elements whose square's
+ * their element; results are contiguous.  1 <= rows < 2^31, 1 <= width <= 16384, groups * width <= 2^20, 2^-126 <= eps <= 1e30, |scale| <= 1e30.  Elements whose square's
  * sum over a group is not below 2^128 make the group's results meaningless; a NaN or an infinity stays in its group (and, backward, in
  * d_weight).  Weight gradients are fp32 sums in an order that the shape fixes. */
 typedef struct {

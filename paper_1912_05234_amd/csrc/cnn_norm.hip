@@ -14,10 +14,11 @@ struct PutWeight {
   __device__ void operator()(int64_t c, float sum) const { d_weight[c] = sum; }
 };
 
+// (The hardware's root takes a number below 2^-126 for 0: a smaller eps would make rows of zeros NaN.)
 bool shape_ok(const cnn_norm_shape* s) {
   return s && s->rows >= 1 && s->rows < (int64_t)1 << 31 && s->groups >= 1 && s->width >= 1 && s->width <= MOST_WIDTH &&
          (int64_t)s->groups * s->width <= MOST_COLUMNS && type_known(s->type) && (s->stream_type == s->type || s->stream_type == CNN_F32) &&
-         s->eps > 0.0f && s->eps <= 1e30f && __builtin_fabsf(s->scale) <= 1e30f;
+         s->eps >= 0x1p-126f && s->eps <= 1e30f && __builtin_fabsf(s->scale) <= 1e30f;
 }
 
 bool rows_ok(const cnn_rows* r, int type) {
