@@ -357,20 +357,21 @@ int cnn_add_norm_fwd(const cnn_norm_shape* shape, const cnn_rows* x, const cnn_r
 size_t cnn_norm_bwd_workspace_bytes(const cnn_norm_shape* shape);
 int cnn_add_norm_bwd(const cnn_norm_shape* shape, const cnn_rows* d_y, const cnn_rows* r, const cnn_rows* d_r, const float* weight, void* d_x,
                      void* d_residual, float* d_weight, void* workspace, size_t workspace_bytes, void* hip_stream);
-/* Behind a block: y = residual + scale * n w silu(gate) with n of x and silu(z) = z / (1 + exp(-z)); gate (of `type`) and residual (of stream_type) may be
- * NULL (a factor of 1; 0).  y is of stream_type. */
+/* Behind a block: y = residual + scale * n w silu(gate) with n of x and silu(z) = z / (1 + exp(-z)), 0 where 1 / (1 + exp(-z)) is below 2^-126; gate (of `type`)
+ * and residual (of stream_type) may be NULL (a factor of 1; 0).  y is of stream_type. */
 int cnn_norm_gate_fwd(const cnn_norm_shape* shape, const cnn_rows* x, const cnn_rows* gate, const cnn_rows* residual, const float* weight, void* y,
                       void* hip_stream);
 /* d_x, d_gate (NULL where the gate is) and d_weight for the error d_y (of stream_type) of y.  (The residual's gradient is d_y itself.) */
 int cnn_norm_gate_bwd(const cnn_norm_shape* shape, const cnn_rows* d_y, const cnn_rows* x, const cnn_rows* gate, const float* weight, void* d_x,
                       void* d_gate, float* d_weight, void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* Log probabilities of rows of logits l[vocab]: ln p_v = scale * l_v - ln sum exp(scale * l), scale > 0 (an inverse temperature).
+/* Log probabilities of rows of logits l[vocab]: ln p_v = scale * l_v - ln sum exp(scale * l), 0 < scale <= 1e30 (an inverse temperature).
  *   log_probs[rows,given]   ln p of the tokens[rows,given] (int32, or int64 with wide_tokens != 0); 0 for a token outside 0 .. vocab-1 (padding)
  *   entropy[rows]           - sum p ln p (nullable)
  *   top_tokens, top_log_probs[rows,top]   the `top` largest logits in descending order, equal ones (0 and -0 among them) in the order of their tokens
  *   stats[rows,3]           what the backward call needs: max l, ln sum exp(scale * (l - max)), the entropy (nullable)
- * Results are fp32; the sum is one of fp32 numbers, so a log probability or entropy next to 0 is exact to some 2^-22, not relative to itself.  A logit of -inf is an impossible token: p = 0.  A row of nothing else has log_probs and top_log_probs of -inf and an entropy of 0,
+ * Results are fp32; the sum is one of fp32 numbers, so a log probability or entropy next to 0 is exact to some 2^-22, not relative to itself; a
+ * probability below 2^-126 counts as 0 in sums and gradients.  A logit of -inf is an impossible token: p = 0.  A row of nothing else has log_probs and top_log_probs of -inf and an entropy of 0,
  * and its gradient is zero.  A NaN or +inf makes its row's results NaN, except that top_tokens are tokens of the row and padding's log_probs are 0.
  * 1 <= rows < 2^31, 1 <= vocab <= 2^24, 1 <= given <= 256, 0 <= top <= min(64, vocab).  Logits as a cnn_rows of `type`;
  * tokens, stats and the errors need only be aligned to their element. */
@@ -388,7 +389,7 @@ int cnn_log_probs_fwd(const cnn_log_probs_shape* shape, const cnn_rows* logits, 
 int cnn_log_probs_bwd(const cnn_log_probs_shape* shape, const cnn_rows* logits, const void* tokens, const float* stats, const float* d_log_probs,
                       const float* d_entropy, void* d_logits, void* hip_stream);
 
-/* Causal convolution of K taps along each channel: p_t = bias + sum_k weight[d,k] x_{t-K+1+k}, y = p, or silu(p) = p / (1 + exp(-p)) with silu != 0.
+/* Causal convolution of K taps along each channel: p_t = bias + sum_k weight[d,k] x_{t-K+1+k}, y = p, or silu(p) = p / (1 + exp(-p)) with silu != 0 (as above).
  * weight[D,K] and bias[D] (nullable) are fp32.  x (and d_y) of `type` with their strides, in elements, none negative, aligned to their element; y and d_x
  * are contiguous, [B,T,D].  A state [B,K-1,D] of `type` holds a sequence's last K - 1 inputs, the newest last: what stands before its first token
  * (initial_state, nullable: zeros), and what it leaves (final_state, nullable: not wanted), of a short sequence the initial state's rest too.  They may not be the
@@ -422,9 +423,10 @@ int cnn_causal_conv_step(const cnn_causal_conv_shape* shape, const cnn_tokens* x
  * consecutive channels to a group.  Results y, d_x, d_dt [B,T,D] and
  * d_b, d_c [B,T,G,N] are contiguous; states [B,D,N] are fp32, an initial or final one may be NULL (zero; not wanted), and they may be the same memory.  lengths
  * as for cnn_causal_conv_fwd.  1 <= N <= 128, B * D <= 2^24, B * T < 2^31 - 64, D <= 2^20.  Inputs up to a sequence's length must be finite: one that is not
- * makes results NaN that the formulas leave finite, also of tokens before it, of its own channel and, backward, its group's d_b and d_c.  Everything is
- * computed in fp32 and rounded once; a decay below 2^-126 counts as 0.  `workspace` holds states of pieces of the sequences, and backward partial sums; its size query returns 0 where none is
- * needed and for refused shapes. */
+ * makes results NaN that the formulas leave finite, also of tokens before it, of its own channel and, backward, its group's d_b and d_c.  So do an a of 2^127 and more
+ * in magnitude, and decays above 1 whose product over any tokens of a sequence passes 2^128.  Everything is computed in fp32 and rounded once; a decay below
+ * 2^-126 counts as 0.  `workspace` holds states of pieces of the sequences, and backward partial sums; its size query returns 0 where none is needed and for
+ * refused shapes. */
 typedef struct {
   int B, T, D, N, G, type, softplus;
 } cnn_selective_scan_shape;

@@ -15,7 +15,8 @@
 //
 // Measured: 8191 rows of 32003 bfloat16 150 us forward (524 MB; the vector unit's share, an exponential and some six operations an element, is
 // 60 of them), 187 with five top tokens, 181 backward (1.05 GB, 5.8 TB/s, past the caches); 64 rows of 50021 with twenty top tokens 14.7: one workgroup to a
-// row, a chain of loads, sums and barriers; 78400 rows of 256 19 and 21.
+// row, a chain of loads, sums and barriers; 78400 rows of 256 19 (8 at a copy's rate) and 21.  Forward no load is on its way while a row's exponentials are
+// computed: memory's time and the vector unit's nearly add up.
 #include "cnn_common.h"
 #include "cnn_lanes.h"
 #include "cnn_types.h"

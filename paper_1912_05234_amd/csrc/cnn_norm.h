@@ -14,6 +14,9 @@
 // kernel, in an order that the shape alone fixes.  16381 rows of 2048 bfloat16 with a stream of floats, backward (537 MB), take 90 us: 85 at 6.3 TB/s and
 // 4.5 for the second kernel (a copy of 1 GiB reaches 5.2); 78400 rows of 2 x 64 floats behind a gate, backward (201 MB), 44; 64 rows of 64 floats
 // 5.5, the call.
+//
+// Groups of more than 8192 elements, whose sixteen waves leave 128 registers to a lane, spill: backward 20 to 105 of them (4000 rows of 12000 floats behind a gate 543
+// us of 185 at a copy's rate, 4000 of 16384 bfloat16 with a stream of floats 356 of 202), forward 6 to 17 behind a gate with a stream of floats (116 of 111).
 #pragma once
 
 #include "cnn_common.h"

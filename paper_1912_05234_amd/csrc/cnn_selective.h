@@ -601,7 +601,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NL =
 // ---- launches, one source to an element type ---------------------------------------------------------------------------------
 enum Pass { TOKENS, ENDS, ENDS_AND_ERRORS, GRADIENT };
 
-// Of a workgroup of the backward pass, by the states that a channel's lanes hold: as many as LDS holds checkpoints and sums of two workgroups for.
+// Of a workgroup of the backward pass, by the states that a channel's lanes hold.  Checkpoints, sums and rows take 35 to 42 KB of LDS up to 16 states, 28 up to
+// 32; beyond, with one wave, 24 and 48 KB, of which a compute unit holds six and three.  More waves there are not measured: they would have fewer
+// workgroups' sums of d_b and d_c to add (4 x 1000 tokens of 256 x 16 states take 48 us, of 32 88, of 64 213, of 128 593).
 constexpr int waves_of(int states) { return states <= 16 ? 4 : states <= 32 ? 2 : 1; }
 
 struct Form {  // states to a lane, lanes to a channel
@@ -615,7 +617,8 @@ void launch_f16(const Args& a, Pass pass, Form f, dim3 grid, hipStream_t st);
 template <class T, int NL, int S>
 void launch_form(const Args& a, Pass pass, dim3 grid, hipStream_t st) {
   // Backward a lane has four states, whose U tokens, with their decays, are 64 registers (eight, with 128, spill: 100 x 784 tokens of 128 x 16 states took
-  // 410 us that way and 259 this way); eight only where a channel has more than 16 lanes hold.  Forward eight,
+  // 410 us that way and 259 this way; here 10 registers spill, 14 to 22 where a channel has one lane or eight); eight only where a channel has more than 16 lanes
+  // hold.  Forward eight,
   // which share a token's work on its channel among more states (a prompt of 2 x 4096 tokens of 2048 x 16 states: 147 us, and 150 with four),
   // or four where there are no more or more waves are wanted.
   if constexpr (NL == 4 || S == 16) {

@@ -8,7 +8,8 @@
 // read twice (from the caches).  Backward it recomputes p, keeps the last K - 1 errors d_p beside the inputs, and a chunk goes K - 1
 // tokens past its end for them.  The weights' gradients are summed in registers over a chunk, over a workgroup's chunks in LDS, and
 // over workgroups by a second kernel, in an order that the shape alone fixes.  100 sequences of up to 784 tokens of 128 floats (60 MB) take 14.8 us forward;
-// 4 x 4093 x 2048 bfloat16 backward (201 MB) 66: its 200 registers leave two waves to a SIMD, too few to keep memory busy.
+// 4 x 4093 x 2048 bfloat16 backward (201 MB) 66: two waves to a SIMD, as many as the launch has (159 registers, floats 168, would leave three), wait for half of
+// their time, and the 31 us in which the vector unit issues are only partly those in which memory moves its 39.
 #include <utility>
 
 #include "cnn_common.h"
