@@ -236,6 +236,7 @@ __global__ __launch_bounds__(THREADS) void conv_tokens_backward_kernel(Args a) {
           for (int k = 0; k < K; ++k) sum += w[K - 1 - k][j] * error[i + k][j];
           out[j] = sum;
         }
+        if constexpr (std::is_same<T, _Float16>::value) as_floats(out);
         if constexpr (INSIDE) {
           put_loose(d_x + u * a.D, out, V);
           continue;

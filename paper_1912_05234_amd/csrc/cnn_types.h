@@ -132,6 +132,14 @@ __device__ __forceinline__ void forget(P& pack) {
   pack = __builtin_bit_cast(P, all);
 }
 
+// Elements as the floats that they are: a product and sum whose result is stored as a half may else be rounded to that at once, not to a float first, where
+// nothing comes between, and a result would depend on the path that it takes (an ulp of one half in 2^14).
+template <int N>
+__device__ __forceinline__ void as_floats(float (&v)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) asm("" : "+v"(v[j]));
+}
+
 // Calls fn with a value of the element type that `type` names.
 template <class FN>
 auto with_type(int type, FN fn) {
